@@ -440,7 +440,7 @@ def _extend_plain(s):
     free = torch.nonzero(refs == 0)[:, 0]
     wanted = torch.where(fits, need, 0)
     last = torch.cumsum(wanted, 0)
-    served = fits & (last <= free.numel())
+    served = fits & ((need == 0) | (last <= free.numel()))
     block = torch.arange(table.shape[1], device=table.device)
     fresh = served[:, None] & (block >= old[:, None]) & (block < (old + need)[:, None])
     order = (last - wanted)[:, None] + block - old[:, None]
