@@ -1,0 +1,663 @@
+// Attention of new tokens over a cache in pages.
+//
+// The rows of one cache head are the new tokens' query heads that read it:
+// row r of a sequence is (token r / G, head r % G of the group), so a group of
+// heads shares every key that is loaded.  A workgroup takes a block of rows and
+// a range of keys, walks the range in tiles with the running maximum m and sum
+// l of the softmax, and keeps everything transposed:
+//     S^T = K Q^T   (A = K rows from LDS, B = Q in registers)
+//     O^T += V^T P^T (A = V^T from LDS by transposing reads, B = P)
+// so that a row is a column (lane & 15) of every accumulator: its maximum and
+// sum take two lane exchanges a tile, its rescaling none, and the accumulator
+// tiles of S^T are, as they stand, the B operand of the second product (the
+// permuted contraction order of gdn_device.h).
+//
+// Two kernels from one body:
+//   k_attn_tile  many rows: 4 waves with 32 rows each share a tile of keys;
+//   k_attn_few   few rows (at most 32): 4 waves share the rows, each walks its
+//                own keys of a tile and the results are joined in LDS.
+// Where the row blocks do not fill the GPU, a block's keys are split over
+// several workgroups, whose unnormalised sums k_attn_join adds.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "gdn_device.h"
+#include "gdn_paged_kernels.h"
+
+namespace gdn {
+
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+#define LDS_AS __attribute__((address_space(3)))
+#define CONST_AS __attribute__((address_space(4)))
+
+// 64 lanes x 16 bytes from base + off (bytes, one per lane) straight into LDS
+// at lds + lane * 16; base and lds are the same for the whole wave.  As
+// dma_frag: the caller waits.
+__device__ inline void dma_rows(const unsigned char* base, unsigned off, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base)
+               : "memory");
+}
+
+// One row block's place in the problem.
+struct Block {
+  int n, hk;          // sequence, cache head
+  int q0, m;          // first token row of the sequence, its new tokens
+  int kv;             // its cached tokens
+  int r0, r1;         // rows [r0, r1) of the m * G
+  int seen, hi;       // keys that some row sees lie in [seen, hi)
+  int lo;             // seen, down to a multiple of 16
+  // first and one past the last key that token i sees
+  __device__ int first(const AttnArgs& a, int i) const {
+    return a.window > 0 ? max(0, kv - m + i - a.window + 1) : 0;
+  }
+  __device__ int last(const AttnArgs& a, int i) const {
+    return a.causal ? max(0, kv - m + i + 1) : kv;
+  }
+  __device__ void range(const AttnArgs& a) {
+    seen = first(a, r0 / a.G);
+    lo = seen & ~15;
+    hi = min(kv, last(a, (r1 - 1) / a.G));
+  }
+};
+
+template <class E, int D, int QT, int RW, int KW, int KT> struct AttnCfg {
+  static constexpr int NK = KT / KW;                // keys of a wave
+  static constexpr int NTH = 64 * RW * KW;
+  static constexpr int RB = D * (int)sizeof(E);     // bytes of a key
+  static constexpr int NP = RB / 16;                // 16-byte pieces of it
+  static constexpr int ROWS = RW * QT * 16;
+  static constexpr int TILE = KT * RB;              // bytes of a tile of k (or v)
+  static constexpr int JOIN = KW > 1 ? KW * ROWS * (D + 2) * 4 : 0;
+  static constexpr int LDS = 4 * TILE > JOIN ? 4 * TILE : JOIN;
+  static constexpr int RPI = 64 / NP;               // keys of one wave-wide copy
+  static_assert(NK % 16 == 0 && KT % 16 == 0, "a wave works on whole groups of 16 keys");
+};
+
+// Place of 16-byte piece p of key row r in a tile: the pieces of a row are
+// exchanged by an XOR that spreads the rows a read touches over the banks.
+// K is read 16 rows at a time, the same piece of each: 16 different pieces.
+template <int NP> __device__ inline int k_swz(int r) { return NP >= 16 ? r & 15 : (r >> 1) & 7; }
+// bf16 V is read two neighbouring pieces of 4 rows by 16 lanes (8 rows by 32),
+// fp32 V four neighbouring pieces of rows 4 apart.
+template <class E, int NP> __device__ inline int v_swz(int r) {
+  if constexpr (sizeof(E) == 4) return ((r >> 2) & 3) << 2;
+  return NP >= 16 ? (r & 7) << 1 : ((r >> 1) & 3) << 1;
+}
+
+template <class E> struct Piece;  // 16 bytes of channels and their products
+template <> struct Piece<bf16> {
+  using type = bf16x8;
+  __device__ static inline f32x4 mma(type a, type b, f32x4 c) { return Mfma<bf16>::mma(a, b, c); }
+};
+template <> struct Piece<float> {
+  using type = f32x4;
+  __device__ static inline f32x4 mma(type a, type b, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = Mfma<float>::mma(a[j], b[j], c);
+    return c;
+  }
+};
+
+template <class E> __device__ inline bool finite4(const uint4& x) {
+  const unsigned w[4] = {x.x, x.y, x.z, x.w};
+  bool ok = true;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(E) == 4)
+      ok = ok && (w[i] & 0x7f800000u) != 0x7f800000u;
+    else
+      ok = ok && (w[i] & 0x7f80u) != 0x7f80u && (w[i] & 0x7f800000u) != 0x7f800000u;
+  }
+  return ok;
+}
+
+template <class E, int D, int QT, int RW, int KW, int KT>
+__device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
+                                  unsigned char* smem) {
+  using C = AttnCfg<E, D, QT, RW, KW, KT>;
+  using P = Piece<E>;
+  constexpr int NK = C::NK, NT = NK / 16, RB = C::RB, NP = C::NP, KB = RB / 64, DT = D / 16;
+  const int lane = lane_id(), g = lane >> 4, c16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = KW == 1 ? wave : 0, kw = KW == 1 ? 0 : wave;
+
+  // the last range goes to the end, however long the cache has become
+  const int begin = b.lo + split * a.len;
+  const int end = split == a.splits - 1 ? b.hi : min(b.hi, begin + a.len);
+
+  // this lane's rows: Q in registers, the keys each sees
+  typename P::type q[QT][KB];
+  int first[QT], last[QT];
+  const int wr0 = b.r0 + rw * QT * 16;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = wr0 + t * 16 + c16;
+    const bool real = r < b.r1;
+    const int i = real ? r / a.G : 0, h = b.hk * a.G + (real ? r - i * a.G : 0);
+    const unsigned char* p = a.q.data + (int64_t)(b.q0 + i) * a.q.ts + h * a.q.hs;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (real) x = *reinterpret_cast<const uint4*>(p + (4 * kb + g) * 16);
+      q[t][kb] = *reinterpret_cast<typename P::type*>(&x);
+    }
+    first[t] = b.first(a, i);
+    last[t] = real ? min(b.kv, b.last(a, i)) : 0;
+  }
+  // over the block's and the wave's rows: the keys that all of them see
+  const int all_lo = b.first(a, (b.r1 - 1) / a.G), all_hi = min(b.kv, b.last(a, b.r0 / a.G));
+  const int we = min(b.r1, wr0 + QT * 16) - 1;
+  const bool idle = wr0 >= b.r1;
+  const int w_lo = idle ? 0 : b.first(a, we / a.G), w_hi = idle ? 0 : b.last(a, wr0 / a.G);
+  const int w_end = idle ? 0 : b.last(a, we / a.G), w_begin = idle ? 0 : b.first(a, wr0 / a.G);
+
+  f32x4 o[DT][QT];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const CONST_AS int* pages = (const CONST_AS int*)(a.cache.table + (int64_t)b.n * a.cache.max_blocks);
+  const int shift = a.cache.shift, mask = (1 << shift) - 1;
+  const unsigned char* const kbase = a.cache.k + (int64_t)b.hk * a.cache.head;
+  const unsigned char* const vbase = a.cache.v + (int64_t)b.hk * a.cache.head;
+  const unsigned lds0 = (unsigned)(uintptr_t)smem;
+
+  // page of the group of 16 keys from key0 on; -1 past the end or for a hole
+  auto page_of = [&](int key0) -> int {
+    if (key0 >= end) return -1;
+    const int p = pages[__builtin_amdgcn_readfirstlane(key0) >> shift];
+    return (unsigned)p < (unsigned)a.cache.num_pages ? p : -1;
+  };
+  // this wave's copies of the tile from key k0 on: groups of 16 keys, of k and
+  // of v (a group that is not there is read from page 0 and not used)
+  unsigned koff[16 / C::RPI], voff[16 / C::RPI];
+#pragma unroll
+  for (int j = 0; j < 16 / C::RPI; ++j) {
+    const int r = j * C::RPI + lane / NP, p = lane % NP;
+    koff[j] = r * (unsigned)a.cache.slot + ((p ^ k_swz<NP>(r)) << 4);
+    voff[j] = r * (unsigned)a.cache.slot + ((p ^ v_swz<E, NP>(r)) << 4);
+  }
+  auto copy_tile = [&](int k0, int buf) {
+    constexpr int GROUPS = KT / 16;
+    constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int grp = KW == 1 ? wave + i * RW : wave * NT + i;
+      if (grp >= GROUPS) break;
+      const int key0 = k0 + 16 * grp;
+      const int page = max(0, page_of(key0));
+      const int64_t off = (int64_t)page * a.cache.page + (int64_t)(key0 & mask) * a.cache.slot;
+      const unsigned dst = lds0 + buf * 2 * C::TILE + grp * 16 * RB;
+#pragma unroll
+      for (int j = 0; j < 16 / C::RPI; ++j) dma_rows(kbase + off, koff[j], dst + j * 1024);
+#pragma unroll
+      for (int j = 0; j < 16 / C::RPI; ++j)
+        dma_rows(vbase + off, voff[j], dst + C::TILE + j * 1024);
+    }
+  };
+
+  const int tiles = (end - begin + KT - 1) / KT;
+  if (tiles > 0) copy_tile(begin, 0);
+  for (int it = 0; it < tiles; ++it) {
+    const int k0 = begin + it * KT;
+    const int kw0 = k0 + kw * NK;  // this wave's keys
+    unsigned char* const kt = smem + (it & 1) * 2 * C::TILE;
+    unsigned char* const vt = kt + C::TILE;
+    // the tile is there, the other buffer no longer read
+    wait_vmcnt<0>();
+    if (KW == 1)
+      lds_barrier();
+    else
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (it + 1 < tiles) copy_tile(k0 + KT, (it + 1) & 1);
+
+    // groups that are not there
+    unsigned gone = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      if (page_of(kw0 + 16 * t) < 0) gone |= 1u << t;
+    // Keys that no row sees may hold anything: their v is cleared.  Where some
+    // rows see a key and others do not, an infinity or NaN in its v must not
+    // meet a p of zero: those tiles take the product key by key.
+    bool odd = false;
+    const int f0 = KW == 1 ? k0 : kw0;
+    if (f0 + NK > min(all_hi, end) || f0 < all_lo || gone) {
+      bool bad = false;
+      constexpr int STEP = KW == 1 ? C::NTH : 64;
+      const int tid = KW == 1 ? (int)threadIdx.x : lane;
+#pragma unroll 1
+      for (int i = tid; i < NK * NP; i += STEP) {
+        const int r = i / NP, key = f0 + r;
+        uint4* p = reinterpret_cast<uint4*>(vt + kw * NK * RB + i * 16);
+        if (key >= end || key < b.seen || (gone >> (r >> 4) & 1))
+          *p = make_uint4(0, 0, 0, 0);
+        else
+          bad = bad || !finite4<E>(*p);
+      }
+      if (KW == 1)
+        odd = __syncthreads_or(bad);
+      else
+        odd = __ballot(bad) != 0;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    if (idle || kw0 >= min(w_end, end) || kw0 + NK <= w_begin) continue;  // nothing seen
+
+    // S^T
+    f32x4 s[NT][QT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < QT; ++u) s[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const unsigned char* krow = kt + (kw * NK + c16) * RB;
+    const int ks = k_swz<NP>(c16);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const auto x = *reinterpret_cast<const typename P::type*>(
+            krow + t * 16 * RB + (((4 * kb + g) ^ ks) << 4));
+#pragma unroll
+        for (int u = 0; u < QT; ++u) s[t][u] = P::mma(x, q[u][kb], s[t][u]);
+      }
+    }
+    // what a row does not see
+    const bool partial = kw0 + NK > min(w_hi, end) || kw0 < w_lo || gone;
+    if (partial) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = kw0 + 16 * t + 4 * g + e;
+#pragma unroll
+          for (int u = 0; u < QT; ++u)
+            if (key >= min(last[u], end) || key < first[u] || (gone >> t & 1)) s[t][u][e] = -INFINITY;
+        }
+    }
+    // running softmax in base 2
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][u][e]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float mn = fmaxf(m[u], mx * a.c);
+      const float ref = mn == -INFINITY ? 0.f : mn;  // nothing seen so far: all p are 0
+      if (__any(mn > m[u])) {
+        const float al = __builtin_amdgcn_exp2f(m[u] - ref);
+        l[u] *= al;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[d][u][e] *= al;
+        m[u] = mn;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[t][u][e], a.c, -ref));
+          s[t][u][e] = p;
+          sum += p;
+        }
+      l[u] += sum;
+    }
+    // O^T
+    unsigned char* const vw = vt + kw * NK * RB;
+    if (odd) {
+#pragma unroll 1
+      for (int k = 0; k < NK; ++k) {
+        const int key = kw0 + k;
+        float p[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+          float x = 0.f;
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (16 * t + e == (k & ~12)) x = s[t][u][e];
+          p[u] = __shfl(x, ((k >> 2) & 3) * 16 + c16);
+        }
+        const bool there = key < end && !(gone >> (k >> 4) & 1);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const int ch = (16 * d + 4 * g) * (int)sizeof(E);
+          const f32x4 x = load4<E>(reinterpret_cast<const E*>(
+              vw + k * RB + (((ch >> 4) ^ v_swz<E, NP>(k)) << 4) + (ch & 15)));
+#pragma unroll
+          for (int u = 0; u < QT; ++u)
+            if (there && key < last[u] && key >= first[u])
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[d][u][e] = fmaf(p[u], x[e], o[d][u][e]);
+        }
+      }
+    } else if constexpr (sizeof(E) == 4) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const unsigned char* row = vw + (16 * t + 4 * g + e) * RB;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const float x = *reinterpret_cast<const float*>(
+                row + (((4 * d + (c16 >> 2)) ^ (g << 2)) << 4) + (c16 & 3) * 4);
+#pragma unroll
+            for (int u = 0; u < QT; ++u) o[d][u] = Mfma<float>::mma(x, s[t][u][e], o[d][u]);
+          }
+        }
+    } else {
+      // lane i of 16 points at 4 channels of key row i / 4 and receives one
+      // channel (its own, i) of the 4 rows
+      const int vr = 4 * g + (c16 >> 2);
+      unsigned char* const row = vw + vr * RB + (c16 & 1) * 8;
+      const int vs = ((c16 >> 1) & 1) ^ v_swz<E, NP>(vr);
+      auto turned = [&](int t, int d) {
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (LDS_AS s16x4*)(row + t * 16 * RB + (((2 * d) ^ vs) << 4)));
+      };
+      if constexpr (NT == 1) {
+        s16x4 p[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+          const bf16x4 x = {(bf16)s[0][u][0], (bf16)s[0][u][1], (bf16)s[0][u][2], (bf16)s[0][u][3]};
+          p[u] = *reinterpret_cast<const s16x4*>(&x);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const s16x4 x = turned(0, d);
+#pragma unroll
+          for (int u = 0; u < QT; ++u)
+            o[d][u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p[u], o[d][u], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
+          bf16x8 p[QT];
+#pragma unroll
+          for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              p[u][e] = (bf16)s[t][u][e];
+              p[u][4 + e] = (bf16)s[t + 1][u][e];
+            }
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const s16x4 x0 = turned(t, d), x1 = turned(t + 1, d);
+            const s16x8 x = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+              o[d][u] = Mfma<bf16>::mma(*reinterpret_cast<const bf16x8*>(&x), p[u], o[d][u]);
+          }
+        }
+      }
+    }
+  }
+
+  // the row's sum over the four lane groups
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    l[u] += __shfl_xor(l[u], 16);
+    l[u] += __shfl_xor(l[u], 32);
+  }
+
+  const int64_t rows = (int64_t)a.tok.total * a.Hq;
+  // channels ch.. of row r, unnormalised sums x, maximum and sum mm, ll
+  auto put = [&](int r, int ch, f32x4 x, float mm, float ll) {
+    const int i = r / a.G, h = b.hk * a.G + r - i * a.G;
+    const int64_t at = (int64_t)(b.q0 + i) * a.Hq + h;
+    if (a.splits > 1) {
+      const int64_t w = split * rows + at;
+      *reinterpret_cast<f32x4*>(a.part + w * D + ch) = x;
+      if (ch == 0) {
+        a.part_ml[2 * w] = mm;
+        a.part_ml[2 * w + 1] = ll;
+      }
+      return;
+    }
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    E* p = reinterpret_cast<E*>(a.o.data + (int64_t)(b.q0 + i) * a.o.ts + h * a.o.hs) + ch;
+    if constexpr (sizeof(E) == 4) {
+      *reinterpret_cast<f32x4*>(p) = f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    } else {
+      const bf16x4 y = {(bf16)(x[0] * inv), (bf16)(x[1] * inv), (bf16)(x[2] * inv),
+                        (bf16)(x[3] * inv)};
+      *reinterpret_cast<bf16x4*>(p) = y;
+    }
+    if (ch == 0 && a.lse)
+      a.lse[at] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
+  };
+
+  if constexpr (KW == 1) {
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      const int r = wr0 + u * 16 + c16;
+      if (r < b.r1)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) put(r, 16 * d + 4 * g, o[d][u], m[u], l[u]);
+    }
+  } else {
+    // join the waves' sums in LDS
+    constexpr int R = C::ROWS;
+    float* sum = reinterpret_cast<float*>(smem);
+    float* ml = sum + KW * R * D;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      const int r = u * 16 + c16;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        *reinterpret_cast<f32x4*>(sum + ((kw * R + r) * D + 16 * d + 4 * g)) = o[d][u];
+      if (g == 0) {
+        ml[(kw * R + r) * 2] = m[u];
+        ml[(kw * R + r) * 2 + 1] = l[u];
+      }
+    }
+    __syncthreads();
+    const int nr = b.r1 - b.r0;
+    for (int i = threadIdx.x; i < nr * (D / 4); i += C::NTH) {
+      const int r = i / (D / 4), ch = (i - r * (D / 4)) * 4;
+      float mx = -INFINITY, ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) mx = fmaxf(mx, ml[(w * R + r) * 2]);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float al = __builtin_amdgcn_exp2f(ml[(w * R + r) * 2] - ref);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(sum + ((w * R + r) * D + ch));
+        ll += al * ml[(w * R + r) * 2 + 1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += al * y[e];
+      }
+      put(b.r0 + r, ch, x, mx, ll);
+    }
+  }
+}
+
+// Few rows: one row block per sequence and cache head, its keys split.
+// Grid: ((n * splits + split) * Hk + hk).
+template <class E, int D, int QT, int KW, int KT>
+__global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
+  using C = AttnCfg<E, D, QT, 1, KW, KT>;
+  __shared__ __align__(1024) unsigned char smem[C::LDS];
+  Block b;
+  b.hk = blockIdx.x % a.Hk;
+  const int rest = blockIdx.x / a.Hk, split = rest % a.splits;
+  b.n = rest / a.splits;
+  b.q0 = seq_start(a.tok, b.n);
+  b.m = seq_start(a.tok, b.n + 1) - b.q0;
+  b.r0 = 0;
+  b.r1 = b.m * a.G;
+  if (b.m == 0 || b.r1 > C::ROWS) return;
+  b.kv = cached(a.cache, b.n);
+  b.range(a);
+  // a range past the keys: no partial result is read there
+  if (split > 0 && b.lo + split * a.len >= b.hi) return;
+  attn_block<E, D, QT, 1, KW, KT>(a, b, split, smem);
+}
+
+// Many rows.  Grid: ((slot * splits + split) * Hk + hk); the sequence and row
+// block of a slot follow from the boundaries: sequence n's slots begin at
+// floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
+// the next one's.
+template <class E, int D, int KT>
+__global__ __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) void k_attn_tile(AttnArgs a,
+                                                                                int slots) {
+  using C = AttnCfg<E, D, 2, 4, 1, KT>;
+  static_assert(C::ROWS == TILE_ROWS, "row block");
+  __shared__ __align__(1024) unsigned char smem[C::LDS];
+  Block b;
+  b.hk = blockIdx.x % a.Hk;
+  const int rest = blockIdx.x / a.Hk, split = rest % a.splits;
+  // the last row blocks see the most keys: they go first
+  const int slot = slots - 1 - rest / a.splits;
+  int tile;
+  if (a.tok.cu) {
+    const int64_t G = a.G;
+    int lo = 0, hi = a.tok.N;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((int)(a.tok.cu[mid] * G / TILE_ROWS) + mid <= slot) lo = mid; else hi = mid;
+    }
+    b.n = lo;
+    tile = slot - ((int)(a.tok.cu[lo] * G / TILE_ROWS) + lo);
+  } else {
+    const int per = (int)(((int64_t)a.tok.T * a.G + TILE_ROWS - 1) / TILE_ROWS);
+    b.n = slot / per;
+    tile = slot - b.n * per;
+  }
+  b.q0 = seq_start(a.tok, b.n);
+  b.m = seq_start(a.tok, b.n + 1) - b.q0;
+  const int64_t rows = (int64_t)b.m * a.G;
+  if ((int64_t)tile * TILE_ROWS >= rows || rows <= FEW_ROWS) return;
+  b.r0 = tile * TILE_ROWS;
+  b.r1 = (int)min(rows, (int64_t)b.r0 + TILE_ROWS);
+  b.kv = cached(a.cache, b.n);
+  b.range(a);
+  if (split > 0 && b.lo + split * a.len >= b.hi) return;
+  attn_block<E, D, 2, 4, 1, KT>(a, b, split, smem);
+}
+
+// Joins the splits' sums: D / 4 threads to a row.
+template <class E, int D> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
+  constexpr int TPR = D / 4;
+  const int64_t rows = (int64_t)a.tok.total * a.Hq;
+  const int64_t at = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (at >= rows) return;
+  const int ch = (threadIdx.x % TPR) * 4;
+  const int t = (int)(at / a.Hq), h = (int)(at - (int64_t)t * a.Hq);
+  Block b;
+  b.n = seq_of(a.tok, t);
+  b.q0 = seq_start(a.tok, b.n);
+  b.m = seq_start(a.tok, b.n + 1) - b.q0;
+  const int64_t all = (int64_t)b.m * a.G;
+  if ((all <= FEW_ROWS) != (a.few != 0)) return;
+  const int r = (t - b.q0) * a.G + h % a.G;
+  const int R = a.few ? FEW_ROWS : TILE_ROWS;
+  b.r0 = r / R * R;
+  b.r1 = (int)min(all, (int64_t)b.r0 + R);
+  b.kv = cached(a.cache, b.n);
+  b.range(a);
+  const int live = min(a.splits, max(1, (b.hi - b.lo + a.len - 1) / a.len));
+  float mx = -INFINITY, ll = 0.f;
+  for (int s = 0; s < live; ++s) mx = fmaxf(mx, a.part_ml[2 * (s * rows + at)]);
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < live; ++s) {
+    const int64_t w = s * rows + at;
+    const float al = __builtin_amdgcn_exp2f(a.part_ml[2 * w] - ref);
+    ll += al * a.part_ml[2 * w + 1];
+    const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + w * D + ch);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += al * y[e];
+  }
+  const float inv = ll == 0.f ? 0.f : 1.f / ll;
+  E* p = reinterpret_cast<E*>(a.o.data + (int64_t)t * a.o.ts + h * a.o.hs) + ch;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) p[e] = to_e<E>(x[e] * inv);
+  if (ch == 0 && a.lse)
+    a.lse[at] = ll == 0.f ? -INFINITY : (mx + log2f(ll)) * 0.6931471805599453f;
+}
+
+// ---- launchers
+
+namespace {
+
+// Tiles: as many keys as leave two buffers of k and v in LDS at the waves'
+// groups of 16.  {keys, waves} of the few-rows kernel, keys of the other.
+template <class E, int D> struct Few {
+  static constexpr int RB = D * (int)sizeof(E);
+  static constexpr int KW = RB >= 1024 ? 2 : 4;
+  static constexpr int KT = RB <= 256 ? 128 : RB == 512 ? 64 : 32;
+};
+template <class E, int D> struct Tile {
+  static constexpr int KT = D * (int)sizeof(E) >= 1024 ? 32 : 64;
+};
+
+template <class F> hipError_t by_dim(Dt dt, int d, F&& f) {
+  auto go = [&](auto e) {
+    using E = decltype(e);
+    if (d == 64) return f(E{}, std::integral_constant<int, 64>{});
+    if (d == 128) return f(E{}, std::integral_constant<int, 128>{});
+    return f(E{}, std::integral_constant<int, 256>{});
+  };
+  if (d != 64 && d != 128 && d != 256) return hipErrorInvalidValue;
+  return dt == Dt::F32 ? go(float{}) : go(bf16{});
+}
+
+}  // namespace
+
+int attn_few_keys(Dt dt, int d) {
+  const int rb = d * (dt == Dt::F32 ? 4 : 2);
+  return rb <= 256 ? 128 : rb == 512 ? 64 : 32;
+}
+int attn_tile_keys(Dt dt, int d) { return d * (dt == Dt::F32 ? 4 : 2) >= 1024 ? 32 : 64; }
+
+hipError_t launch_attn_few(Dt dt, int d, bool rows16, const AttnArgs& a, hipStream_t s) {
+  const unsigned grid = (unsigned)((int64_t)a.tok.N * a.splits * a.Hk);
+  return by_dim(dt, d, [&](auto e, auto dim) {
+    using E = decltype(e);
+    constexpr int D = decltype(dim)::value;
+    using F = Few<E, D>;
+    if (rows16)
+      hipLaunchKernelGGL((k_attn_few<E, D, 1, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_attn_few<E, D, 2, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStream_t s) {
+  const unsigned grid = (unsigned)((int64_t)slots * a.splits * a.Hk);
+  return by_dim(dt, d, [&](auto e, auto dim) {
+    using E = decltype(e);
+    constexpr int D = decltype(dim)::value;
+    hipLaunchKernelGGL((k_attn_tile<E, D, Tile<E, D>::KT>), dim3(grid), dim3(256), 0, s, a, slots);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s) {
+  const int64_t rows = (int64_t)a.tok.total * a.Hq;
+  return by_dim(dt, d, [&](auto e, auto dim) {
+    using E = decltype(e);
+    constexpr int D = decltype(dim)::value, PER = 256 / (D / 4);
+    hipLaunchKernelGGL((k_attn_join<E, D>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(256), 0,
+                       s, a);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace gdn

@@ -1,0 +1,517 @@
+// Rotary positions, storing new tokens in a paged cache, and the management of
+// its pages.  All of it moves data once and computes little: bound by HBM, and
+// by launches where there is little to move.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "gdn_device.h"
+#include "gdn_paged_kernels.h"
+
+namespace gdn {
+
+// ------------------------------------------------------------------ rotation
+
+namespace {
+
+// cos and sin of a fraction of a turn, |f| <= 1/2.  bf16: the hardware's
+// v_sin and v_cos (absolute error about 2e-7 at this range... far below a
+// bf16 rounding); fp32: the library functions, correct to an ulp or two.
+template <class E> __device__ inline float2 cos_sin(float f) {
+  if constexpr (sizeof(E) == 2)
+    return make_float2(__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f));
+  float s, c;
+  sincospif(2.f * f, &s, &c);
+  return make_float2(c, s);
+}
+
+template <class E> struct Pc {  // 16 bytes of channels
+  static constexpr int N = 16 / sizeof(E);
+  E e[N];
+};
+template <class E> __device__ inline Pc<E> load_piece(const unsigned char* p) {
+  const uint4 x = *reinterpret_cast<const uint4*>(p);
+  return *reinterpret_cast<const Pc<E>*>(&x);
+}
+template <class E> __device__ inline void store_piece(unsigned char* p, const Pc<E>& x) {
+  *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&x);
+}
+
+}  // namespace
+
+constexpr int ROT_TOKENS = 16;   // most tokens of a workgroup
+constexpr int ROT_TABLE = 1024;  // angles it holds
+
+// A workgroup takes a.per tokens: first the cos and sin of their angles into
+// LDS, once for all heads, with each token's place; then the rows of q, k (and
+// v) go through it in units of 16 bytes a lane.
+//   WIDE: a unit is one 16-byte piece (interleaved pairs lie inside one) or, in
+//   the layout of halves, the two pieces that hold the two sides of its pairs,
+//   where those start at multiples of 16 bytes; else a unit is one pair.
+template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
+  constexpr int N = Pc<E>::N;
+  __shared__ float2 cs[ROT_TABLE];
+  __shared__ int64_t kat[ROT_TOKENS];  // where the token's k and v go; -1: nowhere
+  const int half = a.rot / 2;
+  const int t0 = blockIdx.x * a.per, nt = min(a.per, a.tok.total - t0);
+
+  for (int i = threadIdx.x; i < nt * max(half, 1); i += 256) {
+    const int tt = half ? i / half : i, j = half ? i - tt * half : 0, t = t0 + tt;
+    int pos;
+    if (a.positions) {
+      pos = a.positions[t];
+    } else {
+      const int n = seq_of(a.tok, t), q0 = seq_start(a.tok, n);
+      pos = t - q0;
+      if (a.append) {
+        pos += cached(a.cache, n) - (seq_start(a.tok, n + 1) - q0);
+        if (j == 0) {
+          int64_t at = -1;
+          if (pos >= 0) {
+            const int p = a.cache.table[(int64_t)n * a.cache.max_blocks + (pos >> a.cache.shift)];
+            if ((unsigned)p < (unsigned)a.cache.num_pages)
+              at = p * a.cache.page + (pos & ((1 << a.cache.shift) - 1)) * a.cache.slot;
+          }
+          kat[tt] = at;
+        }
+      }
+    }
+    if (half) {
+      const double f = (double)pos * a.turns[j];
+      float2 x = cos_sin<E>((float)(f - rint(f)));
+      x.x *= a.scale;
+      x.y *= a.scale * a.sign;
+      cs[i] = x;
+    }
+  }
+  __syncthreads();
+
+  const bool halves = a.layout == 0;
+  // units of a row that is turned, and of one that is copied (v)
+  const int turn = WIDE && halves ? half / N : (WIDE ? a.d / N : half);
+  const int rest = WIDE ? (halves ? (a.d - a.rot) / N : 0) : a.d - a.rot;
+  const int per_row = turn + rest, per_v = a.d / N;
+  const int nq = (a.q.data ? a.Hq : 0) * per_row, nk = (a.k.data ? a.Hk : 0) * per_row;
+  const int nv = (a.v.data ? a.Hk : 0) * per_v, per_token = nq + nk + nv;
+
+#pragma unroll 2
+  for (int i = threadIdx.x; i < nt * per_token; i += 256) {
+    const int tt = i / per_token, u = i - tt * per_token;
+    const int64_t t = t0 + tt;
+    if (u >= nq + nk) {
+      const int h = (u - nq - nk) / per_v, p = (u - nq - nk) - h * per_v;
+      const int64_t at = kat[tt];
+      if (at >= 0)
+        store_piece(a.cache.v + at + h * a.cache.head + p * 16,
+                    load_piece<E>(a.v.data + t * a.v.ts + h * a.v.hs + p * 16));
+      continue;
+    }
+    const bool is_q = u < nq;
+    const int h = (is_q ? u : u - nq) / per_row, p = (is_q ? u : u - nq) - h * per_row;
+    const unsigned char* x = is_q ? a.q.data + t * a.q.ts + h * a.q.hs
+                                  : a.k.data + t * a.k.ts + h * a.k.hs;
+    unsigned char* y;
+    if (is_q) {
+      y = a.q_out.data + t * a.q_out.ts + h * a.q_out.hs;
+    } else if (a.append) {
+      const int64_t at = kat[tt];
+      if (at < 0) continue;
+      y = a.cache.k + at + h * a.cache.head;
+    } else {
+      y = a.k_out.data + t * a.k_out.ts + h * a.k_out.hs;
+    }
+    const float2* w = cs + tt * half;
+    if constexpr (WIDE) {
+      if (halves) {
+        if (p >= turn) {
+          const int at = (a.rot / N + p - turn) * 16;
+          store_piece(y + at, load_piece<E>(x + at));
+          continue;
+        }
+        const int at1 = p * 16, at2 = (p + turn) * 16;
+        Pc<E> x1 = load_piece<E>(x + at1), x2 = load_piece<E>(x + at2), y1, y2;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float2 c = w[p * N + j];
+          const float u1 = to_f(x1.e[j]), u2 = to_f(x2.e[j]);
+          y1.e[j] = to_e<E>(u1 * c.x - u2 * c.y);
+          y2.e[j] = to_e<E>(u2 * c.x + u1 * c.y);
+        }
+        store_piece(y + at1, y1);
+        store_piece(y + at2, y2);
+      } else {
+        Pc<E> z = load_piece<E>(x + p * 16);
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+          const int pair = p * (N / 2) + j;
+          if (pair < half) {
+            const float2 c = w[pair];
+            const float u1 = to_f(z.e[2 * j]), u2 = to_f(z.e[2 * j + 1]);
+            z.e[2 * j] = to_e<E>(u1 * c.x - u2 * c.y);
+            z.e[2 * j + 1] = to_e<E>(u2 * c.x + u1 * c.y);
+          }
+        }
+        store_piece(y + p * 16, z);
+      }
+    } else {  // halves that do not start at multiples of 16 bytes
+      const E* xe = reinterpret_cast<const E*>(x);
+      E* ye = reinterpret_cast<E*>(y);
+      if (p >= turn) {
+        const int ch = a.rot + p - turn;
+        ye[ch] = xe[ch];
+      } else {
+        const float2 c = w[p];
+        const float u1 = to_f(xe[p]), u2 = to_f(xe[p + half]);
+        ye[p] = to_e<E>(u1 * c.x - u2 * c.y);
+        ye[p + half] = to_e<E>(u2 * c.x + u1 * c.y);
+      }
+    }
+  }
+}
+
+hipError_t launch_rotate(Dt dt, RotateArgs a, hipStream_t s) {
+  // Tokens of a workgroup: enough to fill it a few times over where there are
+  // many, one where there are few.
+  int per = (a.tok.total + 2047) / 2048;
+  per = per < 1 ? 1 : per > ROT_TOKENS ? ROT_TOKENS : per;
+  const int half = a.rot / 2;
+  while (per > 1 && per * half > ROT_TABLE) --per;
+  a.per = per;
+  const dim3 grid((unsigned)((a.tok.total + per - 1) / per));
+  const int n = dt == Dt::F32 ? 4 : 8;
+  const bool wide = a.layout == 1 || half % n == 0;
+  auto go = [&](auto e) {
+    using E = decltype(e);
+    if (wide)
+      hipLaunchKernelGGL((k_rotate<E, true>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_rotate<E, false>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  };
+  return dt == Dt::F32 ? go(float{}) : go(bf16{});
+}
+
+// ------------------------------------------------------------------ pages
+//
+// What a page call decides is a few prefix sums over the sequences and over
+// refs: one workgroup of 16 waves does it (k_*_plan), in index order, so the
+// result is the same on every run; the rows of the table and the data follow
+// in kernels over the whole GPU.
+
+namespace {
+
+constexpr int PLAN = 1024;
+
+__device__ inline int blocks_of(int len, const Book& b) {
+  const int64_t n = ((int64_t)max(len, 0) + b.page_size - 1) / b.page_size;
+  return (int)min(n, (int64_t)b.max_blocks);
+}
+__device__ inline bool held(const Book& b, int p) { return (unsigned)p < (unsigned)b.num_pages; }
+
+// Exclusive prefix sum over the workgroup's threads; *total: the sum.
+__device__ inline int scan(int x, int* total) {
+  __shared__ int wsum[PLAN / 64];
+  const int lane = lane_id(), wave = wave_id();
+  int v = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(v, d);
+    if (lane >= d) v += y;
+  }
+  __syncthreads();  // wsum of an earlier call is read
+  if (lane == 63) wsum[wave] = v;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN / 64; ++w) {
+    if (w < wave) before += wsum[w];
+    all += wsum[w];
+  }
+  *total = all;
+  return before + v - x;
+}
+
+constexpr int SCAN_PER = 8;  // pages of a thread in one step
+
+// Calls f(page, place) for every page in [0, num) with pick(page) in index
+// order of place = its rank among them; returns how many there are.
+template <class Pick, class F> __device__ inline int ranked(int num, Pick&& pick, F&& f) {
+  int base = 0;
+  for (int p0 = 0; p0 < num; p0 += PLAN * SCAN_PER) {
+    const int mine = p0 + threadIdx.x * SCAN_PER;
+    unsigned bits = 0;
+#pragma unroll
+    for (int j = 0; j < SCAN_PER; ++j)
+      if (mine + j < num && pick(mine + j)) bits |= 1u << j;
+    int total, at = base + scan(__popc(bits), &total);
+#pragma unroll
+    for (int j = 0; j < SCAN_PER; ++j)
+      if (bits >> j & 1) f(mine + j, at++);
+    base += total;
+  }
+  return base;
+}
+
+}  // namespace
+
+// rank[s] = the place, among the pages given out, of sequence s's first (-1:
+// it gets none); dst[i] = the i-th free page; refs_out: with those given out.
+__global__ __launch_bounds__(PLAN) void k_extend_plan(Book b, const int32_t* add,
+                                                      int32_t* short_of, PageWork w) {
+  const int found = ranked(
+      b.num_pages,
+      [&](int p) {
+        const int r = b.refs[p];
+        if (b.refs_out != b.refs) b.refs_out[p] = r;
+        return r <= 0;
+      },
+      [&](int p, int i) { w.dst[i] = p; });
+  int base = 0;
+  for (int s0 = 0; s0 < b.S; s0 += PLAN) {
+    const int s = s0 + threadIdx.x;
+    int need = 0, len = 0, more = 0;
+    bool fits = false;
+    if (s < b.S) {
+      len = max(b.lens[s], 0);
+      more = max(add[s], 0);
+      const int64_t blocks = ((int64_t)len + more + b.page_size - 1) / b.page_size;
+      const int64_t old = ((int64_t)len + b.page_size - 1) / b.page_size;
+      need = (int)min(blocks - old, (int64_t)1 << 30);
+      fits = blocks <= b.max_blocks;
+    }
+    // what a sequence wants is cut at found + 1, which keeps the sums in range
+    // and refuses the same sequences
+    const int want = fits ? min(need, found + 1) : 0;
+    int total;
+    const int before = min(base, found + 1) + scan(want, &total);
+    const bool served = fits && (need == 0 || before + want <= found);
+    if (s < b.S) {
+      w.rank[s] = served && need > 0 ? before : -1;
+      short_of[s] = served ? 0 : need;
+      w.lens[s] = len;  // the old length, for the rows
+      b.lens_out[s] = served ? len + more : len;
+    }
+    base = min(base, found + 1) + total;
+  }
+}
+
+// Rows of the table, one workgroup each; the new blocks' pages are marked held.
+__global__ __launch_bounds__(256) void k_extend_rows(Book b, PageWork w) {
+  const int s = blockIdx.x, first = w.rank[s], old = blocks_of(w.lens[s], b);
+  const int now = first >= 0 ? blocks_of(b.lens_out[s], b) : old;
+  for (int i = threadIdx.x; i < b.max_blocks; i += 256) {
+    const int64_t at = (int64_t)s * b.max_blocks + i;
+    if (i >= old && i < now) {
+      const int p = w.dst[first + i - old];
+      b.table_out[at] = p;
+      b.refs_out[p] = 1;
+    } else if (b.table_out != b.table) {
+      b.table_out[at] = b.table[at];
+    }
+  }
+}
+
+hipError_t launch_extend(const Book& b, const int32_t* add, int32_t* short_of, const PageWork& w,
+                         hipStream_t s) {
+  hipLaunchKernelGGL(k_extend_plan, dim3(1), dim3(PLAN), 0, s, b, add, short_of, w);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_extend_rows, dim3(b.S), dim3(256), 0, s, b, w);
+  return hipGetLastError();
+}
+
+// count[0] = copies; src, dst: their pages; rank[i]: row i's copy or -1, -2: no
+// page was left.  w.lens, w.table hold the old lengths and, in place, rows.
+__global__ __launch_bounds__(PLAN) void k_select_plan(Book b, const int32_t* parents,
+                                                      int32_t* short_of, PageWork w) {
+  const int tid = threadIdx.x;
+  for (int s = tid; s < b.S; s += PLAN) {
+    __hip_atomic_store(&w.heir[s], b.S, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    w.lens[s] = b.lens[s];
+  }
+  __syncthreads();
+  for (int i = tid; i < b.S; i += PLAN) {
+    const int p = parents[i];
+    if ((unsigned)p < (unsigned)b.S) atomicMin(&w.heir[p], i);
+  }
+  const int found = ranked(
+      b.num_pages,
+      [&](int p) {
+        const int r = b.refs[p];
+        if (b.refs_out != b.refs) b.refs_out[p] = r;
+        return r <= 0;
+      },
+      [&](int p, int i) { w.dst[i] = p; });
+  __syncthreads();
+  int base = 0;
+  for (int i0 = 0; i0 < b.S; i0 += PLAN) {
+    const int i = i0 + tid;
+    int src = -1;
+    if (i < b.S) {
+      const int p = parents[i];
+      if ((unsigned)p < (unsigned)b.S) {
+        const int len = b.lens[p], last = len / b.page_size;
+        if (len > 0 && len % b.page_size != 0 && last < b.max_blocks &&
+            __hip_atomic_load(&w.heir[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i) {
+          src = b.table[(int64_t)p * b.max_blocks + last];
+          if (!held(b, src)) src = -1;
+        }
+      }
+    }
+    int total;
+    const int at = base + scan(src >= 0, &total);
+    if (i < b.S) {
+      const bool none = src >= 0 && at >= found;
+      if (src >= 0 && !none) w.src[at] = src;
+      w.rank[i] = src < 0 ? -1 : none ? -2 : at;
+      short_of[i] = none;
+    }
+    base += total;
+  }
+  if (tid == 0) w.count[0] = min(base, found);
+}
+
+__global__ __launch_bounds__(256) void k_copy_ints(const int32_t* x, int32_t* y, int64_t n) {
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) y[i] = x[i];
+}
+
+// New rows, one workgroup each, and the references of old and new ones.
+__global__ __launch_bounds__(256) void k_select_rows(Book b, const int32_t* parents, PageWork w,
+                                                     const int32_t* table) {
+  const int i = blockIdx.x, p = parents[i], rank = w.rank[i];
+  const bool real = (unsigned)p < (unsigned)b.S && rank != -2;
+  const int len = real ? max(w.lens[p], 0) : 0, now = blocks_of(len, b);
+  const int was = blocks_of(w.lens[i], b);
+  if (threadIdx.x == 0) b.lens_out[i] = len;
+  for (int j = threadIdx.x; j < b.max_blocks; j += 256) {
+    if (j < was) {
+      const int o = table[(int64_t)i * b.max_blocks + j];
+      if (held(b, o)) atomicAdd(&b.refs_out[o], -1);
+    }
+    int x = -1;
+    if (j < now) {
+      x = rank >= 0 && j == now - 1 ? w.dst[rank] : table[(int64_t)p * b.max_blocks + j];
+      if (held(b, x)) atomicAdd(&b.refs_out[x], 1);
+    }
+    b.table_out[(int64_t)i * b.max_blocks + j] = x;
+  }
+}
+
+hipError_t launch_select(const Book& b, const int32_t* parents, int32_t* short_of,
+                         const PageWork& w, hipStream_t s) {
+  const int32_t* table = b.table;
+  if (b.table_out == b.table) {
+    const int64_t n = (int64_t)b.S * b.max_blocks;
+    hipLaunchKernelGGL(k_copy_ints, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 2048)),
+                       dim3(256), 0, s, b.table, w.table, n);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    table = w.table;
+  }
+  hipLaunchKernelGGL(k_select_plan, dim3(1), dim3(PLAN), 0, s, b, parents, short_of, w);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_select_rows, dim3(b.S), dim3(256), 0, s, b, parents, w, table);
+  return hipGetLastError();
+}
+
+// count[0] = moves, count[1] = pages in use; src, dst: the moves; map.
+__global__ __launch_bounds__(PLAN) void k_compact_plan(Book b, int32_t* map, PageWork w) {
+  int mine = 0;
+  for (int p = threadIdx.x; p < b.num_pages; p += PLAN) mine += b.refs[p] > 0;
+  int n;
+  scan(mine, &n);
+  // below n the free ones (holes), from n on those in use: as many
+  const int moves = ranked(n, [&](int p) { return b.refs[p] <= 0; },
+                           [&](int p, int i) { w.dst[i] = p; });
+  ranked(b.num_pages - n, [&](int p) { return b.refs[n + p] > 0; },
+         [&](int p, int i) { w.src[i] = n + p; });
+  for (int p = threadIdx.x; p < b.num_pages; p += PLAN)
+    map[p] = p < n && b.refs[p] > 0 ? p : -1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < moves; i += PLAN) map[w.src[i]] = w.dst[i];
+  if (threadIdx.x == 0) {
+    w.count[0] = moves;
+    w.count[1] = n;
+  }
+}
+
+// Rows of the table, renumbered; what a sequence does not hold becomes -1.
+__global__ __launch_bounds__(256) void k_compact_rows(Book b, const int32_t* map) {
+  const int64_t n = (int64_t)b.S * b.max_blocks;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+    const int s = (int)(i / b.max_blocks), j = (int)(i - (int64_t)s * b.max_blocks);
+    int x = -1;
+    if (j < blocks_of(b.lens[s], b)) {
+      x = b.table[i];
+      x = held(b, x) ? map[x] : -1;
+    }
+    b.table_out[i] = x;
+  }
+}
+// refs: the moves take theirs along (a page that is moved from lies at n or
+// past it, one that is moved to below: no thread reads what another writes).
+__global__ __launch_bounds__(256) void k_compact_refs(Book b, const int32_t* map, PageWork w) {
+  const int n = w.count[1];
+  for (int p = blockIdx.x * 256 + threadIdx.x; p < b.num_pages; p += gridDim.x * 256) {
+    if (p < n) {
+      if (map[p] >= 0 && b.refs_out != b.refs) b.refs_out[p] = b.refs[p];
+    } else if (map[p] >= 0) {
+      b.refs_out[map[p]] = b.refs[p];
+      b.refs_out[p] = 0;
+    } else {
+      b.refs_out[p] = 0;
+    }
+  }
+}
+
+hipError_t launch_compact(const Book& b, int32_t* map, const PageWork& w, hipStream_t s) {
+  hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(PLAN), 0, s, b, map, w);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  const int64_t n = (int64_t)b.S * b.max_blocks;
+  hipLaunchKernelGGL(k_compact_rows, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 2048)),
+                     dim3(256), 0, s, b, map);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_compact_refs, dim3((unsigned)std::min(b.num_pages / 256 + 1, 1024)),
+                     dim3(256), 0, s, b, map, w);
+  return hipGetLastError();
+}
+
+// Page copies in units of 16 KiB: (pair, part, unit), strided over the grid.
+constexpr int MOVE_UNIT = 16384;
+__global__ __launch_bounds__(256) void k_move(Pool p, const int32_t* src, const int32_t* dst,
+                                              const int32_t* count, int n) {
+  const int64_t per = (p.bytes + MOVE_UNIT - 1) / MOVE_UNIT;
+  const int64_t units = (int64_t)(count ? *count : n) * p.parts * per;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int64_t i = u / (p.parts * per), r = u - i * (p.parts * per);
+    const int part = (int)(r / per);
+    const int64_t at = (r - part * per) * MOVE_UNIT;
+    const int from = src[i], to = dst[i];
+    if ((unsigned)from >= (unsigned)p.num_pages || (unsigned)to >= (unsigned)p.num_pages) continue;
+    const unsigned char* x = p.data + part * p.part + from * p.page + at;
+    unsigned char* y = p.data + part * p.part + to * p.page + at;
+    const int64_t left = p.bytes - at;
+    if (left >= MOVE_UNIT) {
+      uint4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v[j] = *reinterpret_cast<const uint4*>(x + j * 4096 + threadIdx.x * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) store_stream(y + j * 4096 + threadIdx.x * 16, v[j]);
+    } else {
+      for (int64_t o = threadIdx.x * 16; o < left; o += 4096)
+        store_stream(y + o, *reinterpret_cast<const uint4*>(x + o));
+    }
+  }
+}
+
+hipError_t launch_move(const Pool& p, const int32_t* src, const int32_t* dst,
+                       const int32_t* count, int n, hipStream_t s) {
+  const int64_t per = (p.bytes + MOVE_UNIT - 1) / MOVE_UNIT;
+  const int64_t units = (int64_t)n * p.parts * per;
+  hipLaunchKernelGGL(k_move, dim3((unsigned)std::min<int64_t>(units, 4096)), dim3(256), 0, s, p,
+                     src, dst, count, n);
+  return hipGetLastError();
+}
+
+}  // namespace gdn

@@ -1,0 +1,460 @@
+// C ABI of the attention layer: argument validation, workspace and launch
+// sizes.  Every check runs before the first launch; nothing here allocates,
+// frees or synchronises.
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "../../include/gdn_paged.h"
+#include "gdn_paged_kernels.h"
+
+namespace {
+
+using gdn::AttnArgs;
+using gdn::Dt;
+
+constexpr int64_t MAX_STRIDE = (int64_t)1 << 27;  // bytes between slots of a page
+constexpr int64_t MAX_PAGES = (int64_t)1 << 20;   // of a book
+
+bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+size_t up(size_t x) { return (x + 255) / 256 * 256; }
+Dt type_of(gdn_dtype d) { return d == GDN_F32 ? Dt::F32 : Dt::BF16; }
+int size_of(gdn_dtype d) { return d == GDN_F32 ? 4 : 2; }
+gdn_status done(hipError_t e) { return e == hipSuccess ? GDN_OK : GDN_ERR_HIP; }
+
+gdn_status check_tokens(const gdn_tokens* t, gdn::Tokens* out) {
+  if (!t) return GDN_ERR_NULL;
+  if (t->dtype != GDN_F32 && t->dtype != GDN_BF16) return GDN_ERR_UNSUPPORTED;
+  if (t->d != 64 && t->d != 128 && t->d != 256) return GDN_ERR_UNSUPPORTED;
+  if (t->B < 1 || t->T < 1 || t->Hq < 1 || t->Hk < 1) return GDN_ERR_SHAPE;
+  const int64_t total = (int64_t)t->B * t->T;
+  // rows (tokens x heads) are counted in 31 bits
+  if (total * std::max(t->Hq, t->Hk) >= (int64_t)1 << 31) return GDN_ERR_SHAPE;
+  out->total = (int)total;
+  out->cu = t->cu_seqlens;
+  out->N = t->B;
+  out->T = t->T;
+  if (t->cu_seqlens) {
+    if (t->B != 1) return GDN_ERR_SHAPE;
+    const int32_t* cu = t->cu_seqlens_host;
+    if (!cu || t->num_seqs < 1 || cu[0] != 0 || cu[t->num_seqs] != t->T) return GDN_ERR_CU_SEQLENS;
+    for (int n = 0; n < t->num_seqs; ++n)
+      if (cu[n + 1] < cu[n]) return GDN_ERR_CU_SEQLENS;
+    if (!aligned(t->cu_seqlens, 4)) return GDN_ERR_ALIGN;
+    out->N = t->num_seqs;
+    out->T = 0;
+  } else if (t->cu_seqlens_host) {
+    return GDN_ERR_CU_SEQLENS;
+  }
+  return GDN_OK;
+}
+
+// A row tensor (nullptr or no data: absent) in bytes.
+gdn_status check_rows(const gdn_rows* r, int esz, gdn::Rows* out) {
+  if (!r || !r->data) return GDN_ERR_NULL;
+  if (!aligned(r->data, 16) || r->token_stride * esz % 16 || r->head_stride * esz % 16)
+    return GDN_ERR_ALIGN;
+  out->data = (unsigned char*)r->data;
+  out->ts = r->token_stride * esz;
+  out->hs = r->head_stride * esz;
+  return GDN_OK;
+}
+
+gdn_status check_cache(const gdn_cache* c, int esz, bool pointers, gdn::Cache* out) {
+  if (!c) return GDN_ERR_NULL;
+  if (c->num_pages < 1 || c->max_blocks < 1 || c->page_size < 16 || c->page_size > 1024 ||
+      (c->page_size & (c->page_size - 1)))
+    return GDN_ERR_SHAPE;
+  if ((int64_t)c->max_blocks * c->page_size >= (int64_t)1 << 31) return GDN_ERR_SHAPE;
+  if (pointers) {
+    if (!c->k || !c->v || !c->table || !c->kv_lens) return GDN_ERR_NULL;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->table, 4) ||
+        !aligned(c->kv_lens, 4) || c->page_stride * esz % 16 || c->head_stride * esz % 16 ||
+        c->token_stride * esz % 16)
+      return GDN_ERR_ALIGN;
+    if (c->token_stride < 0 || c->token_stride * esz >= MAX_STRIDE) return GDN_ERR_SHAPE;
+  }
+  out->k = (unsigned char*)c->k;
+  out->v = (unsigned char*)c->v;
+  out->page = c->page_stride * esz;
+  out->head = c->head_stride * esz;
+  out->slot = c->token_stride * esz;
+  out->table = c->table;
+  out->lens = c->kv_lens;
+  out->num_pages = c->num_pages;
+  out->shift = 0;
+  while ((1 << out->shift) < c->page_size) ++out->shift;
+  out->max_blocks = c->max_blocks;
+  return GDN_OK;
+}
+
+gdn_status check_rotary(const gdn_rotary* r, int d) {
+  if (r->rot < 2 || r->rot > d || r->rot % 2 || (r->layout != 0 && r->layout != 1) ||
+      !isfinite(r->scale))
+    return GDN_ERR_VALUE;
+  if (!r->turns) return GDN_ERR_NULL;
+  return aligned(r->turns, 8) ? GDN_OK : GDN_ERR_ALIGN;
+}
+
+gdn_status rotate(const gdn_tokens* t, const gdn_rotary* r, const gdn_rows* q, const gdn_rows* k,
+                  const int32_t* positions, const gdn_rows* q_out, const gdn_rows* k_out,
+                  float sign, void* stream) {
+  gdn::RotateArgs a;
+  memset(&a, 0, sizeof a);
+  gdn_status st = check_tokens(t, &a.tok);
+  if (st != GDN_OK) return st;
+  if (!r) return GDN_ERR_NULL;
+  if ((st = check_rotary(r, t->d)) != GDN_OK) return st;
+  const int esz = size_of(t->dtype);
+  if ((st = check_rows(q, esz, &a.q)) != GDN_OK) return st;
+  if ((st = check_rows(q_out, esz, &a.q_out)) != GDN_OK) return st;
+  const bool has_k = k && k->data;
+  if (has_k != (k_out && k_out->data)) return GDN_ERR_NULL;
+  if (has_k) {
+    if ((st = check_rows(k, esz, &a.k)) != GDN_OK) return st;
+    if ((st = check_rows(k_out, esz, &a.k_out)) != GDN_OK) return st;
+  }
+  if (!aligned(positions, 4)) return GDN_ERR_ALIGN;
+  a.positions = positions;
+  a.turns = r->turns;
+  a.Hq = t->Hq;
+  a.Hk = t->Hk;
+  a.d = t->d;
+  a.rot = r->rot;
+  a.layout = r->layout;
+  a.scale = r->scale;
+  a.sign = sign;
+  return done(gdn::launch_rotate(type_of(t->dtype), a, (hipStream_t)stream));
+}
+
+// How a call's work is cut: row blocks of the two kernels, splits of their keys.
+struct Plan {
+  bool few = false, tile = false;  // which kernels have sequences
+  bool rows16 = true;              // no few-rows sequence has more than 16 rows
+  int slots = 0;                   // of the tile kernel
+  int few_splits = 1, few_len = 0, tile_splits = 1, tile_len = 0;
+  size_t part = 0, bytes = 0;      // workspace: offset of {maximum, sum}; size
+};
+
+// Splits so that about `want` workgroups have keys, no range shorter than `least`.
+void split(int64_t units, int64_t keys, int step, int64_t want, int64_t least, int* splits,
+           int* len) {
+  int64_t s = units >= want / 2 ? 1 : (want + units - 1) / units;
+  s = std::max<int64_t>(1, std::min(s, keys / least));
+  int64_t l = (keys + s - 1) / s;
+  l = (l + step - 1) / step * step;
+  *len = (int)l;
+  *splits = (int)((keys + l - 1) / l);
+}
+
+gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cache* c,
+                     const gdn_attn* a, Plan* out) {
+  if (!a) return GDN_ERR_NULL;
+  if (!(a->scale > 0.f) || !isfinite(a->scale) || a->window < 0 || a->max_kv < 0 ||
+      (a->window > 0 && !a->causal))
+    return GDN_ERR_VALUE;
+  if (t->Hq % t->Hk) return GDN_ERR_SHAPE;
+  Plan p;
+  const int64_t G = t->Hq / t->Hk;
+  int64_t most_few = 0, most = 0, n_few = 0;  // new tokens of a sequence
+  auto see = [&](int64_t m) {
+    if (m * G <= gdn::FEW_ROWS) {
+      if (m == 0) return;
+      ++n_few;
+      most_few = std::max(most_few, m);
+    } else {
+      p.tile = true;
+      most = std::max(most, m);
+    }
+  };
+  if (tok.cu)
+    for (int n = 0; n < tok.N; ++n) see(t->cu_seqlens_host[n + 1] - t->cu_seqlens_host[n]);
+  else
+    see(tok.T);
+  if (!tok.cu && n_few) n_few = tok.N;
+  p.few = n_few > 0;
+  p.rows16 = most_few * G <= 16;
+  const int R = gdn::TILE_ROWS;
+  p.slots = tok.cu ? (int)((int64_t)tok.total * G / R) + tok.N
+                   : tok.N * (int)(((int64_t)tok.T * G + R - 1) / R);
+  const int64_t room = (int64_t)c->max_blocks * c->page_size;
+  const int64_t kv = std::max<int64_t>(1, a->max_kv > 0 ? std::min<int64_t>(a->max_kv, room) : room);
+  const Dt dt = type_of(t->dtype);
+  // A block of m tokens sees at most window + m - 1 keys, and its range begins
+  // at a multiple of 16.
+  auto keys = [&](int64_t m) { return a->window > 0 ? std::min(kv, a->window + m + 14) : kv; };
+  if (p.few)
+    split(n_few * t->Hk, keys(most_few), gdn::attn_few_keys(dt, t->d), 512,
+          gdn::attn_few_keys(dt, t->d), &p.few_splits, &p.few_len);
+  if (p.tile)
+    split((int64_t)p.slots * t->Hk, keys(std::min<int64_t>(most, R / G + 2)),
+          gdn::attn_tile_keys(dt, t->d), 512, 256, &p.tile_splits, &p.tile_len);
+  const int64_t splits = std::max(p.few_splits, p.tile_splits);
+  if ((int64_t)tok.N * p.few_splits * t->Hk >= (int64_t)1 << 31 ||
+      (int64_t)p.slots * p.tile_splits * t->Hk >= (int64_t)1 << 31)
+    return GDN_ERR_SHAPE;
+  if (splits > 1) {
+    const int64_t rows = (int64_t)tok.total * t->Hq;
+    p.part = up((size_t)(splits * rows * t->d * 4));
+    p.bytes = p.part + up((size_t)(splits * rows * 8));
+  }
+  *out = p;
+  return GDN_OK;
+}
+
+gdn_status check_book(const gdn_book* b, bool lens_out, gdn::Book* out) {
+  if (!b) return GDN_ERR_NULL;
+  if (b->S < 1 || b->max_blocks < 1 || b->num_pages < 1 || b->page_size < 1 ||
+      b->num_pages > MAX_PAGES || (int64_t)b->max_blocks * b->page_size >= (int64_t)1 << 31)
+    return GDN_ERR_SHAPE;
+  if (!b->table || !b->lens || !b->refs || !b->table_out || !b->refs_out ||
+      (lens_out && !b->lens_out))
+    return GDN_ERR_NULL;
+  const void* ptrs[] = {b->table, b->lens, b->refs, b->table_out, b->lens_out, b->refs_out};
+  for (const void* p : ptrs)
+    if (!aligned(p, 4)) return GDN_ERR_ALIGN;
+  *out = gdn::Book{b->S,    b->max_blocks, b->num_pages, b->page_size, b->table,
+                   b->lens, b->refs,       b->table_out, b->lens_out,  b->refs_out};
+  return GDN_OK;
+}
+
+gdn_status check_pool(const gdn_pool* p, gdn::Pool* out) {
+  if (!p->data) return GDN_ERR_NULL;
+  if (p->parts < 1 || p->num_pages < 1 || p->page_bytes < 16) return GDN_ERR_SHAPE;
+  if (!aligned(p->data, 16) || p->part_stride % 16 || p->page_stride % 16 || p->page_bytes % 16)
+    return GDN_ERR_ALIGN;
+  *out = gdn::Pool{(unsigned char*)p->data, p->parts,       p->num_pages,
+                   p->part_stride,          p->page_stride, p->page_bytes};
+  return GDN_OK;
+}
+
+size_t carve_pages(int64_t S, int64_t blocks, int64_t pages, unsigned char* base,
+                   gdn::PageWork* w) {
+  size_t off = 0;
+  auto take = [&](int64_t n) {
+    int32_t* p = base ? (int32_t*)(base + off) : nullptr;
+    off += up((size_t)n * 4);
+    return p;
+  };
+  const int64_t list = std::max(S, pages);
+  gdn::PageWork x;
+  x.count = take(4);
+  x.src = take(list);
+  x.dst = take(list);
+  x.heir = take(S);
+  x.rank = take(S);
+  x.lens = take(S);
+  x.table = take(S * blocks);
+  if (w) *w = x;
+  return off;
+}
+
+gdn_status pages_call(const gdn_book* b, bool lens_out, const gdn_pool* pool, void* workspace,
+                      size_t bytes, gdn::Book* book, gdn::Pool* pl, gdn::PageWork* w) {
+  gdn_status st = check_book(b, lens_out, book);
+  if (st != GDN_OK) return st;
+  if (pool) {
+    if ((st = check_pool(pool, pl)) != GDN_OK) return st;
+    if (pool->num_pages != b->num_pages) return GDN_ERR_SHAPE;
+  }
+  if (workspace && !aligned(workspace, 16)) return GDN_ERR_ALIGN;
+  const size_t need = carve_pages(b->S, b->max_blocks, b->num_pages, nullptr, nullptr);
+  if (!workspace || bytes < need) return GDN_ERR_WORKSPACE;
+  carve_pages(b->S, b->max_blocks, b->num_pages, (unsigned char*)workspace, w);
+  return GDN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gdn_status gdn_rotary_turns(int32_t rot, double base, int32_t scaling, double factor,
+                            double original, double slow, double fast, double* turns,
+                            float* scale) {
+  if (!turns || !scale) return GDN_ERR_NULL;
+  if (rot < 2 || rot % 2 || !(base > 1) || !isfinite(base) || scaling < 0 || scaling > 3)
+    return GDN_ERR_VALUE;
+  if (scaling != GDN_ROTARY_PLAIN && (!(factor >= 1) || !isfinite(factor))) return GDN_ERR_VALUE;
+  if (scaling == GDN_ROTARY_PARTS &&
+      (!(original >= 1) || !isfinite(original) || !isfinite(slow) || !isfinite(fast) ||
+       !(fast > slow)))
+    return GDN_ERR_VALUE;
+  const double turn = 6.283185307179586476925286766559;
+  if (scaling == GDN_ROTARY_BASE && rot > 2) base *= pow(factor, (double)rot / (rot - 2));
+  *scale = scaling == GDN_ROTARY_PARTS ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+  for (int i = 0; i < rot / 2; ++i) {
+    double f = pow(base, -2.0 * i / rot) / turn;
+    if (scaling == GDN_ROTARY_LINEAR) f /= factor;
+    if (scaling == GDN_ROTARY_PARTS) {
+      const double g = std::min(1.0, std::max(0.0, (original * f - slow) / (fast - slow)));
+      f = f / factor * (1 - g) + f * g;
+    }
+    turns[i] = f;
+  }
+  return GDN_OK;
+}
+
+gdn_status gdn_rotary_fwd(const gdn_tokens* t, const gdn_rotary* r, const gdn_rows* q,
+                          const gdn_rows* k, const int32_t* positions, const gdn_rows* q_out,
+                          const gdn_rows* k_out, void* stream) {
+  return rotate(t, r, q, k, positions, q_out, k_out, 1.f, stream);
+}
+
+gdn_status gdn_rotary_bwd(const gdn_tokens* t, const gdn_rotary* r, const gdn_rows* dq_out,
+                          const gdn_rows* dk_out, const int32_t* positions, const gdn_rows* dq,
+                          const gdn_rows* dk, void* stream) {
+  return rotate(t, r, dq_out, dk_out, positions, dq, dk, -1.f, stream);
+}
+
+gdn_status gdn_cache_append(const gdn_tokens* t, const gdn_rotary* r, const gdn_rows* q,
+                            const gdn_rows* k, const gdn_rows* v, const gdn_cache* cache,
+                            const gdn_rows* q_out, void* stream) {
+  gdn::RotateArgs a;
+  memset(&a, 0, sizeof a);
+  gdn_status st = check_tokens(t, &a.tok);
+  if (st != GDN_OK) return st;
+  const int esz = size_of(t->dtype);
+  if (r && (st = check_rotary(r, t->d)) != GDN_OK) return st;
+  if ((st = check_cache(cache, esz, true, &a.cache)) != GDN_OK) return st;
+  if ((st = check_rows(k, esz, &a.k)) != GDN_OK) return st;
+  if ((st = check_rows(v, esz, &a.v)) != GDN_OK) return st;
+  const bool has_q = q && q->data;
+  if (has_q != (q_out && q_out->data)) return GDN_ERR_NULL;
+  if (has_q) {
+    if ((st = check_rows(q, esz, &a.q)) != GDN_OK) return st;
+    if ((st = check_rows(q_out, esz, &a.q_out)) != GDN_OK) return st;
+  }
+  a.Hq = t->Hq;
+  a.Hk = t->Hk;
+  a.d = t->d;
+  a.append = 1;
+  a.sign = 1.f;
+  if (r) {
+    a.turns = r->turns;
+    a.rot = r->rot;
+    a.layout = r->layout;
+    a.scale = r->scale;
+  }
+  return done(gdn::launch_rotate(type_of(t->dtype), a, (hipStream_t)stream));
+}
+
+size_t gdn_cache_attn_workspace_size(const gdn_tokens* t, const gdn_cache* cache,
+                                     const gdn_attn* a) {
+  gdn::Tokens tok;
+  gdn::Cache c;
+  Plan p;
+  if (check_tokens(t, &tok) != GDN_OK || check_cache(cache, 1, false, &c) != GDN_OK ||
+      plan_attn(t, tok, cache, a, &p) != GDN_OK)
+    return 0;
+  return p.bytes;
+}
+
+gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_rows* q,
+                          const gdn_cache* cache, const gdn_rows* o, float* lse, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  AttnArgs a;
+  memset(&a, 0, sizeof a);
+  gdn_status st = check_tokens(t, &a.tok);
+  if (st != GDN_OK) return st;
+  const int esz = size_of(t->dtype);
+  if ((st = check_cache(cache, esz, true, &a.cache)) != GDN_OK) return st;
+  if ((st = check_rows(q, esz, &a.q)) != GDN_OK) return st;
+  if ((st = check_rows(o, esz, &a.o)) != GDN_OK) return st;
+  if (!aligned(lse, 4)) return GDN_ERR_ALIGN;
+  Plan p;
+  if ((st = plan_attn(t, a.tok, cache, at, &p)) != GDN_OK) return st;
+  if (p.bytes) {
+    if (!workspace || workspace_bytes < p.bytes) return GDN_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return GDN_ERR_ALIGN;
+    a.part = (float*)workspace;
+    a.part_ml = (float*)((unsigned char*)workspace + p.part);
+  }
+  a.lse = lse;
+  a.Hq = t->Hq;
+  a.Hk = t->Hk;
+  a.G = t->Hq / t->Hk;
+  a.causal = at->causal != 0;
+  a.window = at->window;
+  a.c = at->scale * 1.4426950408889634f;
+  const Dt dt = type_of(t->dtype);
+  hipStream_t s = (hipStream_t)stream;
+  if (p.few) {
+    a.few = 1;
+    a.splits = p.few_splits;
+    a.len = p.few_len;
+    if (gdn::launch_attn_few(dt, t->d, p.rows16, a, s) != hipSuccess) return GDN_ERR_HIP;
+    if (a.splits > 1 && gdn::launch_attn_join(dt, t->d, a, s) != hipSuccess) return GDN_ERR_HIP;
+  }
+  if (p.tile) {
+    a.few = 0;
+    a.splits = p.tile_splits;
+    a.len = p.tile_len;
+    if (gdn::launch_attn_tile(dt, t->d, p.slots, a, s) != hipSuccess) return GDN_ERR_HIP;
+    if (a.splits > 1 && gdn::launch_attn_join(dt, t->d, a, s) != hipSuccess) return GDN_ERR_HIP;
+  }
+  return GDN_OK;
+}
+
+size_t gdn_pages_workspace_size(const gdn_book* b) {
+  if (!b || b->S < 1 || b->max_blocks < 1 || b->num_pages < 1 || b->num_pages > MAX_PAGES) return 0;
+  return carve_pages(b->S, b->max_blocks, b->num_pages, nullptr, nullptr);
+}
+
+gdn_status gdn_pages_extend(const gdn_book* b, const int32_t* add, int32_t* short_of,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  gdn::Book book;
+  gdn::PageWork w;
+  gdn_status st = pages_call(b, true, nullptr, workspace, workspace_bytes, &book, nullptr, &w);
+  if (st != GDN_OK) return st;
+  if (!add || !short_of) return GDN_ERR_NULL;
+  if (!aligned(add, 4) || !aligned(short_of, 4)) return GDN_ERR_ALIGN;
+  return done(gdn::launch_extend(book, add, short_of, w, (hipStream_t)stream));
+}
+
+gdn_status gdn_pages_select(const gdn_book* b, const int32_t* parents, const gdn_pool* pool,
+                            int32_t* short_of, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  gdn::Book book;
+  gdn::Pool pl;
+  gdn::PageWork w;
+  gdn_status st = pages_call(b, true, pool, workspace, workspace_bytes, &book, &pl, &w);
+  if (st != GDN_OK) return st;
+  if (!parents || !short_of) return GDN_ERR_NULL;
+  if (!aligned(parents, 4) || !aligned(short_of, 4)) return GDN_ERR_ALIGN;
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t e = gdn::launch_select(book, parents, short_of, w, s);
+  if (e == hipSuccess && pool) e = gdn::launch_move(pl, w.src, w.dst, w.count, b->S, s);
+  return done(e);
+}
+
+gdn_status gdn_pages_compact(const gdn_book* b, const gdn_pool* pool, int32_t* map,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  gdn::Book book;
+  gdn::Pool pl;
+  gdn::PageWork w;
+  gdn_status st = pages_call(b, false, pool, workspace, workspace_bytes, &book, &pl, &w);
+  if (st != GDN_OK) return st;
+  if (!map) return GDN_ERR_NULL;
+  if (!aligned(map, 4)) return GDN_ERR_ALIGN;
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t e = gdn::launch_compact(book, map, w, s);
+  if (e == hipSuccess && pool) e = gdn::launch_move(pl, w.src, w.dst, w.count, b->num_pages, s);
+  return done(e);
+}
+
+gdn_status gdn_pages_copy(const gdn_pool* pool, const int32_t* src, const int32_t* dst, int32_t n,
+                          void* stream) {
+  if (!pool) return GDN_ERR_NULL;
+  gdn::Pool pl;
+  gdn_status st = check_pool(pool, &pl);
+  if (st != GDN_OK) return st;
+  if (n < 0) return GDN_ERR_SHAPE;
+  if (n == 0) return GDN_OK;
+  if (!src || !dst) return GDN_ERR_NULL;
+  if (!aligned(src, 4) || !aligned(dst, 4)) return GDN_ERR_ALIGN;
+  return done(gdn::launch_move(pl, src, dst, nullptr, n, (hipStream_t)stream));
+}
+
+}  // extern "C"
