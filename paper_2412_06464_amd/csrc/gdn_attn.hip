@@ -114,12 +114,34 @@ template <class E> __device__ inline bool finite4(const uint4& x) {
   return ok;
 }
 
+// Over the four lanes (16 apart) of a column: the largest value, the sum.
+// v_permlane swaps move the other halves next to each other without LDS.
+__device__ inline float col_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float col_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// The running maximum follows only when a score passes it by this much (in
+// base 2): p stays below 2^8, which costs no accuracy (p, l and o keep their
+// relative precision), and o is rescaled a few times instead of in most tiles.
+constexpr float SLACK = 8.f;
+
 template <class E, int D, int QT, int RW, int KW, int KT>
 __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
                                   unsigned char* smem) {
   using C = AttnCfg<E, D, QT, RW, KW, KT>;
   using P = Piece<E>;
   constexpr int NK = C::NK, NT = NK / 16, RB = C::RB, NP = C::NP, KB = RB / 64, DT = D / 16;
+  constexpr int GROUPS = KT / 16;
+  constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;  // groups this wave copies
   const int lane = lane_id(), g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rw = KW == 1 ? wave : 0, kw = KW == 1 ? 0 : wave;
@@ -127,6 +149,57 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   // the last range goes to the end, however long the cache has become
   const int begin = b.lo + split * a.len;
   const int end = split == a.splits - 1 ? b.hi : min(b.hi, begin + a.len);
+  const int tiles = (end - begin + KT - 1) / KT;
+
+  const CONST_AS int* pages = (const CONST_AS int*)(a.cache.table + (int64_t)b.n * a.cache.max_blocks);
+  const int shift = a.cache.shift, mask = (1 << shift) - 1, num_pages = a.cache.num_pages;
+  const unsigned char* const kbase = a.cache.k + (int64_t)b.hk * a.cache.head;
+  const unsigned char* const vbase = a.cache.v + (int64_t)b.hk * a.cache.head;
+  const unsigned lds0 = (unsigned)(uintptr_t)smem;
+
+  // Pages of the groups of 16 keys of the tile from k0 on that this wave works
+  // on (KW == 1: all of the tile's); they are looked up a tile ahead of their
+  // use, by scalar loads, which the copies in flight do not delay.
+  auto look_up = [&](int k0, int (&pg)[NT]) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int key = k0 + kw * NK + 16 * t;
+      pg[t] = key < end ? pages[__builtin_amdgcn_readfirstlane(key) >> shift] : -1;
+    }
+  };
+  auto there = [&](int page) { return (unsigned)page < (unsigned)num_pages; };
+  // This wave's copies of a tile: groups of 16 keys, of k and of v (a group
+  // that is not there is read from page 0 and not used).
+  unsigned koff[16 / C::RPI], voff[16 / C::RPI];
+#pragma unroll
+  for (int j = 0; j < 16 / C::RPI; ++j) {
+    const int r = j * C::RPI + lane / NP, p = lane % NP;
+    koff[j] = r * (unsigned)a.cache.slot + ((p ^ k_swz<NP>(r)) << 4);
+    voff[j] = r * (unsigned)a.cache.slot + ((p ^ v_swz<E, NP>(r)) << 4);
+  }
+  auto copy_tile = [&](int k0, const int (&pg)[NT], int buf) {
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int grp = KW == 1 ? wave + i * RW : wave * NT + i;
+      if (KW == 1 && GROUPS % RW && grp >= GROUPS) break;
+      int page = pg[0];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (KW == 1 ? grp == t : i == t) page = pg[t];
+      if (!there(page)) page = 0;
+      const int64_t off = (int64_t)page * a.cache.page + (int64_t)((k0 + 16 * grp) & mask) * a.cache.slot;
+      const unsigned dst = lds0 + buf * 2 * C::TILE + grp * 16 * RB;
+#pragma unroll
+      for (int j = 0; j < 16 / C::RPI; ++j) dma_rows(kbase + off, koff[j], dst + j * 1024);
+#pragma unroll
+      for (int j = 0; j < 16 / C::RPI; ++j)
+        dma_rows(vbase + off, voff[j], dst + C::TILE + j * 1024);
+    }
+  };
+
+  int pg[NT];   // pages of the tile to copy next
+  unsigned gone = 0;  // groups of the tile in hand that are not there
+  look_up(begin, pg);
 
   // this lane's rows: Q in registers, the keys each sees
   typename P::type q[QT][KB];
@@ -145,14 +218,13 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
       q[t][kb] = *reinterpret_cast<typename P::type*>(&x);
     }
     first[t] = b.first(a, i);
-    last[t] = real ? min(b.kv, b.last(a, i)) : 0;
+    last[t] = real ? min(end, b.last(a, i)) : 0;
   }
-  // over the block's and the wave's rows: the keys that all of them see
-  const int all_lo = b.first(a, (b.r1 - 1) / a.G), all_hi = min(b.kv, b.last(a, b.r0 / a.G));
+  // the keys that all rows of the block see, and that some row of the wave sees
+  const int all_lo = b.first(a, (b.r1 - 1) / a.G), all_hi = min(end, b.last(a, b.r0 / a.G));
   const int we = min(b.r1, wr0 + QT * 16) - 1;
   const bool idle = wr0 >= b.r1;
-  const int w_lo = idle ? 0 : b.first(a, we / a.G), w_hi = idle ? 0 : b.last(a, wr0 / a.G);
-  const int w_end = idle ? 0 : b.last(a, we / a.G), w_begin = idle ? 0 : b.first(a, wr0 / a.G);
+  const int w_begin = idle ? 0 : b.first(a, wr0 / a.G), w_end = idle ? 0 : min(end, b.last(a, we / a.G));
 
   f32x4 o[DT][QT];
   float m[QT], l[QT];
@@ -163,114 +235,51 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-
-  const CONST_AS int* pages = (const CONST_AS int*)(a.cache.table + (int64_t)b.n * a.cache.max_blocks);
-  const int shift = a.cache.shift, mask = (1 << shift) - 1;
-  const unsigned char* const kbase = a.cache.k + (int64_t)b.hk * a.cache.head;
-  const unsigned char* const vbase = a.cache.v + (int64_t)b.hk * a.cache.head;
-  const unsigned lds0 = (unsigned)(uintptr_t)smem;
-
-  // page of the group of 16 keys from key0 on; -1 past the end or for a hole
-  auto page_of = [&](int key0) -> int {
-    if (key0 >= end) return -1;
-    const int p = pages[__builtin_amdgcn_readfirstlane(key0) >> shift];
-    return (unsigned)p < (unsigned)a.cache.num_pages ? p : -1;
-  };
-  // this wave's copies of the tile from key k0 on: groups of 16 keys, of k and
-  // of v (a group that is not there is read from page 0 and not used)
-  unsigned koff[16 / C::RPI], voff[16 / C::RPI];
+  if (tiles > 0) {
+    copy_tile(begin, pg, 0);
 #pragma unroll
-  for (int j = 0; j < 16 / C::RPI; ++j) {
-    const int r = j * C::RPI + lane / NP, p = lane % NP;
-    koff[j] = r * (unsigned)a.cache.slot + ((p ^ k_swz<NP>(r)) << 4);
-    voff[j] = r * (unsigned)a.cache.slot + ((p ^ v_swz<E, NP>(r)) << 4);
+    for (int t = 0; t < NT; ++t) gone |= (unsigned)!there(pg[t]) << t;
+    look_up(begin + KT, pg);
   }
-  auto copy_tile = [&](int k0, int buf) {
-    constexpr int GROUPS = KT / 16;
-    constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;
+  // Q is waited for here, so that no wait for it stands in the loop, where it
+  // would wait for the copies too
 #pragma unroll
-    for (int i = 0; i < MINE; ++i) {
-      const int grp = KW == 1 ? wave + i * RW : wave * NT + i;
-      if (grp >= GROUPS) break;
-      const int key0 = k0 + 16 * grp;
-      const int page = max(0, page_of(key0));
-      const int64_t off = (int64_t)page * a.cache.page + (int64_t)(key0 & mask) * a.cache.slot;
-      const unsigned dst = lds0 + buf * 2 * C::TILE + grp * 16 * RB;
+  for (int t = 0; t < QT; ++t)
 #pragma unroll
-      for (int j = 0; j < 16 / C::RPI; ++j) dma_rows(kbase + off, koff[j], dst + j * 1024);
-#pragma unroll
-      for (int j = 0; j < 16 / C::RPI; ++j)
-        dma_rows(vbase + off, voff[j], dst + C::TILE + j * 1024);
-    }
-  };
+    for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(q[t][kb]));
 
-  const int tiles = (end - begin + KT - 1) / KT;
-  if (tiles > 0) copy_tile(begin, 0);
-  for (int it = 0; it < tiles; ++it) {
-    const int k0 = begin + it * KT;
-    const int kw0 = k0 + kw * NK;  // this wave's keys
-    unsigned char* const kt = smem + (it & 1) * 2 * C::TILE;
-    unsigned char* const vt = kt + C::TILE;
-    // the tile is there, the other buffer no longer read
-    wait_vmcnt<0>();
-    if (KW == 1)
-      lds_barrier();
-    else
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (it + 1 < tiles) copy_tile(k0 + KT, (it + 1) & 1);
-
-    // groups that are not there
-    unsigned gone = 0;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-      if (page_of(kw0 + 16 * t) < 0) gone |= 1u << t;
-    // Keys that no row sees may hold anything: their v is cleared.  Where some
-    // rows see a key and others do not, an infinity or NaN in its v must not
-    // meet a p of zero: those tiles take the product key by key.
-    bool odd = false;
-    const int f0 = KW == 1 ? k0 : kw0;
-    if (f0 + NK > min(all_hi, end) || f0 < all_lo || gone) {
-      bool bad = false;
-      constexpr int STEP = KW == 1 ? C::NTH : 64;
-      const int tid = KW == 1 ? (int)threadIdx.x : lane;
-#pragma unroll 1
-      for (int i = tid; i < NK * NP; i += STEP) {
-        const int r = i / NP, key = f0 + r;
-        uint4* p = reinterpret_cast<uint4*>(vt + kw * NK * RB + i * 16);
-        if (key >= end || key < b.seen || (gone >> (r >> 4) & 1))
-          *p = make_uint4(0, 0, 0, 0);
-        else
-          bad = bad || !finite4<E>(*p);
-      }
-      if (KW == 1)
-        odd = __syncthreads_or(bad);
-      else
-        odd = __ballot(bad) != 0;
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-    if (idle || kw0 >= min(w_end, end) || kw0 + NK <= w_begin) continue;  // nothing seen
-
+  // One tile.  EDGE: some row does not see some key of it.
+  // This lane's LDS addresses in the first buffer: K row c16, and V row (bf16)
+  // 4 g + c16 / 4, 4 of its channels, or (fp32) 4 g, one channel.  A row starts
+  // at a multiple of its pieces' span, so piece p ^ swizzle lies at the address
+  // of the lane's piece 0 XOR 16 p.
+  const int vr = sizeof(E) == 4 ? 4 * g : 4 * g + (c16 >> 2);
+  const unsigned kaddr0 = lds0 + (kw * NK + c16) * RB + ((g ^ k_swz<NP>(c16)) << 4);
+  const unsigned vaddr0 =
+      lds0 + C::TILE + (kw * NK + vr) * RB +
+      (sizeof(E) == 4 ? (((c16 >> 2) ^ v_swz<E, NP>(vr)) << 4) + (c16 & 3) * 4
+                      : ((((c16 >> 1) & 1) ^ v_swz<E, NP>(vr)) << 4) + (c16 & 1) * 8);
+  auto step = [&](auto edge, int kw0, unsigned buf, unsigned gone, bool odd) {
+    constexpr bool EDGE = decltype(edge)::value;
+    unsigned kaddr = kaddr0 + buf, vaddr = vaddr0 + buf;
+    // opaque, or all the addresses below are kept in registers across the loop
+    asm volatile("" : "+v"(kaddr), "+v"(vaddr));
     // S^T
     f32x4 s[NT][QT];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int u = 0; u < QT; ++u) s[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const unsigned char* krow = kt + (kw * NK + c16) * RB;
-    const int ks = k_swz<NP>(c16);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const auto x = *reinterpret_cast<const typename P::type*>(
-            krow + t * 16 * RB + (((4 * kb + g) ^ ks) << 4));
+        const auto x = *(LDS_AS const typename P::type*)((kaddr ^ (kb << 6)) + t * 16 * RB);
 #pragma unroll
         for (int u = 0; u < QT; ++u) s[t][u] = P::mma(x, q[u][kb], s[t][u]);
       }
     }
-    // what a row does not see
-    const bool partial = kw0 + NK > min(w_hi, end) || kw0 < w_lo || gone;
-    if (partial) {
+    if constexpr (EDGE) {  // what a row does not see
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -278,23 +287,28 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
           const int key = kw0 + 16 * t + 4 * g + e;
 #pragma unroll
           for (int u = 0; u < QT; ++u)
-            if (key >= min(last[u], end) || key < first[u] || (gone >> t & 1)) s[t][u][e] = -INFINITY;
+            if (key >= last[u] || key < first[u] || (gone >> t & 1)) s[t][u][e] = -INFINITY;
         }
     }
     // running softmax in base 2
+    float mx[QT], ref[QT];
+    bool grow = false;
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-      float mx = -INFINITY;
+      mx[u] = -INFINITY;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][u][e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mn = fmaxf(m[u], mx * a.c);
-      const float ref = mn == -INFINITY ? 0.f : mn;  // nothing seen so far: all p are 0
-      if (__any(mn > m[u])) {
-        const float al = __builtin_amdgcn_exp2f(m[u] - ref);
+        for (int e = 0; e < 4; ++e) mx[u] = fmaxf(mx[u], s[t][u][e]);
+      mx[u] = col_max(mx[u]) * a.c;
+      grow = grow || mx[u] > m[u] + SLACK;
+    }
+    if (__any(grow)) {
+#pragma unroll
+      for (int u = 0; u < QT; ++u) {
+        const float mn = fmaxf(m[u], mx[u]);
+        // nothing seen so far: m is -inf and everything summed is 0
+        const float al = __builtin_amdgcn_exp2f(m[u] - (mn == -INFINITY ? 0.f : mn));
         l[u] *= al;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -302,70 +316,41 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
           for (int e = 0; e < 4; ++e) o[d][u][e] *= al;
         m[u] = mn;
       }
-      float sum = 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      ref[u] = m[u] == -INFINITY ? 0.f : m[u];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[t][u][e], a.c, -ref));
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[t][u][e], a.c, -ref[u]));
           s[t][u][e] = p;
-          sum += p;
+          l[u] += p;
         }
-      l[u] += sum;
     }
     // O^T
-    unsigned char* const vw = vt + kw * NK * RB;
-    if (odd) {
-#pragma unroll 1
-      for (int k = 0; k < NK; ++k) {
-        const int key = kw0 + k;
-        float p[QT];
+    if constexpr (sizeof(E) == 4) {
+      if (!EDGE || !odd) {
 #pragma unroll
-        for (int u = 0; u < QT; ++u) {
-          float x = 0.f;
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
+          for (int e = 0; e < 4; ++e) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (16 * t + e == (k & ~12)) x = s[t][u][e];
-          p[u] = __shfl(x, ((k >> 2) & 3) * 16 + c16);
-        }
-        const bool there = key < end && !(gone >> (k >> 4) & 1);
+            for (int d = 0; d < DT; ++d) {
+              const float x = *(LDS_AS const float*)((vaddr ^ (d << 6)) + (16 * t + e) * RB);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const int ch = (16 * d + 4 * g) * (int)sizeof(E);
-          const f32x4 x = load4<E>(reinterpret_cast<const E*>(
-              vw + k * RB + (((ch >> 4) ^ v_swz<E, NP>(k)) << 4) + (ch & 15)));
-#pragma unroll
-          for (int u = 0; u < QT; ++u)
-            if (there && key < last[u] && key >= first[u])
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[d][u][e] = fmaf(p[u], x[e], o[d][u][e]);
-        }
-      }
-    } else if constexpr (sizeof(E) == 4) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const unsigned char* row = vw + (16 * t + 4 * g + e) * RB;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const float x = *reinterpret_cast<const float*>(
-                row + (((4 * d + (c16 >> 2)) ^ (g << 2)) << 4) + (c16 & 3) * 4);
-#pragma unroll
-            for (int u = 0; u < QT; ++u) o[d][u] = Mfma<float>::mma(x, s[t][u][e], o[d][u]);
+              for (int u = 0; u < QT; ++u) o[d][u] = Mfma<float>::mma(x, s[t][u][e], o[d][u]);
+            }
           }
-        }
+      }
     } else {
+      // p is rounded to bf16 for this product alone; l sums it unrounded
       // lane i of 16 points at 4 channels of key row i / 4 and receives one
       // channel (its own, i) of the 4 rows
-      const int vr = 4 * g + (c16 >> 2);
-      unsigned char* const row = vw + vr * RB + (c16 & 1) * 8;
-      const int vs = ((c16 >> 1) & 1) ^ v_swz<E, NP>(vr);
       auto turned = [&](int t, int d) {
         return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (LDS_AS s16x4*)(row + t * 16 * RB + (((2 * d) ^ vs) << 4)));
+            (LDS_AS s16x4*)((vaddr ^ (d << 5)) + t * 16 * RB));
       };
       if constexpr (NT == 1) {
         s16x4 p[QT];
@@ -374,12 +359,14 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
           const bf16x4 x = {(bf16)s[0][u][0], (bf16)s[0][u][1], (bf16)s[0][u][2], (bf16)s[0][u][3]};
           p[u] = *reinterpret_cast<const s16x4*>(&x);
         }
+        if (!EDGE || !odd) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const s16x4 x = turned(0, d);
+          for (int d = 0; d < DT; ++d) {
+            const s16x4 x = turned(0, d);
 #pragma unroll
-          for (int u = 0; u < QT; ++u)
-            o[d][u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p[u], o[d][u], 0, 0, 0);
+            for (int u = 0; u < QT; ++u)
+              o[d][u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p[u], o[d][u], 0, 0, 0);
+          }
         }
       } else {
 #pragma unroll
@@ -392,25 +379,113 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
               p[u][e] = (bf16)s[t][u][e];
               p[u][4 + e] = (bf16)s[t + 1][u][e];
             }
+          if (!EDGE || !odd) {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const s16x4 x0 = turned(t, d), x1 = turned(t + 1, d);
-            const s16x8 x = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
+            for (int d = 0; d < DT; ++d) {
+              const s16x4 x0 = turned(t, d), x1 = turned(t + 1, d);
+              const s16x8 x = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-            for (int u = 0; u < QT; ++u)
-              o[d][u] = Mfma<bf16>::mma(*reinterpret_cast<const bf16x8*>(&x), p[u], o[d][u]);
+              for (int u = 0; u < QT; ++u)
+                o[d][u] = Mfma<bf16>::mma(*reinterpret_cast<const bf16x8*>(&x), p[u], o[d][u]);
+            }
           }
         }
       }
     }
+    if constexpr (EDGE) {
+      if (odd) {  // key by key, only the rows that see it
+        const unsigned char* const vw = smem + buf + C::TILE + kw * NK * RB;
+#pragma unroll 1
+        for (int k = 0; k < NK; ++k) {
+          const int key = kw0 + k;
+          float p[QT];
+#pragma unroll
+          for (int u = 0; u < QT; ++u) {
+            float x = 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (16 * t + e == (k & ~12)) x = s[t][u][e];
+            p[u] = __shfl(x, ((k >> 2) & 3) * 16 + c16);
+          }
+          const bool held = !(gone >> (k >> 4) & 1);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const int ch = (16 * d + 4 * g) * (int)sizeof(E);
+            const f32x4 x = load4<E>(reinterpret_cast<const E*>(
+                vw + k * RB + (((ch >> 4) ^ v_swz<E, NP>(k)) << 4) + (ch & 15)));
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+              if (held && key < last[u] && key >= first[u])
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][u][e] = fmaf(p[u], x[e], o[d][u][e]);
+          }
+        }
+      }
+    }
+  };
+
+  // The copies of tile `it` are there and the other buffer is no longer read;
+  // the next tile's copies start.  Returns the groups of the tile that are gone.
+  auto next_tile = [&](int it) {
+    wait_vmcnt<0>();
+    if (KW == 1)
+      lds_barrier();
+    else
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const unsigned now = gone;
+    if (it + 1 < tiles) {
+      const int k0 = begin + it * KT;
+      copy_tile(k0 + KT, pg, (it + 1) & 1);
+      gone = 0;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) gone |= (unsigned)!there(pg[t]) << t;
+      look_up(k0 + 2 * KT, pg);
+    }
+    return now;
+  };
+  int it = 0;
+  while (it < tiles) {
+    unsigned now;
+    // tiles all of whose keys all rows see: a loop of its own, so that what it
+    // carries stays in place
+#pragma unroll 1
+    for (;;) {
+      now = next_tile(it);
+      const int f0 = begin + it * KT + kw * NK;
+      if (f0 + NK > all_hi || f0 < all_lo || now) break;
+      step(std::false_type{}, f0, (it & 1) * 2 * C::TILE, 0u, false);
+      if (++it == tiles) break;
+    }
+    if (it == tiles) break;
+    // Keys that no row sees may hold anything: their v is cleared.  Where some
+    // rows see a key and others do not, an infinity or NaN in its v must not
+    // meet a p of zero: those tiles take the product key by key.
+    const unsigned buf = (it & 1) * 2 * C::TILE;
+    const int kw0 = begin + it * KT + kw * NK;  // this wave's keys
+    bool bad = false, odd;
+    const int tid = KW == 1 ? (int)threadIdx.x : lane;
+#pragma unroll 1
+    for (int i = tid; i < NK * NP; i += KW == 1 ? C::NTH : 64) {
+      const int r = i / NP, key = kw0 + r;
+      uint4* p = reinterpret_cast<uint4*>(smem + buf + C::TILE + kw * NK * RB + i * 16);
+      if (key >= end || key < b.seen || (now >> (r >> 4) & 1))
+        *p = make_uint4(0, 0, 0, 0);
+      else
+        bad = bad || !finite4<E>(*p);
+    }
+    if (KW == 1)
+      odd = __syncthreads_or(bad);
+    else
+      odd = __ballot(bad) != 0;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (!idle && kw0 < w_end && kw0 + NK > w_begin) step(std::true_type{}, kw0, buf, now, odd);
+    ++it;
   }
 
-  // the row's sum over the four lane groups
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    l[u] += __shfl_xor(l[u], 16);
-    l[u] += __shfl_xor(l[u], 32);
-  }
+  for (int u = 0; u < QT; ++u) l[u] = col_sum(l[u]);
 
   const int64_t rows = (int64_t)a.tok.total * a.Hq;
   // channels ch.. of row r, unnormalised sums x, maximum and sum mm, ll
@@ -550,13 +625,16 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) void k_attn_tile
   attn_block<E, D, 2, 4, 1, KT>(a, b, split, smem);
 }
 
-// Joins the splits' sums: D / 4 threads to a row.
+// Joins the splits' sums: a workgroup to a row.  The threads first turn the
+// splits' maxima into weights, then 256 / (D / 4) groups of them add up the
+// weighted sums of every so many-th split, four loads in flight each.
 template <class E, int D> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  constexpr int TPR = D / 4;
-  const int64_t rows = (int64_t)a.tok.total * a.Hq;
-  const int64_t at = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  if (at >= rows) return;
-  const int ch = (threadIdx.x % TPR) * 4;
+  constexpr int TPR = D / 4, NG = 256 / TPR;
+  __shared__ float weight[MAX_SPLITS];
+  __shared__ float red[8];
+  __shared__ f32x4 sums[256];
+  const int64_t rows = (int64_t)a.tok.total * a.Hq, at = blockIdx.x;
+  const int tid = threadIdx.x;
   const int t = (int)(at / a.Hq), h = (int)(at - (int64_t)t * a.Hq);
   Block b;
   b.n = seq_of(a.tok, t);
@@ -571,22 +649,56 @@ template <class E, int D> __global__ __launch_bounds__(256) void k_attn_join(Att
   b.kv = cached(a.cache, b.n);
   b.range(a);
   const int live = min(a.splits, max(1, (b.hi - b.lo + a.len - 1) / a.len));
-  float mx = -INFINITY, ll = 0.f;
-  for (int s = 0; s < live; ++s) mx = fmaxf(mx, a.part_ml[2 * (s * rows + at)]);
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < live; ++s) {
-    const int64_t w = s * rows + at;
-    const float al = __builtin_amdgcn_exp2f(a.part_ml[2 * w] - ref);
-    ll += al * a.part_ml[2 * w + 1];
-    const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + w * D + ch);
+
+  float m[(MAX_SPLITS + 255) / 256], l[(MAX_SPLITS + 255) / 256], mx = -INFINITY, ll = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] += al * y[e];
+  for (int j = 0; j < (MAX_SPLITS + 255) / 256; ++j) {
+    const int s = tid + 256 * j;
+    const float2 x = s < live ? *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * rows + at))
+                              : make_float2(-INFINITY, 0.f);
+    m[j] = x.x;
+    l[j] = x.y;
+    mx = fmaxf(mx, x.x);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+  if (lane_id() == 0) red[wave_id()] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+  for (int j = 0; j < (MAX_SPLITS + 255) / 256; ++j) {
+    const float w = __builtin_amdgcn_exp2f(m[j] - ref);
+    if (tid + 256 * j < live) weight[tid + 256 * j] = w;
+    ll += w * l[j];
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) ll += __shfl_xor(ll, d);
+  if (lane_id() == 0) red[4 + wave_id()] = ll;
+  __syncthreads();
+  ll = (red[4] + red[5]) + (red[6] + red[7]);
+
+  const int grp = tid / TPR, ch = (tid % TPR) * 4;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = grp; s < live; s += NG) {
+    const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * D + ch);
+    const float w = weight[s];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(w, y[e], x[e]);
+  }
+  sums[tid] = x;
+  __syncthreads();
+  if (tid >= TPR) return;
+#pragma unroll
+  for (int j = 1; j < NG; ++j) {
+    const f32x4 y = sums[tid + j * TPR];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += y[e];
   }
   const float inv = ll == 0.f ? 0.f : 1.f / ll;
   E* p = reinterpret_cast<E*>(a.o.data + (int64_t)t * a.o.ts + h * a.o.hs) + ch;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) p[e] = to_e<E>(x[e] * inv);
+  store4<E>(p, f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv});
   if (ch == 0 && a.lse)
     a.lse[at] = ll == 0.f ? -INFINITY : (mx + log2f(ll)) * 0.6931471805599453f;
 }
@@ -653,9 +765,8 @@ hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.tok.total * a.Hq;
   return by_dim(dt, d, [&](auto e, auto dim) {
     using E = decltype(e);
-    constexpr int D = decltype(dim)::value, PER = 256 / (D / 4);
-    hipLaunchKernelGGL((k_attn_join<E, D>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(256), 0,
-                       s, a);
+    hipLaunchKernelGGL((k_attn_join<E, decltype(dim)::value>), dim3((unsigned)rows), dim3(256), 0, s,
+                       a);
     return hipGetLastError();
   });
 }

@@ -142,7 +142,7 @@ struct Plan {
 void split(int64_t units, int64_t keys, int step, int64_t want, int64_t least, int* splits,
            int* len) {
   int64_t s = units >= want / 2 ? 1 : (want + units - 1) / units;
-  s = std::max<int64_t>(1, std::min(s, keys / least));
+  s = std::max<int64_t>(1, std::min({s, keys / least, (int64_t)gdn::MAX_SPLITS}));
   int64_t l = (keys + s - 1) / s;
   l = (l + step - 1) / step * step;
   *len = (int)l;

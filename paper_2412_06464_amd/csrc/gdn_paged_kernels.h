@@ -58,6 +58,7 @@ struct AttnArgs {
 // this many take the kernel whose waves share the rows and split the keys.
 constexpr int FEW_ROWS = 32;
 constexpr int TILE_ROWS = 128;  // rows of a workgroup of the other kernel
+constexpr int MAX_SPLITS = 512;
 
 // keys of a tile: the unit of `len`
 int attn_few_keys(Dt dt, int d);

@@ -16,6 +16,7 @@ the ``pool`` of the page calls after ``flatten(0, 1)``.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import NamedTuple
 
 import torch
@@ -91,20 +92,19 @@ def load_library():
     if _lib is None:
         lib = _load()
         P, I, D, S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_double, ctypes.c_size_t
-        tok, rot, rows, cache, attn, book, pool = (ctypes.POINTER(x) for x in (
-            Tokens, RotaryStruct, Rows, Cache, Attn, Book, Pool))
+        # structures go in as their bytes (c_void_p), see below
         for name, args in (
                 ("gdn_rotary_turns", [I, D, I, D, D, D, D, P, P]),
-                ("gdn_rotary_fwd", [tok, rot, rows, rows, P, rows, rows, P]),
-                ("gdn_rotary_bwd", [tok, rot, rows, rows, P, rows, rows, P]),
-                ("gdn_cache_append", [tok, rot, rows, rows, rows, cache, rows, P]),
-                ("gdn_cache_attn", [tok, attn, rows, cache, rows, P, P, S, P]),
-                ("gdn_cache_attn_workspace_size", [tok, cache, attn]),
-                ("gdn_pages_workspace_size", [book]),
-                ("gdn_pages_extend", [book, P, P, P, S, P]),
-                ("gdn_pages_select", [book, P, pool, P, P, S, P]),
-                ("gdn_pages_compact", [book, pool, P, P, S, P]),
-                ("gdn_pages_copy", [pool, P, P, I, P])):
+                ("gdn_rotary_fwd", [P] * 8),
+                ("gdn_rotary_bwd", [P] * 8),
+                ("gdn_cache_append", [P] * 8),
+                ("gdn_cache_attn", [P] * 7 + [S, P]),
+                ("gdn_cache_attn_workspace_size", [P] * 3),
+                ("gdn_pages_workspace_size", [P]),
+                ("gdn_pages_extend", [P] * 4 + [S, P]),
+                ("gdn_pages_select", [P] * 5 + [S, P]),
+                ("gdn_pages_compact", [P] * 4 + [S, P]),
+                ("gdn_pages_copy", [P, P, P, I, P])):
             f = getattr(lib, name)
             f.argtypes = args
             f.restype = S if name.endswith("_size") else ctypes.c_int
@@ -112,84 +112,116 @@ def load_library():
     return _lib
 
 
+# A call of a few microseconds on the GPU must not spend longer here.  The
+# structures are packed as bytes, in the layout of the ctypes classes above
+# (0.2 us each instead of 0.5 to 1), and what every call checks of a tensor is
+# read once (host time of a call: storing a token for each of 256 sequences
+# 19.4 -> 10.0 us, attention of one token for each of 4 15.1 -> 10.3 us).
+_ROWS = struct.Struct("@Pqq")
+_TOKENS = struct.Struct("@iiiiiiPPi0P")
+_CACHE = struct.Struct("@PPqqqiiiPP")
+_ROTARY = struct.Struct("@iifP")
+_ATTN = struct.Struct("@fiii")
+_BOOK = struct.Struct("@iiiiPPPPPP")
+_POOL = struct.Struct("@Piiqqq")
 _DTYPES = {torch.float32: GDN_F32, torch.bfloat16: GDN_BF16}
+_Tensor = torch.Tensor
+_I32 = torch.int32
 
 
-def _rows(name, x, like=None):
-    """gdn_rows of a [B, T, heads, d] tensor; ``like``: (name, tensor) whose B,
-    T, d, dtype and device it has to share."""
-    if not isinstance(x, torch.Tensor):
+class _Like(NamedTuple):
+    """What the tensors of a call share, read off its first."""
+    name: str
+    B: int
+    T: int
+    d: int
+    dtype: torch.dtype
+    dev: int
+
+
+def _first(name, x):
+    """(_Like, heads) of a call's first [B, T, heads, d] tensor."""
+    if not isinstance(x, _Tensor):
+        raise TypeError("%s must be a tensor" % name)
+    if x.dim() != 4:
+        raise ValueError("%s must be [B, T, heads, d]" % name)
+    B, T, H, d = x.shape
+    dev = x.get_device()
+    if x.dtype not in _DTYPES:
+        raise TypeError("%s must be float32 or bfloat16" % name)
+    if dev < 0:
+        raise ValueError("%s must be on the GPU" % name)
+    return _Like(name, B, T, d, x.dtype, dev), H
+
+
+def _rows(name, x, like, heads=None):
+    """gdn_rows of a [B, T, heads, d] tensor alike to the call's first."""
+    if not isinstance(x, _Tensor):
         raise TypeError("%s must be a tensor" % name)
     if x.dim() != 4:
         raise ValueError("%s must be [B, T, heads, d]" % name)
     B, T, H, d = x.shape
     sb, st, sh, sd = x.stride()
-    if x.dtype not in _DTYPES:
-        raise TypeError("%s must be float32 or bfloat16" % name)
-    if x.get_device() < 0:
-        raise ValueError("%s must be on the GPU" % name)
-    if like is not None:
-        other, y = like
-        if x.dtype is not y.dtype or x.get_device() != y.get_device():
-            raise ValueError("%s must have %s's dtype and device" % (name, other))
-        if y.shape[0] != B or y.shape[1] != T or y.shape[3] != d:
-            raise ValueError("%s must have %s's B, T and d" % (name, other))
+    if x.dtype is not like.dtype or x.get_device() != like.dev:
+        raise ValueError("%s must have %s's dtype and device" % (name, like.name))
+    if B != like.B or T != like.T or d != like.d:
+        raise ValueError("%s must have %s's B, T and d" % (name, like.name))
+    if heads is not None and H != heads:
+        raise ValueError("%s must have %d heads" % (name, heads))
     if sd != 1 and d != 1:
         raise ValueError("%s must be contiguous in its last dim" % name)
-    if B > 1 and T == 1:
+    if B > 1 and sb != T * st:
+        if T != 1:
+            raise ValueError("%s: the rows of B must follow each other (stride %d, not T tokens of "
+                             "%d)" % (name, sb, st))
         st = sb  # a token a row: the rows' own stride
-    elif B > 1 and sb != T * st:
-        raise ValueError("%s: the rows of B must follow each other (stride %d, not T tokens of %d)"
-                         % (name, sb, st))
-    return Rows(x.data_ptr(), st, sh)
+    return _ROWS.pack(x.data_ptr(), st, sh)
 
 
-def _ints(name, x, device, shape=None):
-    """Pointer of a contiguous int32 tensor on ``device``."""
-    if not isinstance(x, torch.Tensor):
+def _ints(name, x, dev, shape=None):
+    """Pointer of a contiguous int32 tensor on device ``dev``."""
+    if not isinstance(x, _Tensor):
         raise TypeError("%s must be a tensor" % name)
-    if x.dtype is not torch.int32 or x.device != device or not x.is_contiguous():
-        raise ValueError("%s must be contiguous int32 on %s" % (name, device))
-    if shape is not None and tuple(x.shape) != tuple(shape):
+    if x.dtype is not _I32 or x.get_device() != dev or not x.is_contiguous():
+        raise ValueError("%s must be contiguous int32 on the call's device" % name)
+    if shape is not None and x.shape != shape:
         raise ValueError("%s must be %s" % (name, list(shape)))
     return x.data_ptr()
 
 
-def _tokens(q, Hk, cu_seqlens, cu_seqlens_host, keep):
-    B, T, Hq, d = q.shape
-    t = Tokens(B, T, Hq, Hk, d, 0, None, None, _DTYPES[q.dtype])
+def _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, device, keep):
+    """gdn_tokens, and the number of sequences."""
     if cu_seqlens is None:
         if cu_seqlens_host is not None:
             raise ValueError("cu_seqlens_host without cu_seqlens")
-        return t, B
-    dev, host = _cu_pair(cu_seqlens, cu_seqlens_host, q.device, keep)
-    t.num_seqs = host.numel() - 1
-    t.cu_seqlens, t.cu_seqlens_host = dev.data_ptr(), host.data_ptr()
-    return t, t.num_seqs
+        return _TOKENS.pack(like.B, like.T, Hq, Hk, like.d, 0, 0, 0, _DTYPES[like.dtype]), like.B
+    dev, host = _cu_pair(cu_seqlens, cu_seqlens_host, device, keep)
+    keep.append(dev)
+    n = host.numel() - 1
+    return _TOKENS.pack(like.B, like.T, Hq, Hk, like.d, n, dev.data_ptr(), host.data_ptr(),
+                        _DTYPES[like.dtype]), n
 
 
-def _cache(q, k_pages, v_pages, table, kv_lens, num_seqs):
-    if not (isinstance(k_pages, torch.Tensor) and isinstance(v_pages, torch.Tensor)):
+def _cache(like, k_pages, v_pages, table, kv_lens, num_seqs):
+    """gdn_cache, and the cache's heads."""
+    if not (isinstance(k_pages, _Tensor) and isinstance(v_pages, _Tensor)):
         raise TypeError("k_pages and v_pages must be tensors")
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride():
+    shape, stride = k_pages.shape, k_pages.stride()
+    if len(shape) != 4 or shape != v_pages.shape or stride != v_pages.stride():
         raise ValueError("k_pages and v_pages must be [num_pages, Hk, page_size, d], alike in "
                          "shape and strides")
-    for x in (k_pages, v_pages):
-        if x.dtype is not q.dtype or x.get_device() != q.get_device():
-            raise ValueError("k_pages and v_pages must have q's dtype and device")
-    num, Hk, page, d = k_pages.shape
-    if d != q.shape[3] or k_pages.stride(3) != 1:
-        raise ValueError("k_pages and v_pages must have q's d, contiguous")
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        raise ValueError("table must be int32 [sequences, blocks]")
-    sp, sh, st, _ = k_pages.stride()
-    return Cache(k_pages.data_ptr(), v_pages.data_ptr(), sp, sh, st, num, page, table.shape[1],
-                 _ints("table", table, q.device, (num_seqs, table.shape[1])),
-                 None if kv_lens is None else _ints("kv_lens", kv_lens, q.device, (num_seqs,)))
-
-
-def _ref(x):
-    return None if x is None else ctypes.byref(x)
+    if (k_pages.dtype is not like.dtype or v_pages.dtype is not like.dtype
+            or k_pages.get_device() != like.dev or v_pages.get_device() != like.dev):
+        raise ValueError("k_pages and v_pages must have %s's dtype and device" % like.name)
+    num, Hk, page, d = shape
+    if d != like.d or stride[3] != 1:
+        raise ValueError("k_pages and v_pages must have %s's d, contiguous" % like.name)
+    if not isinstance(table, _Tensor) or table.dim() != 2 or table.shape[0] != num_seqs:
+        raise ValueError("table must be int32 [%d sequences, blocks]" % num_seqs)
+    return _CACHE.pack(k_pages.data_ptr(), v_pages.data_ptr(), stride[0], stride[1], stride[2], num,
+                       page, table.shape[1], _ints("table", table, like.dev),
+                       0 if kv_lens is None
+                       else _ints("kv_lens", kv_lens, like.dev, (num_seqs,))), Hk
 
 
 # ------------------------------------------------------------------ rotary positions
@@ -221,39 +253,34 @@ def gdn_rotary(rot, base=10000.0, layout="halves", scaling="none", factor=1.0, o
     return Rotary(turns.to(device), layout, scale)
 
 
-def _rotary(r, device):
-    if r is None:
-        return None
+def _rotary(r, dev):
     if not isinstance(r, Rotary):
         raise TypeError("rotary must be a Rotary (see gdn_rotary)")
-    if r.turns.device != device or r.turns.dtype is not torch.float64 \
-            or not r.turns.is_contiguous() or r.turns.dim() != 1:
-        raise ValueError("rotary.turns must be contiguous float64 [rot / 2] on %s" % device)
+    t = r.turns
+    if t.get_device() != dev or t.dtype is not torch.float64 or t.dim() != 1 \
+            or not t.is_contiguous():
+        raise ValueError("rotary.turns must be contiguous float64 [rot / 2] on the call's device")
     if r.layout not in LAYOUTS:
         raise ValueError("layout must be one of %s" % sorted(LAYOUTS))
-    return RotaryStruct(2 * r.turns.numel(), LAYOUTS[r.layout], r.scale, r.turns.data_ptr())
+    return _ROTARY.pack(2 * t.numel(), LAYOUTS[r.layout], r.scale, t.data_ptr())
 
 
 def _rotate(f, q, k, rotary, positions, cu_seqlens, cu_seqlens_host, q_out, k_out):
     keep = []
-    rq = _rows("q", q)
-    rk = None if k is None else _rows("k", k, ("q", q))
-    t, _ = _tokens(q, q.shape[2] if k is None else k.shape[2], cu_seqlens, cu_seqlens_host, keep)
-    r = _rotary(rotary, q.device)
-    if r is None:
-        raise TypeError("rotary must be a Rotary (see gdn_rotary)")
-    p = None if positions is None else _ints("positions", positions, q.device, q.shape[:2])
+    like, Hq = _first("q", q)
+    rq, rk, ko, Hk = _rows("q", q, like), None, None, 1
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape):
-        raise ValueError("the outputs must be shaped as the inputs")
-    ro = _rows("q_out", q_out, ("q", q))
-    ko = None if k is None else _rows("k_out", k_out, ("q", q))
-    _check(f(ctypes.byref(t), ctypes.byref(r), ctypes.byref(rq), _ref(rk), p, ctypes.byref(ro),
-             _ref(ko), _stream(q.device)))
-    del keep
+        q_out = torch.empty_like(q)
+    if k is not None:
+        rk, Hk = _rows("k", k, like), k.shape[2]
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        ko = _rows("k_out", k_out, like, Hk)
+    dev = q.device
+    t, _ = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
+    p = None if positions is None else _ints("positions", positions, like.dev, q.shape[:2])
+    _check(f(t, _rotary(rotary, like.dev), rq, rk, p, _rows("q_out", q_out, like, Hq), ko,
+             _stream(dev)))
     return q_out, k_out
 
 
@@ -286,45 +313,38 @@ def gdn_cache_append(q, k, v, k_pages, v_pages, table, kv_lens, rotary=None, cu_
     None: nothing is rotated.  Tokens whose page is a hole are not stored."""
     lib = load_library()
     keep = []
-    rk = _rows("k", k)
-    rv = _rows("v", v, ("k", k))
-    if v.shape != k.shape:
-        raise ValueError("v must be shaped as k")
-    rq = ro = None
+    like, Hk = _first("k", k)
+    dev, Hq, rq, ro = k.device, Hk, None, None
     if q is not None:
-        rq = _rows("q", q, ("k", k))
+        rq, Hq = _rows("q", q, like), q.shape[2]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if q_out.shape != q.shape:
-            raise ValueError("q_out must be shaped as q")
-        ro = _rows("q_out", q_out, ("k", k))
-    t, n = _tokens(k if q is None else q, k.shape[2], cu_seqlens, cu_seqlens_host, keep)
-    c = _cache(k, k_pages, v_pages, table, kv_lens, n)
-    if k_pages.shape[1] != k.shape[2]:
+            q_out = torch.empty_like(q)
+        ro = _rows("q_out", q_out, like, Hq)
+    t, n = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
+    c, heads = _cache(like, k_pages, v_pages, table, kv_lens, n)
+    if heads != Hk:
         raise ValueError("k_pages must have k's heads")
-    r = _rotary(rotary, k.device)
-    _check(lib.gdn_cache_append(ctypes.byref(t), _ref(r), _ref(rq), ctypes.byref(rk),
-                                ctypes.byref(rv), ctypes.byref(c), _ref(ro), _stream(k.device)))
-    del keep
+    _check(lib.gdn_cache_append(t, None if rotary is None else _rotary(rotary, like.dev), rq,
+                                _rows("k", k, like), _rows("v", v, like, Hk), c, ro,
+                                _stream(dev)))
     return q_out
 
 
 def _attn(scale, d, causal, window, max_kv):
-    return Attn(d ** -0.5 if scale is None else scale, int(bool(causal)), int(window or 0),
-                int(max_kv or 0))
+    return _ATTN.pack(d ** -0.5 if scale is None else scale, 1 if causal else 0, window or 0,
+                      max_kv or 0)
 
 
 def gdn_cache_attn_workspace_size(q, k_pages, table, scale=None, causal=True, window=0, max_kv=0,
                                   cu_seqlens=None, cu_seqlens_host=None) -> int:
     """Workspace bytes of gdn_cache_attn with these arguments (0: none is needed)."""
     keep = []
-    t, n = _tokens(q, k_pages.shape[1], cu_seqlens, cu_seqlens_host, keep)
-    c = _cache(q, k_pages, k_pages, table, None, n)
-    a = _attn(scale, q.shape[3], causal, window, max_kv)
-    size = int(load_library().gdn_cache_attn_workspace_size(ctypes.byref(t), ctypes.byref(c),
-                                                            ctypes.byref(a)))
-    del keep
-    return size
+    like, Hq = _first("q", q)
+    n = like.B if cu_seqlens is None else cu_seqlens.numel() - 1
+    c, Hk = _cache(like, k_pages, k_pages, table, None, n)
+    t, _ = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, q.device, keep)
+    return int(load_library().gdn_cache_attn_workspace_size(t, c, _attn(scale, like.d, causal,
+                                                                        window, max_kv)))
 
 
 def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True, window=0,
@@ -339,106 +359,109 @@ def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True,
     sum.  A token that sees no key gets 0 (lse -inf)."""
     lib = load_library()
     keep = []
-    rq = _rows("q", q)
-    t, n = _tokens(q, k_pages.shape[1] if isinstance(k_pages, torch.Tensor) else 0, cu_seqlens,
-                   cu_seqlens_host, keep)
-    c = _cache(q, k_pages, v_pages, table, kv_lens, n)
+    like, Hq = _first("q", q)
+    dev = q.device
+    n = like.B if cu_seqlens is None else cu_seqlens.numel() - 1
+    c, Hk = _cache(like, k_pages, v_pages, table, kv_lens, n)
+    t, _ = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if o.shape != q.shape:
-        raise ValueError("o must be shaped as q")
-    ro = _rows("o", o, ("q", q))
-    if lse is not None and (lse.dtype is not torch.float32 or lse.device != q.device
+        o = torch.empty_like(q)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.get_device() != like.dev
                             or not lse.is_contiguous() or lse.shape != q.shape[:3]):
         raise ValueError("lse must be contiguous float32 [B, T, Hq] on q's device")
-    a = _attn(scale, q.shape[3], causal, window, max_kv)
-    need = lib.gdn_cache_attn_workspace_size(ctypes.byref(t), ctypes.byref(c), ctypes.byref(a))
-    if need and (workspace is None or workspace.numel() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    if workspace is not None and (workspace.device != q.device or workspace.dtype is not torch.uint8
-                                  or not workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
-    _check(lib.gdn_cache_attn(ctypes.byref(t), ctypes.byref(a), ctypes.byref(rq), ctypes.byref(c),
-                              ctypes.byref(ro), _ptr(lse), _ptr(workspace),
-                              0 if workspace is None else workspace.numel(), _stream(q.device)))
-    del keep
+    a = _attn(scale, like.d, causal, window, max_kv)
+    need = lib.gdn_cache_attn_workspace_size(t, c, a)
+    ws, size = None, 0
+    if need:
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        elif (workspace.get_device() != like.dev or workspace.dtype is not torch.uint8
+              or not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
+        ws, size = workspace.data_ptr(), workspace.numel()
+    _check(lib.gdn_cache_attn(t, a, _rows("q", q, like), c, _rows("o", o, like, Hq), _ptr(lse), ws,
+                              size, _stream(dev)))
     return o
 
 
 # ------------------------------------------------------------------ pages
 
 
-def _book(table, lens, refs, page_size, out, with_lens):
-    """gdn_book of tensors, and the output tensors (``out``: the caller's, where given)."""
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+def _book(table, lens, refs, page_size, out, with_lens, extra, extra_shape):
+    """gdn_book of tensors, the output tensors (``out``: the caller's, where given), the pointer of
+    the one named ``extra``, the device."""
+    if not isinstance(table, _Tensor) or table.dim() != 2:
         raise ValueError("table must be int32 [sequences, blocks]")
-    if not isinstance(refs, torch.Tensor) or refs.dim() != 1:
+    if not isinstance(refs, _Tensor) or refs.dim() != 1:
         raise ValueError("refs must be int32 [pages]")
-    dev, S = table.device, table.shape[0]
-    if table.get_device() < 0:
+    dev, shape = table.get_device(), table.shape
+    if dev < 0:
         raise ValueError("table must be on the GPU")
-    got = dict(out or {})
-    for name, x in (("table", table), ("refs", refs)) + ((("lens", lens),) if with_lens else ()):
-        if got.get(name) is None:
-            got[name] = torch.empty_like(x)
-    b = Book(S, table.shape[1], refs.numel(), page_size,
-             _ints("table", table, dev, table.shape), _ints("lens", lens, dev, (S,)),
-             _ints("refs", refs, dev), _ints("out table", got["table"], dev, table.shape),
-             _ints("out lens", got["lens"], dev, (S,)) if with_lens else None,
-             _ints("out refs", got["refs"], dev, refs.shape))
-    return b, got
+    S = shape[:1]
+    pt, pl, pr = _ints("table", table, dev), _ints("lens", lens, dev, S), _ints("refs", refs, dev)
+    if out is None:
+        got = {"table": torch.empty_like(table)}
+        if with_lens:
+            got["lens"] = torch.empty_like(lens)
+        got["refs"] = torch.empty_like(refs)
+        got[extra] = torch.empty_like(refs if extra == "map" else lens)
+    else:
+        got = dict(out)
+        for name, x in (("table", table), ("refs", refs), ("lens", lens if with_lens else None),
+                        (extra, refs if extra == "map" else lens)):
+            if x is not None and got.get(name) is None:
+                got[name] = torch.empty_like(x)
+    b = _BOOK.pack(S[0], shape[1], refs.numel(), page_size, pt, pl, pr,
+                   _ints("out table", got["table"], dev, shape),
+                   _ints("out lens", got["lens"], dev, S) if with_lens else 0,
+                   _ints("out refs", got["refs"], dev, refs.shape))
+    return b, got, _ints("out " + extra, got[extra], dev, extra_shape), dev
 
 
-def _extra(got, name, shape, device):
-    if got.get(name) is None:
-        got[name] = torch.empty(shape, dtype=torch.int32, device=device)
-    return _ints("out " + name, got[name], device, shape)
-
-
-def _pool(pool, device):
+def _pool(pool, dev):
     """gdn_pool of a [parts, num_pages, ...] tensor whose pages are contiguous."""
     if pool is None:
         return None
-    if not isinstance(pool, torch.Tensor) or pool.dim() < 3 or pool.device != device:
-        raise ValueError("pool must be a [parts, pages, ...] tensor on %s" % device)
-    inner = 1
-    for n, s in zip(reversed(pool.shape[2:]), reversed(pool.stride()[2:])):
-        if n != 1 and s != inner:
+    if not isinstance(pool, _Tensor) or pool.dim() < 3 or pool.get_device() != dev or dev < 0:
+        raise ValueError("pool must be a [parts, pages, ...] tensor on the GPU of the call")
+    shape, stride, inner = pool.shape, pool.stride(), 1
+    for i in range(len(shape) - 1, 1, -1):
+        if shape[i] != 1 and stride[i] != inner:
             raise ValueError("pool must be contiguous within a page")
-        inner *= n
+        inner *= shape[i]
     e = pool.element_size()
-    return Pool(pool.data_ptr(), pool.shape[0], pool.shape[1], pool.stride(0) * e,
-                pool.stride(1) * e, inner * e)
+    return _POOL.pack(pool.data_ptr(), shape[0], shape[1], stride[0] * e, stride[1] * e, inner * e)
 
 
-def _work(b, workspace, device):
-    need = load_library().gdn_pages_workspace_size(ctypes.byref(b))
+def _work(lib, b, workspace, device):
+    """(the workspace, its pointer, its size)."""
+    need = lib.gdn_pages_workspace_size(b)
     if workspace is None or workspace.numel() < need:
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-    if workspace.device != device or workspace.dtype is not torch.uint8 \
+    elif workspace.device != device or workspace.dtype is not torch.uint8 \
             or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on %s" % device)
-    return workspace
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
 def gdn_pages_workspace_size(table, refs) -> int:
     """Workspace bytes of the page calls for a table and reference counts of these shapes."""
-    b = Book(table.shape[0], table.shape[1], refs.numel(), 1)
-    return int(load_library().gdn_pages_workspace_size(ctypes.byref(b)))
+    b = _BOOK.pack(table.shape[0], table.shape[1], refs.numel(), 1, 0, 0, 0, 0, 0, 0)
+    return int(load_library().gdn_pages_workspace_size(b))
 
 
 def gdn_pages_extend(table, lens, refs, add, page_size, out=None, workspace=None):
     """Room for add[s] more tokens in each sequence: dict table, lens, refs, short.
 
     table int32 [S, blocks], lens and add int32 [S], refs int32 [pages] (holders of each page; 0:
-    free).  short[s] > 0: there was no room for the pages it needs, and sequence s is as it was.  ``out``: dict of
-    tensors to write; the inputs themselves update in place."""
-    b, got = _book(table, lens, refs, page_size, out, True)
-    short = _extra(got, "short", lens.shape, table.device)
-    ws = _work(b, workspace, table.device)
-    _check(load_library().gdn_pages_extend(
-        ctypes.byref(b), _ints("add", add, table.device, lens.shape), short, ws.data_ptr(),
-        ws.numel(), _stream(table.device)))
+    free).  short[s] > 0: there was no room for the pages it needs, and sequence s is as it was.
+    ``out``: dict of tensors to write; the inputs themselves update in place."""
+    lib = load_library()
+    b, got, short, dev = _book(table, lens, refs, page_size, out, True, "short", lens.shape)
+    device = table.device
+    ws, p, n = _work(lib, b, workspace, device)
+    _check(lib.gdn_pages_extend(b, _ints("add", add, dev, lens.shape), short, p, n,
+                                _stream(device)))
     return got
 
 
@@ -448,36 +471,34 @@ def gdn_pages_select(table, lens, refs, parents, page_size, pool=None, out=None,
     Frees, forks and reorders sequences in one call: full pages are shared, a partly filled last
     page is copied for every row but the lowest of its parent, in ``pool`` [parts, pages, ...].
     short[i] == 1: no page was left and row i is empty."""
-    b, got = _book(table, lens, refs, page_size, out, True)
-    short = _extra(got, "short", lens.shape, table.device)
-    p = _pool(pool, table.device)
-    ws = _work(b, workspace, table.device)
-    _check(load_library().gdn_pages_select(
-        ctypes.byref(b), _ints("parents", parents, table.device, lens.shape), _ref(p), short,
-        ws.data_ptr(), ws.numel(), _stream(table.device)))
+    lib = load_library()
+    b, got, short, dev = _book(table, lens, refs, page_size, out, True, "short", lens.shape)
+    device = table.device
+    ws, p, n = _work(lib, b, workspace, device)
+    _check(lib.gdn_pages_select(b, _ints("parents", parents, dev, lens.shape), _pool(pool, dev),
+                                short, p, n, _stream(device)))
     return got
 
 
 def gdn_pages_compact(table, lens, refs, page_size, pool=None, out=None, workspace=None):
     """Moves the pages in use into the lowest indexes: dict table, refs, map (new index of each
     page, -1 if it was free).  The data moves in ``pool`` [parts, pages, ...]."""
-    b, got = _book(table, lens, refs, page_size, out, False)
-    to = _extra(got, "map", refs.shape, table.device)
-    p = _pool(pool, table.device)
-    ws = _work(b, workspace, table.device)
-    _check(load_library().gdn_pages_compact(ctypes.byref(b), _ref(p), to, ws.data_ptr(),
-                                            ws.numel(), _stream(table.device)))
+    lib = load_library()
+    b, got, to, dev = _book(table, lens, refs, page_size, out, False, "map", refs.shape)
+    device = table.device
+    ws, p, n = _work(lib, b, workspace, device)
+    _check(lib.gdn_pages_compact(b, _pool(pool, dev), to, p, n, _stream(device)))
     return got
 
 
 def gdn_pages_copy(pool, src, dst):
     """Copies pages src[i] to dst[i] (int32) in every part of ``pool`` [parts, pages, ...], a cache
     or a pool of recurrent states; pairs out of range are skipped."""
-    if not isinstance(pool, torch.Tensor):
+    if not isinstance(pool, _Tensor):
         raise TypeError("pool must be a tensor")
-    p = _pool(pool, pool.device)
-    if not isinstance(src, torch.Tensor) or src.dim() != 1:
+    dev = pool.get_device()
+    p = _pool(pool, dev)
+    if not isinstance(src, _Tensor) or src.dim() != 1:
         raise ValueError("src must be int32 [pairs]")
-    _check(load_library().gdn_pages_copy(
-        ctypes.byref(p), _ints("src", src, pool.device), _ints("dst", dst, pool.device, src.shape),
-        src.numel(), _stream(pool.device)))
+    _check(load_library().gdn_pages_copy(p, _ints("src", src, dev), _ints("dst", dst, dev, src.shape),
+                                         src.numel(), _stream(pool.device)))
