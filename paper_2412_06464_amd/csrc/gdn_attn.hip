@@ -141,6 +141,9 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   using P = Piece<E>;
   constexpr int NK = C::NK, NT = NK / 16, RB = C::RB, NP = C::NP, KB = RB / 64, DT = D / 16;
   constexpr int GROUPS = KT / 16;
+  // Where two waves share a SIMD, the one in its products goes first: the other
+  // fills in with its softmax (a prompt of 8192 tokens at d = 128: 282 -> 266 us).
+  constexpr bool PRIO = KW == 1 && RB <= 512;
   constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;  // groups this wave copies
   const int lane = lane_id(), g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -270,6 +273,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int u = 0; u < QT; ++u) s[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (PRIO) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
@@ -279,6 +283,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
         for (int u = 0; u < QT; ++u) s[t][u] = P::mma(x, q[u][kb], s[t][u]);
       }
     }
+    if (PRIO) __builtin_amdgcn_s_setprio(0);
     if constexpr (EDGE) {  // what a row does not see
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -330,6 +335,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
         }
     }
     // O^T
+    if (PRIO) __builtin_amdgcn_s_setprio(1);
     if constexpr (sizeof(E) == 4) {
       if (!EDGE || !odd) {
 #pragma unroll
@@ -392,6 +398,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
         }
       }
     }
+    if (PRIO) __builtin_amdgcn_s_setprio(0);
     if constexpr (EDGE) {
       if (odd) {  // key by key, only the rows that see it
         const unsigned char* const vw = smem + buf + C::TILE + kw * NK * RB;
@@ -588,7 +595,7 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
 // the next one's.
 template <class E, int D, int KT>
-__global__ __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) void k_attn_tile(AttnArgs a,
+__global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile(AttnArgs a,
                                                                                 int slots) {
   using C = AttnCfg<E, D, 2, 4, 1, KT>;
   static_assert(C::ROWS == TILE_ROWS, "row block");
@@ -707,15 +714,18 @@ template <class E, int D> __global__ __launch_bounds__(256) void k_attn_join(Att
 
 namespace {
 
-// Tiles: as many keys as leave two buffers of k and v in LDS at the waves'
-// groups of 16.  {keys, waves} of the few-rows kernel, keys of the other.
+// Tiles.  The few-rows kernel: as many keys as fill a CU's LDS with two buffers
+// of k and v (most bytes in flight), four waves where that leaves each a group
+// of 16.  The other: as many as let two workgroups share a CU (64 KB of buffers),
+// so that one's products run beside the other's softmax: at d = 256 in bf16 32
+// keys, prompts in a 2K window 284 us, with 64 and one workgroup 317.
 template <class E, int D> struct Few {
   static constexpr int RB = D * (int)sizeof(E);
   static constexpr int KW = RB >= 1024 ? 2 : 4;
   static constexpr int KT = RB <= 256 ? 128 : RB == 512 ? 64 : 32;
 };
 template <class E, int D> struct Tile {
-  static constexpr int KT = D * (int)sizeof(E) >= 1024 ? 32 : 64;
+  static constexpr int KT = D * (int)sizeof(E) >= 512 ? 32 : 64;
 };
 
 template <class F> hipError_t by_dim(Dt dt, int d, F&& f) {
@@ -735,7 +745,7 @@ int attn_few_keys(Dt dt, int d) {
   const int rb = d * (dt == Dt::F32 ? 4 : 2);
   return rb <= 256 ? 128 : rb == 512 ? 64 : 32;
 }
-int attn_tile_keys(Dt dt, int d) { return d * (dt == Dt::F32 ? 4 : 2) >= 1024 ? 32 : 64; }
+int attn_tile_keys(Dt dt, int d) { return d * (dt == Dt::F32 ? 4 : 2) >= 512 ? 32 : 64; }
 
 hipError_t launch_attn_few(Dt dt, int d, bool rows16, const AttnArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)a.tok.N * a.splits * a.Hk);

@@ -45,7 +45,7 @@ constexpr int ROT_TABLE = 1024;  // angles it holds
 
 // A workgroup takes a.per tokens: first the cos and sin of their angles into
 // LDS, once for all heads, with each token's place; then the rows of q, k (and
-// v) go through it in units of 16 bytes a lane.
+// v) go through it.
 //   WIDE: a unit is one 16-byte piece (interleaved pairs lie inside one) or, in
 //   the layout of halves, the two pieces that hold the two sides of its pairs,
 //   where those start at multiples of 16 bytes; else a unit is one pair.
@@ -88,86 +88,141 @@ template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(Ro
   __syncthreads();
 
   const bool halves = a.layout == 0;
-  // units of a row that is turned, and of one that is copied (v)
+  // units of a row that is turned, and those of it that pass unchanged
   const int turn = WIDE && halves ? half / N : (WIDE ? a.d / N : half);
   const int rest = WIDE ? (halves ? (a.d - a.rot) / N : 0) : a.d - a.rot;
-  const int per_row = turn + rest, per_v = a.d / N;
-  const int nq = (a.q.data ? a.Hq : 0) * per_row, nk = (a.k.data ? a.Hk : 0) * per_row;
-  const int nv = (a.v.data ? a.Hk : 0) * per_v, per_token = nq + nk + nv;
+  const int units = turn + rest;
 
-#pragma unroll 2
-  for (int i = threadIdx.x; i < nt * per_token; i += 256) {
-    const int tt = i / per_token, u = i - tt * per_token;
-    const int64_t t = t0 + tt;
-    if (u >= nq + nk) {
-      const int h = (u - nq - nk) / per_v, p = (u - nq - nk) - h * per_v;
-      const int64_t at = kat[tt];
-      if (at >= 0)
-        store_piece(a.cache.v + at + h * a.cache.head + p * 16,
-                    load_piece<E>(a.v.data + t * a.v.ts + h * a.v.hs + p * 16));
-      continue;
-    }
-    const bool is_q = u < nq;
-    const int h = (is_q ? u : u - nq) / per_row, p = (is_q ? u : u - nq) - h * per_row;
-    const unsigned char* x = is_q ? a.q.data + t * a.q.ts + h * a.q.hs
-                                  : a.k.data + t * a.k.ts + h * a.k.hs;
-    unsigned char* y;
-    if (is_q) {
-      y = a.q_out.data + t * a.q_out.ts + h * a.q_out.hs;
-    } else if (a.append) {
-      const int64_t at = kat[tt];
-      if (at < 0) continue;
-      y = a.cache.k + at + h * a.cache.head;
-    } else {
-      y = a.k_out.data + t * a.k_out.ts + h * a.k_out.hs;
-    }
-    const float2* w = cs + tt * half;
-    if constexpr (WIDE) {
-      if (halves) {
-        if (p >= turn) {
-          const int at = (a.rot / N + p - turn) * 16;
-          store_piece(y + at, load_piece<E>(x + at));
-          continue;
-        }
-        const int at1 = p * 16, at2 = (p + turn) * 16;
-        Pc<E> x1 = load_piece<E>(x + at1), x2 = load_piece<E>(x + at2), y1, y2;
+  // A thread keeps its unit p and steps through the rows (of q and k, or of v) of
+  // the workgroup's tokens, four at a time, loaded ahead of their stores (f gets
+  // the token and row of each; a token nt or past it: none).
+  constexpr int BATCH = 4;
+  auto stream = [&](int tid, int H, int per_row, auto&& f) {
+    const int step = max(1, 256 / per_row);  // rows a pass; the threads left over idle
+    const int dt = step / H, dh = step - dt * H;
+    // (a row of more units than threads: units p, p + 256, ...)
+    for (int p = per_row > 256 ? tid : tid % per_row; p < per_row; p += 256) {
+      const int row = per_row > 256 ? 0 : tid / per_row;
+      if (row >= step) return;
+      int tt = row / H, h = row - tt * H;
+      while (tt < nt) {
+        int ts[BATCH], hs[BATCH];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float2 c = w[p * N + j];
-          const float u1 = to_f(x1.e[j]), u2 = to_f(x2.e[j]);
-          y1.e[j] = to_e<E>(u1 * c.x - u2 * c.y);
-          y2.e[j] = to_e<E>(u2 * c.x + u1 * c.y);
-        }
-        store_piece(y + at1, y1);
-        store_piece(y + at2, y2);
-      } else {
-        Pc<E> z = load_piece<E>(x + p * 16);
-#pragma unroll
-        for (int j = 0; j < N / 2; ++j) {
-          const int pair = p * (N / 2) + j;
-          if (pair < half) {
-            const float2 c = w[pair];
-            const float u1 = to_f(z.e[2 * j]), u2 = to_f(z.e[2 * j + 1]);
-            z.e[2 * j] = to_e<E>(u1 * c.x - u2 * c.y);
-            z.e[2 * j + 1] = to_e<E>(u2 * c.x + u1 * c.y);
+        for (int j = 0; j < BATCH; ++j) {
+          ts[j] = tt;
+          hs[j] = h;
+          tt += dt;
+          h += dh;
+          if (h >= H) {
+            h -= H;
+            ++tt;
           }
         }
-        store_piece(y + p * 16, z);
-      }
-    } else {  // halves that do not start at multiples of 16 bytes
-      const E* xe = reinterpret_cast<const E*>(x);
-      E* ye = reinterpret_cast<E*>(y);
-      if (p >= turn) {
-        const int ch = a.rot + p - turn;
-        ye[ch] = xe[ch];
-      } else {
-        const float2 c = w[p];
-        const float u1 = to_f(xe[p]), u2 = to_f(xe[p + half]);
-        ye[p] = to_e<E>(u1 * c.x - u2 * c.y);
-        ye[p + half] = to_e<E>(u2 * c.x + u1 * c.y);
+        f(ts, hs, p);
       }
     }
-  }
+  };
+  const int nq = a.q.data ? a.Hq : 0, nk = a.k.data ? a.Hk : 0;
+  // (plain values: a choice between two structures would put them in memory)
+  unsigned char *const qd = a.q.data, *const kd = a.k.data - nq * a.k.hs;
+  const int64_t qts = a.q.ts, qhs = a.q.hs, kts = a.k.ts, khs = a.k.hs;
+  auto from = [&](int tt, int h) {
+    const bool is_q = h < nq;
+    return (is_q ? qd : kd) + (int64_t)(t0 + tt) * (is_q ? qts : kts) + h * (is_q ? qhs : khs);
+  };
+  unsigned char* const qod = a.q_out.data;
+  const int64_t qots = a.q_out.ts, qohs = a.q_out.hs;
+  const int64_t kots = a.append ? 0 : a.k_out.ts, kohs = a.append ? a.cache.head : a.k_out.hs;
+  unsigned char* const kod = (a.append ? a.cache.k : a.k_out.data) - nq * kohs;
+  auto to = [&](int tt, int h) {
+    const bool is_q = h < nq;
+    unsigned char* r =
+        (is_q ? qod : kod) + (int64_t)(t0 + tt) * (is_q ? qots : kots) + h * (is_q ? qohs : kohs);
+    return a.append && !is_q ? r + kat[tt] : r;
+  };
+  auto there = [&](int tt, int h) { return tt < nt && (h < nq || !a.append || kat[tt] >= 0); };
+  stream(threadIdx.x, nq + nk, units, [&](const int (&ts)[BATCH], const int (&hs)[BATCH], int p) {
+      if constexpr (WIDE) {
+        // the unit's pieces: its own, or those of both sides of its pairs
+        const bool both = halves && p < turn;
+        const int at1 = (halves && p >= turn ? turn + p : p) * 16, at2 = (p + turn) * 16;
+        uint4 x1[BATCH], x2[BATCH];
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j)
+          if (there(ts[j], hs[j])) {
+            const unsigned char* r = from(ts[j], hs[j]);
+            x1[j] = *reinterpret_cast<const uint4*>(r + at1);
+            if (both) x2[j] = *reinterpret_cast<const uint4*>(r + at2);
+          }
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j)
+          if (there(ts[j], hs[j])) {
+            unsigned char* r = to(ts[j], hs[j]);
+            const float2* w = cs + ts[j] * half;
+            if (both) {
+              Pc<E> u = *reinterpret_cast<const Pc<E>*>(&x1[j]);
+              Pc<E> v = *reinterpret_cast<const Pc<E>*>(&x2[j]);
+#pragma unroll
+              for (int e = 0; e < N; ++e) {
+                const float2 c = w[p * N + e];
+                const float u1 = to_f(u.e[e]), u2 = to_f(v.e[e]);
+                u.e[e] = to_e<E>(u1 * c.x - u2 * c.y);
+                v.e[e] = to_e<E>(u2 * c.x + u1 * c.y);
+              }
+              store_piece(r + at1, u);
+              store_piece(r + at2, v);
+            } else if (halves) {
+              *reinterpret_cast<uint4*>(r + at1) = x1[j];
+            } else {
+              Pc<E> u = *reinterpret_cast<const Pc<E>*>(&x1[j]);
+#pragma unroll
+              for (int e = 0; e < N / 2; ++e) {
+                const int pair = p * (N / 2) + e;
+                if (pair < half) {
+                  const float2 c = w[pair];
+                  const float u1 = to_f(u.e[2 * e]), u2 = to_f(u.e[2 * e + 1]);
+                  u.e[2 * e] = to_e<E>(u1 * c.x - u2 * c.y);
+                  u.e[2 * e + 1] = to_e<E>(u2 * c.x + u1 * c.y);
+                }
+              }
+              store_piece(r + at1, u);
+            }
+          }
+      } else {  // halves that do not start at multiples of 16 bytes
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j)
+          if (there(ts[j], hs[j])) {
+            const E* x = reinterpret_cast<const E*>(from(ts[j], hs[j]));
+            E* y = reinterpret_cast<E*>(to(ts[j], hs[j]));
+            if (p < turn) {
+              const float2 c = cs[ts[j] * half + p];
+              const float u1 = to_f(x[p]), u2 = to_f(x[p + half]);
+              y[p] = to_e<E>(u1 * c.x - u2 * c.y);
+              y[p + half] = to_e<E>(u2 * c.x + u1 * c.y);
+            } else {
+              y[half + p] = x[half + p];
+            }
+          }
+      }
+    });
+  // v from the other end: where there are few tokens, by the waves that have no q
+  if (a.v.data)
+    stream(255 - threadIdx.x, a.Hk, a.d / N,
+           [&](const int (&ts)[BATCH], const int (&hs)[BATCH], int p) {
+             uint4 x[BATCH];
+#pragma unroll
+             for (int j = 0; j < BATCH; ++j) {
+               x[j] = make_uint4(0, 0, 0, 0);
+               if (ts[j] < nt)
+                 x[j] = *reinterpret_cast<const uint4*>(a.v.data + (int64_t)(t0 + ts[j]) * a.v.ts +
+                                                        hs[j] * a.v.hs + p * 16);
+             }
+#pragma unroll
+             for (int j = 0; j < BATCH; ++j)
+               if (ts[j] < nt && kat[ts[j]] >= 0)
+                 *reinterpret_cast<uint4*>(a.cache.v + kat[ts[j]] +
+                                           hs[j] * a.cache.head + p * 16) = x[j];
+           });
 }
 
 hipError_t launch_rotate(Dt dt, RotateArgs a, hipStream_t s) {

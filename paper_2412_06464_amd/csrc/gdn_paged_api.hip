@@ -185,8 +185,13 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
   // A block of m tokens sees at most window + m - 1 keys, and its range begins
   // at a multiple of 16.
   auto keys = [&](int64_t m) { return a->window > 0 ? std::min(kv, a->window + m + 14) : kv; };
+  // A workgroup of the few-rows kernel has a CU to itself (128 KB of LDS at most
+  // head dims): 256 of them are wanted; more cost more partial sums than they
+  // balance (two sequences of 131072 keys, 4 cache heads: 97 us, with 512 100,
+  // with 2048 113; 12 of up to 3000 keys in fp32, 8 heads: 22.4 and 26.4).  Two
+  // of the other kernel share a CU: 512, in ranges of 256 keys or more.
   if (p.few)
-    split(n_few * t->Hk, keys(most_few), gdn::attn_few_keys(dt, t->d), 512,
+    split(n_few * t->Hk, keys(most_few), gdn::attn_few_keys(dt, t->d), 256,
           gdn::attn_few_keys(dt, t->d), &p.few_splits, &p.few_len);
   if (p.tile)
     split((int64_t)p.slots * t->Hk, keys(std::min<int64_t>(most, R / G + 2)),
