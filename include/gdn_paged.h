@@ -167,7 +167,7 @@ gdn_status gdn_cache_attn(const gdn_tokens *t, const gdn_attn *a, const gdn_rows
  * data + i * part_stride + p * page_stride (bytes, multiples of 16).  A pool
  * of recurrent states is one too (a page: a sequence's state). */
 typedef struct {
-  int32_t S, max_blocks, num_pages, page_size; /* num_pages <= 2^20 */
+  int32_t S, max_blocks, num_pages, page_size; /* S, num_pages <= 2^20 */
   const int32_t *table, *lens, *refs;
   int32_t *table_out, *lens_out, *refs_out;
 } gdn_book;

@@ -1,4 +1,5 @@
-"""Build libgdn.so (HIP, gfx950) in-tree with hipcc.
+"""Build libgdn.so (HIP, gfx950) in-tree with hipcc, and the attention layer's
+binding helper _paged_binding.so (host code) with the C++ compiler.
 
     python -m paper_2412_06464_amd.build
 """
@@ -12,6 +13,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgdn.so")
+BINDING = os.path.join(HERE, "_paged_binding.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 SOURCES = ["gdn_prep.hip", "gdn_seq.hip", "gdn_grad.hip", "gdn_recurrent.hip", "gdn_block.hip",
@@ -36,6 +38,26 @@ def _compile(src: str, obj: str, extra=()) -> None:
         raise RuntimeError("hipcc failed for %s:\n%s%s" % (src, r.stdout, r.stderr))
 
 
+def build_binding(out: str = BINDING) -> str:
+    """Compile the tensor checks of the attention layer's binding (host code, torch's headers)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = out + ".tmp%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+           *["-I" + d for d in cpp_extension.include_paths()],
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "paged_binding.cpp"),
+           "-o", tmp, *["-L" + d for d in cpp_extension.library_paths()],
+           "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("%s failed for paged_binding.cpp:\n%s%s" % (cmd[0], r.stdout, r.stderr))
+    os.replace(tmp, out)
+    return out
+
+
 def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     """Compile every source for gfx950 and link ``out``.  ``defines`` are
     extra -D flags (tuning experiments; the defaults are the product)."""
@@ -44,8 +66,11 @@ def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     bdir = os.path.join(HERE, "_build" + ("_" + tag if tag else ""))
     os.makedirs(bdir, exist_ok=True)
     objs = [os.path.join(bdir, os.path.splitext(s)[0] + ".o") for s in SOURCES]
-    with cf.ThreadPoolExecutor(len(SOURCES)) as ex:
+    with cf.ThreadPoolExecutor(len(SOURCES) + 1) as ex:
+        binding = ex.submit(build_binding) if out == LIB else None
         list(ex.map(lambda a: _compile(*a, extra), zip(SOURCES, objs)))
+        if binding:
+            binding.result()
     LIBOUT = out
     tmp = LIBOUT + ".tmp%d" % os.getpid()
     cmd = [HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC", *objs, "-o", tmp]

@@ -310,6 +310,43 @@ template <class Pick, class F> __device__ inline int ranked(int num, Pick&& pick
 
 }  // namespace
 
+// Page copies in units of 16 KiB: (pair, part, unit), strided over `groups`
+// workgroups of which this is number `me`.
+constexpr int MOVE_UNIT = 16384;
+constexpr int MOVE_GROUPS = 4096;
+__device__ inline void move_pages(const Pool& p, const int32_t* src, const int32_t* dst, int n,
+                                  int64_t me, int64_t groups) {
+  const int64_t per = (p.bytes + MOVE_UNIT - 1) / MOVE_UNIT;
+  const int64_t units = (int64_t)n * p.parts * per;
+  for (int64_t u = me; u < units; u += groups) {
+    const int64_t i = u / (p.parts * per), r = u - i * (p.parts * per);
+    const int part = (int)(r / per);
+    const int64_t at = (r - part * per) * MOVE_UNIT;
+    const int from = src[i], to = dst[i];
+    if ((unsigned)from >= (unsigned)p.num_pages || (unsigned)to >= (unsigned)p.num_pages) continue;
+    const unsigned char* x = p.data + part * p.part + from * p.page + at;
+    unsigned char* y = p.data + part * p.part + to * p.page + at;
+    const int64_t left = p.bytes - at;
+    if (left >= MOVE_UNIT) {
+      uint4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v[j] = *reinterpret_cast<const uint4*>(x + j * 4096 + threadIdx.x * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) store_stream(y + j * 4096 + threadIdx.x * 16, v[j]);
+    } else {
+      for (int64_t o = threadIdx.x * 16; o < left; o += 4096)
+        store_stream(y + o, *reinterpret_cast<const uint4*>(x + o));
+    }
+  }
+}
+// Workgroups that move the pages of at most n pairs.
+inline unsigned move_groups(const Pool* p, int64_t n) {
+  if (!p) return 0;
+  const int64_t per = (p->bytes + MOVE_UNIT - 1) / MOVE_UNIT;
+  return (unsigned)std::min<int64_t>(n * p->parts * per, MOVE_GROUPS);
+}
+
 // rank[s] = the place, among the pages given out, of sequence s's first (-1:
 // it gets none); dst[i] = the i-th free page; refs_out: with those given out.
 __global__ __launch_bounds__(PLAN) void k_extend_plan(Book b, const int32_t* add,
@@ -431,9 +468,14 @@ __global__ __launch_bounds__(256) void k_copy_ints(const int32_t* x, int32_t* y,
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) y[i] = x[i];
 }
 
-// New rows, one workgroup each, and the references of old and new ones.
+// New rows, one workgroup each, and the references of old and new ones; the
+// workgroups past the rows copy the pages.
 __global__ __launch_bounds__(256) void k_select_rows(Book b, const int32_t* parents, PageWork w,
-                                                     const int32_t* table) {
+                                                     const int32_t* table, Pool pool) {
+  if ((int)blockIdx.x >= b.S) {
+    move_pages(pool, w.src, w.dst, w.count[0], blockIdx.x - b.S, gridDim.x - b.S);
+    return;
+  }
   const int i = blockIdx.x, p = parents[i], rank = w.rank[i];
   const bool real = (unsigned)p < (unsigned)b.S && rank != -2;
   const int len = real ? max(w.lens[p], 0) : 0, now = blocks_of(len, b);
@@ -453,8 +495,8 @@ __global__ __launch_bounds__(256) void k_select_rows(Book b, const int32_t* pare
   }
 }
 
-hipError_t launch_select(const Book& b, const int32_t* parents, int32_t* short_of,
-                         const PageWork& w, hipStream_t s) {
+hipError_t launch_select(const Book& b, const int32_t* parents, const Pool* pool,
+                         int32_t* short_of, const PageWork& w, hipStream_t s) {
   const int32_t* table = b.table;
   if (b.table_out == b.table) {
     const int64_t n = (int64_t)b.S * b.max_blocks;
@@ -465,7 +507,8 @@ hipError_t launch_select(const Book& b, const int32_t* parents, int32_t* short_o
   }
   hipLaunchKernelGGL(k_select_plan, dim3(1), dim3(PLAN), 0, s, b, parents, short_of, w);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_select_rows, dim3(b.S), dim3(256), 0, s, b, parents, w, table);
+  hipLaunchKernelGGL(k_select_rows, dim3(b.S + move_groups(pool, b.S)), dim3(256), 0, s, b, parents,
+                     w, table, pool ? *pool : Pool{});
   return hipGetLastError();
 }
 
@@ -490,82 +533,58 @@ __global__ __launch_bounds__(PLAN) void k_compact_plan(Book b, int32_t* map, Pag
   }
 }
 
-// Rows of the table, renumbered; what a sequence does not hold becomes -1.
-__global__ __launch_bounds__(256) void k_compact_rows(Book b, const int32_t* map) {
-  const int64_t n = (int64_t)b.S * b.max_blocks;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-    const int s = (int)(i / b.max_blocks), j = (int)(i - (int64_t)s * b.max_blocks);
-    int x = -1;
-    if (j < blocks_of(b.lens[s], b)) {
-      x = b.table[i];
-      x = held(b, x) ? map[x] : -1;
+// Rows of the table, renumbered (what a sequence does not hold becomes -1) by the
+// first `rows` workgroups, refs by the next `refs`, the data by the others.
+// refs: the moves take theirs along; a page that is moved from lies at n or past
+// it, one that is moved to below, so no thread reads what another writes.
+__global__ __launch_bounds__(256) void k_compact_rest(Book b, const int32_t* map, PageWork w,
+                                                      Pool pool, int rows, int refs) {
+  const int me = blockIdx.x;
+  if (me < rows) {
+    const int64_t n = (int64_t)b.S * b.max_blocks;
+    for (int64_t i = me * 256ll + threadIdx.x; i < n; i += rows * 256ll) {
+      const int s = (int)(i / b.max_blocks), j = (int)(i - (int64_t)s * b.max_blocks);
+      int x = -1;
+      if (j < blocks_of(b.lens[s], b)) {
+        x = b.table[i];
+        x = held(b, x) ? map[x] : -1;
+      }
+      b.table_out[i] = x;
     }
-    b.table_out[i] = x;
-  }
-}
-// refs: the moves take theirs along (a page that is moved from lies at n or
-// past it, one that is moved to below: no thread reads what another writes).
-__global__ __launch_bounds__(256) void k_compact_refs(Book b, const int32_t* map, PageWork w) {
-  const int n = w.count[1];
-  for (int p = blockIdx.x * 256 + threadIdx.x; p < b.num_pages; p += gridDim.x * 256) {
-    if (p < n) {
-      if (map[p] >= 0 && b.refs_out != b.refs) b.refs_out[p] = b.refs[p];
-    } else if (map[p] >= 0) {
-      b.refs_out[map[p]] = b.refs[p];
-      b.refs_out[p] = 0;
-    } else {
-      b.refs_out[p] = 0;
+  } else if (me < rows + refs) {
+    const int n = w.count[1];
+    for (int p = (me - rows) * 256 + threadIdx.x; p < b.num_pages; p += refs * 256) {
+      if (p < n) {
+        if (map[p] >= 0 && b.refs_out != b.refs) b.refs_out[p] = b.refs[p];
+      } else {
+        if (map[p] >= 0) b.refs_out[map[p]] = b.refs[p];
+        b.refs_out[p] = 0;
+      }
     }
+  } else {
+    move_pages(pool, w.src, w.dst, w.count[0], me - rows - refs, gridDim.x - rows - refs);
   }
 }
 
-hipError_t launch_compact(const Book& b, int32_t* map, const PageWork& w, hipStream_t s) {
+hipError_t launch_compact(const Book& b, const Pool* pool, int32_t* map, const PageWork& w,
+                          hipStream_t s) {
   hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(PLAN), 0, s, b, map, w);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const int64_t n = (int64_t)b.S * b.max_blocks;
-  hipLaunchKernelGGL(k_compact_rows, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 2048)),
-                     dim3(256), 0, s, b, map);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_compact_refs, dim3((unsigned)std::min(b.num_pages / 256 + 1, 1024)),
-                     dim3(256), 0, s, b, map, w);
+  const int rows = (int)std::min<int64_t>((n + 255) / 256, 2048);
+  const int refs = std::min((b.num_pages + 255) / 256, 1024);
+  hipLaunchKernelGGL(k_compact_rest, dim3(rows + refs + move_groups(pool, b.num_pages)), dim3(256),
+                     0, s, b, map, w, pool ? *pool : Pool{}, rows, refs);
   return hipGetLastError();
 }
 
-// Page copies in units of 16 KiB: (pair, part, unit), strided over the grid.
-constexpr int MOVE_UNIT = 16384;
-__global__ __launch_bounds__(256) void k_move(Pool p, const int32_t* src, const int32_t* dst,
-                                              const int32_t* count, int n) {
-  const int64_t per = (p.bytes + MOVE_UNIT - 1) / MOVE_UNIT;
-  const int64_t units = (int64_t)(count ? *count : n) * p.parts * per;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int64_t i = u / (p.parts * per), r = u - i * (p.parts * per);
-    const int part = (int)(r / per);
-    const int64_t at = (r - part * per) * MOVE_UNIT;
-    const int from = src[i], to = dst[i];
-    if ((unsigned)from >= (unsigned)p.num_pages || (unsigned)to >= (unsigned)p.num_pages) continue;
-    const unsigned char* x = p.data + part * p.part + from * p.page + at;
-    unsigned char* y = p.data + part * p.part + to * p.page + at;
-    const int64_t left = p.bytes - at;
-    if (left >= MOVE_UNIT) {
-      uint4 v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        v[j] = *reinterpret_cast<const uint4*>(x + j * 4096 + threadIdx.x * 16);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) store_stream(y + j * 4096 + threadIdx.x * 16, v[j]);
-    } else {
-      for (int64_t o = threadIdx.x * 16; o < left; o += 4096)
-        store_stream(y + o, *reinterpret_cast<const uint4*>(x + o));
-    }
-  }
+__global__ __launch_bounds__(256) void k_move(Pool p, const int32_t* src, const int32_t* dst, int n) {
+  move_pages(p, src, dst, n, blockIdx.x, gridDim.x);
 }
 
-hipError_t launch_move(const Pool& p, const int32_t* src, const int32_t* dst,
-                       const int32_t* count, int n, hipStream_t s) {
-  const int64_t per = (p.bytes + MOVE_UNIT - 1) / MOVE_UNIT;
-  const int64_t units = (int64_t)n * p.parts * per;
-  hipLaunchKernelGGL(k_move, dim3((unsigned)std::min<int64_t>(units, 4096)), dim3(256), 0, s, p,
-                     src, dst, count, n);
+hipError_t launch_move(const Pool& p, const int32_t* src, const int32_t* dst, int n,
+                       hipStream_t s) {
+  hipLaunchKernelGGL(k_move, dim3(move_groups(&p, n)), dim3(256), 0, s, p, src, dst, n);
   return hipGetLastError();
 }
 

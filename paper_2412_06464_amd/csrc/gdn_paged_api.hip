@@ -212,7 +212,7 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
 gdn_status check_book(const gdn_book* b, bool lens_out, gdn::Book* out) {
   if (!b) return GDN_ERR_NULL;
   if (b->S < 1 || b->max_blocks < 1 || b->num_pages < 1 || b->page_size < 1 ||
-      b->num_pages > MAX_PAGES || (int64_t)b->max_blocks * b->page_size >= (int64_t)1 << 31)
+      b->num_pages > MAX_PAGES || b->S > MAX_PAGES || (int64_t)b->max_blocks * b->page_size >= (int64_t)1 << 31)
     return GDN_ERR_SHAPE;
   if (!b->table || !b->lens || !b->refs || !b->table_out || !b->refs_out ||
       (lens_out && !b->lens_out))
@@ -403,7 +403,9 @@ gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_row
 }
 
 size_t gdn_pages_workspace_size(const gdn_book* b) {
-  if (!b || b->S < 1 || b->max_blocks < 1 || b->num_pages < 1 || b->num_pages > MAX_PAGES) return 0;
+  if (!b || b->S < 1 || b->max_blocks < 1 || b->num_pages < 1 ||
+      b->num_pages > MAX_PAGES || b->S > MAX_PAGES)
+    return 0;
   return carve_pages(b->S, b->max_blocks, b->num_pages, nullptr, nullptr);
 }
 
@@ -428,10 +430,8 @@ gdn_status gdn_pages_select(const gdn_book* b, const int32_t* parents, const gdn
   if (st != GDN_OK) return st;
   if (!parents || !short_of) return GDN_ERR_NULL;
   if (!aligned(parents, 4) || !aligned(short_of, 4)) return GDN_ERR_ALIGN;
-  hipStream_t s = (hipStream_t)stream;
-  hipError_t e = gdn::launch_select(book, parents, short_of, w, s);
-  if (e == hipSuccess && pool) e = gdn::launch_move(pl, w.src, w.dst, w.count, b->S, s);
-  return done(e);
+  return done(gdn::launch_select(book, parents, pool ? &pl : nullptr, short_of, w,
+                                 (hipStream_t)stream));
 }
 
 gdn_status gdn_pages_compact(const gdn_book* b, const gdn_pool* pool, int32_t* map,
@@ -443,10 +443,7 @@ gdn_status gdn_pages_compact(const gdn_book* b, const gdn_pool* pool, int32_t* m
   if (st != GDN_OK) return st;
   if (!map) return GDN_ERR_NULL;
   if (!aligned(map, 4)) return GDN_ERR_ALIGN;
-  hipStream_t s = (hipStream_t)stream;
-  hipError_t e = gdn::launch_compact(book, map, w, s);
-  if (e == hipSuccess && pool) e = gdn::launch_move(pl, w.src, w.dst, w.count, b->num_pages, s);
-  return done(e);
+  return done(gdn::launch_compact(book, pool ? &pl : nullptr, map, w, (hipStream_t)stream));
 }
 
 gdn_status gdn_pages_copy(const gdn_pool* pool, const int32_t* src, const int32_t* dst, int32_t n,
@@ -459,7 +456,7 @@ gdn_status gdn_pages_copy(const gdn_pool* pool, const int32_t* src, const int32_
   if (n == 0) return GDN_OK;
   if (!src || !dst) return GDN_ERR_NULL;
   if (!aligned(src, 4) || !aligned(dst, 4)) return GDN_ERR_ALIGN;
-  return done(gdn::launch_move(pl, src, dst, nullptr, n, (hipStream_t)stream));
+  return done(gdn::launch_move(pl, src, dst, n, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -90,12 +90,14 @@ struct PageWork {
 };
 hipError_t launch_extend(const Book& b, const int32_t* add, int32_t* short_of, const PageWork& w,
                          hipStream_t s);
-hipError_t launch_select(const Book& b, const int32_t* parents, int32_t* short_of,
-                         const PageWork& w, hipStream_t s);
-hipError_t launch_compact(const Book& b, int32_t* map, const PageWork& w, hipStream_t s);
-// Copies page src[i] to dst[i] for i < *count (device) or n (count == nullptr).
-hipError_t launch_move(const Pool& p, const int32_t* src, const int32_t* dst,
-                       const int32_t* count, int n, hipStream_t s);
+// (pool: nullptr where no data moves)
+hipError_t launch_select(const Book& b, const int32_t* parents, const Pool* pool,
+                         int32_t* short_of, const PageWork& w, hipStream_t s);
+hipError_t launch_compact(const Book& b, const Pool* pool, int32_t* map, const PageWork& w,
+                          hipStream_t s);
+// Copies page src[i] to dst[i], i < n (n >= 1).
+hipError_t launch_move(const Pool& p, const int32_t* src, const int32_t* dst, int n,
+                       hipStream_t s);
 
 // ---- device helpers
 

@@ -16,12 +16,14 @@ the ``pool`` of the page calls after ``flatten(0, 1)``.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
+import os
 import struct
 from typing import NamedTuple
 
 import torch
 
-from .gdn import GDN_BF16, GDN_F32, _check, _cu_pair, _ptr, _stream, load_library as _load
+from .gdn import _check, _cu_pair, _ptr, _stream, load_library as _load
 
 EXPORTS = ("gdn_rotary_turns", "gdn_rotary_fwd", "gdn_rotary_bwd", "gdn_cache_append",
            "gdn_cache_attn", "gdn_cache_attn_workspace_size", "gdn_pages_workspace_size",
@@ -112,116 +114,52 @@ def load_library():
     return _lib
 
 
-# A call of a few microseconds on the GPU must not spend longer here.  The
-# structures are packed as bytes, in the layout of the ctypes classes above
-# (0.2 us each instead of 0.5 to 1), and what every call checks of a tensor is
-# read once (host time of a call: storing a token for each of 256 sequences
-# 19.4 -> 10.0 us, attention of one token for each of 4 15.1 -> 10.3 us).
-_ROWS = struct.Struct("@Pqq")
-_TOKENS = struct.Struct("@iiiiiiPPi0P")
-_CACHE = struct.Struct("@PPqqqiiiPP")
-_ROTARY = struct.Struct("@iifP")
+# A call of a few microseconds on the GPU must not spend longer here: the
+# tensors are checked and the structures of the C ABI filled in by a native
+# helper (csrc/paged_binding.cpp); structures go in as their bytes.  Host time
+# of a call, with all of it in Python and so: storing a token for each of 256
+# sequences 19.4 and 6.9 us, attention of one token for each of 4 15.1 and 8.7.
 _ATTN = struct.Struct("@fiii")
 _BOOK = struct.Struct("@iiiiPPPPPP")
-_POOL = struct.Struct("@Piiqqq")
-_DTYPES = {torch.float32: GDN_F32, torch.bfloat16: GDN_BF16}
 _Tensor = torch.Tensor
-_I32 = torch.int32
 
 
-class _Like(NamedTuple):
-    """What the tensors of a call share, read off its first."""
-    name: str
-    B: int
-    T: int
-    d: int
-    dtype: torch.dtype
-    dev: int
+def _native():
+    """The native helper; raises if it is not built."""
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_paged_binding.so")
+    if not os.path.exists(path):
+        raise RuntimeError("_paged_binding.so is not built (%s); run "
+                           "`python -m paper_2412_06464_amd.build`" % path)
+    spec = importlib.util.spec_from_file_location("_paged_binding", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    return mod
 
 
-def _first(name, x):
-    """(_Like, heads) of a call's first [B, T, heads, d] tensor."""
-    if not isinstance(x, _Tensor):
-        raise TypeError("%s must be a tensor" % name)
-    if x.dim() != 4:
-        raise ValueError("%s must be [B, T, heads, d]" % name)
-    B, T, H, d = x.shape
-    dev = x.get_device()
-    if x.dtype not in _DTYPES:
-        raise TypeError("%s must be float32 or bfloat16" % name)
-    if dev < 0:
-        raise ValueError("%s must be on the GPU" % name)
-    return _Like(name, B, T, d, x.dtype, dev), H
+class _Helper:
+    """The helper's functions, loaded at their first use."""
+
+    def __getattr__(self, name):
+        mod = _native()
+        for f in ("first", "rows", "like", "fresh", "ints", "tokens", "cache", "rotary",
+                  "pool"):
+            setattr(self, f, getattr(mod, f))
+        return getattr(self, name)
 
 
-def _rows(name, x, like, heads=None):
-    """gdn_rows of a [B, T, heads, d] tensor alike to the call's first."""
-    if not isinstance(x, _Tensor):
-        raise TypeError("%s must be a tensor" % name)
-    if x.dim() != 4:
-        raise ValueError("%s must be [B, T, heads, d]" % name)
-    B, T, H, d = x.shape
-    sb, st, sh, sd = x.stride()
-    if x.dtype is not like.dtype or x.get_device() != like.dev:
-        raise ValueError("%s must have %s's dtype and device" % (name, like.name))
-    if B != like.B or T != like.T or d != like.d:
-        raise ValueError("%s must have %s's B, T and d" % (name, like.name))
-    if heads is not None and H != heads:
-        raise ValueError("%s must have %d heads" % (name, heads))
-    if sd != 1 and d != 1:
-        raise ValueError("%s must be contiguous in its last dim" % name)
-    if B > 1 and sb != T * st:
-        if T != 1:
-            raise ValueError("%s: the rows of B must follow each other (stride %d, not T tokens of "
-                             "%d)" % (name, sb, st))
-        st = sb  # a token a row: the rows' own stride
-    return _ROWS.pack(x.data_ptr(), st, sh)
+_n = _Helper()
 
 
-def _ints(name, x, dev, shape=None):
-    """Pointer of a contiguous int32 tensor on device ``dev``."""
-    if not isinstance(x, _Tensor):
-        raise TypeError("%s must be a tensor" % name)
-    if x.dtype is not _I32 or x.get_device() != dev or not x.is_contiguous():
-        raise ValueError("%s must be contiguous int32 on the call's device" % name)
-    if shape is not None and x.shape != shape:
-        raise ValueError("%s must be %s" % (name, list(shape)))
-    return x.data_ptr()
-
-
-def _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, device, keep):
-    """gdn_tokens, and the number of sequences."""
-    if cu_seqlens is None:
-        if cu_seqlens_host is not None:
-            raise ValueError("cu_seqlens_host without cu_seqlens")
-        return _TOKENS.pack(like.B, like.T, Hq, Hk, like.d, 0, 0, 0, _DTYPES[like.dtype]), like.B
-    dev, host = _cu_pair(cu_seqlens, cu_seqlens_host, device, keep)
-    keep.append(dev)
-    n = host.numel() - 1
-    return _TOKENS.pack(like.B, like.T, Hq, Hk, like.d, n, dev.data_ptr(), host.data_ptr(),
-                        _DTYPES[like.dtype]), n
-
-
-def _cache(like, k_pages, v_pages, table, kv_lens, num_seqs):
-    """gdn_cache, and the cache's heads."""
-    if not (isinstance(k_pages, _Tensor) and isinstance(v_pages, _Tensor)):
-        raise TypeError("k_pages and v_pages must be tensors")
-    shape, stride = k_pages.shape, k_pages.stride()
-    if len(shape) != 4 or shape != v_pages.shape or stride != v_pages.stride():
-        raise ValueError("k_pages and v_pages must be [num_pages, Hk, page_size, d], alike in "
-                         "shape and strides")
-    if (k_pages.dtype is not like.dtype or v_pages.dtype is not like.dtype
-            or k_pages.get_device() != like.dev or v_pages.get_device() != like.dev):
-        raise ValueError("k_pages and v_pages must have %s's dtype and device" % like.name)
-    num, Hk, page, d = shape
-    if d != like.d or stride[3] != 1:
-        raise ValueError("k_pages and v_pages must have %s's d, contiguous" % like.name)
-    if not isinstance(table, _Tensor) or table.dim() != 2 or table.shape[0] != num_seqs:
-        raise ValueError("table must be int32 [%d sequences, blocks]" % num_seqs)
-    return _CACHE.pack(k_pages.data_ptr(), v_pages.data_ptr(), stride[0], stride[1], stride[2], num,
-                       page, table.shape[1], _ints("table", table, like.dev),
-                       0 if kv_lens is None
-                       else _ints("kv_lens", kv_lens, like.dev, (num_seqs,))), Hk
+def _tokens(first, Hq, Hk, cu_seqlens, cu_seqlens_host, device, keep):
+    """gdn_tokens; boundaries that are not as the library takes them are converted."""
+    if cu_seqlens is None and cu_seqlens_host is not None:
+        raise ValueError("cu_seqlens_host without cu_seqlens")
+    t = _n.tokens(first, Hq, Hk, cu_seqlens, cu_seqlens_host)
+    if t is None:
+        pair = _cu_pair(cu_seqlens, cu_seqlens_host, device, keep)
+        keep.append(pair)
+        t = _n.tokens(first, Hq, Hk, *pair)
+    return t
 
 
 # ------------------------------------------------------------------ rotary positions
@@ -253,34 +191,33 @@ def gdn_rotary(rot, base=10000.0, layout="halves", scaling="none", factor=1.0, o
     return Rotary(turns.to(device), layout, scale)
 
 
-def _rotary(r, dev):
+def _rotary(r, first):
     if not isinstance(r, Rotary):
         raise TypeError("rotary must be a Rotary (see gdn_rotary)")
-    t = r.turns
-    if t.get_device() != dev or t.dtype is not torch.float64 or t.dim() != 1 \
-            or not t.is_contiguous():
-        raise ValueError("rotary.turns must be contiguous float64 [rot / 2] on the call's device")
     if r.layout not in LAYOUTS:
         raise ValueError("layout must be one of %s" % sorted(LAYOUTS))
-    return _ROTARY.pack(2 * t.numel(), LAYOUTS[r.layout], r.scale, t.data_ptr())
+    return _n.rotary(r.turns, LAYOUTS[r.layout], r.scale, first)
 
 
 def _rotate(f, q, k, rotary, positions, cu_seqlens, cu_seqlens_host, q_out, k_out):
     keep = []
-    like, Hq = _first("q", q)
-    rq, rk, ko, Hk = _rows("q", q, like), None, None, 1
+    rq = _n.first("q", q)
+    B, T, Hq, _ = q.shape
+    rk, ko, Hk = None, None, 1
     if q_out is None:
-        q_out = torch.empty_like(q)
+        q_out, ro = _n.like(q)
+    else:
+        ro = _n.rows("q_out", q_out, "q", q, Hq)
     if k is not None:
-        rk, Hk = _rows("k", k, like), k.shape[2]
+        rk, Hk = _n.rows("k", k, "q", q, -1), k.shape[2]
         if k_out is None:
-            k_out = torch.empty_like(k)
-        ko = _rows("k_out", k_out, like, Hk)
+            k_out, ko = _n.like(k)
+        else:
+            ko = _n.rows("k_out", k_out, "q", q, Hk)
     dev = q.device
-    t, _ = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
-    p = None if positions is None else _ints("positions", positions, like.dev, q.shape[:2])
-    _check(f(t, _rotary(rotary, like.dev), rq, rk, p, _rows("q_out", q_out, like, Hq), ko,
-             _stream(dev)))
+    t = _tokens(q, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
+    p = None if positions is None else _n.ints("positions", positions, q, B, T)
+    _check(f(t, _rotary(rotary, q), rq, rk, p, ro, ko, _stream(dev)))
     return q_out, k_out
 
 
@@ -313,20 +250,22 @@ def gdn_cache_append(q, k, v, k_pages, v_pages, table, kv_lens, rotary=None, cu_
     None: nothing is rotated.  Tokens whose page is a hole are not stored."""
     lib = load_library()
     keep = []
-    like, Hk = _first("k", k)
+    rk = _n.first("k", k)
+    B, _, Hk, _ = k.shape
     dev, Hq, rq, ro = k.device, Hk, None, None
     if q is not None:
-        rq, Hq = _rows("q", q, like), q.shape[2]
+        rq, Hq = _n.rows("q", q, "k", k, -1), q.shape[2]
         if q_out is None:
-            q_out = torch.empty_like(q)
-        ro = _rows("q_out", q_out, like, Hq)
-    t, n = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
-    c, heads = _cache(like, k_pages, v_pages, table, kv_lens, n)
-    if heads != Hk:
+            q_out, ro = _n.like(q)
+        else:
+            ro = _n.rows("q_out", q_out, "k", k, Hq)
+    n = B if cu_seqlens is None else cu_seqlens.shape[0] - 1
+    c = _n.cache("k", k, k_pages, v_pages, table, kv_lens, n)
+    if k_pages.shape[1] != Hk:
         raise ValueError("k_pages must have k's heads")
-    _check(lib.gdn_cache_append(t, None if rotary is None else _rotary(rotary, like.dev), rq,
-                                _rows("k", k, like), _rows("v", v, like, Hk), c, ro,
-                                _stream(dev)))
+    t = _tokens(k, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
+    _check(lib.gdn_cache_append(t, None if rotary is None else _rotary(rotary, k), rq, rk,
+                                _n.rows("v", v, "k", k, Hk), c, ro, _stream(dev)))
     return q_out
 
 
@@ -339,12 +278,13 @@ def gdn_cache_attn_workspace_size(q, k_pages, table, scale=None, causal=True, wi
                                   cu_seqlens=None, cu_seqlens_host=None) -> int:
     """Workspace bytes of gdn_cache_attn with these arguments (0: none is needed)."""
     keep = []
-    like, Hq = _first("q", q)
-    n = like.B if cu_seqlens is None else cu_seqlens.numel() - 1
-    c, Hk = _cache(like, k_pages, k_pages, table, None, n)
-    t, _ = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, q.device, keep)
-    return int(load_library().gdn_cache_attn_workspace_size(t, c, _attn(scale, like.d, causal,
-                                                                        window, max_kv)))
+    _n.first("q", q)
+    B, _, Hq, d = q.shape
+    n = B if cu_seqlens is None else cu_seqlens.shape[0] - 1
+    c = _n.cache("q", q, k_pages, k_pages, table, None, n)
+    t = _tokens(q, Hq, k_pages.shape[1], cu_seqlens, cu_seqlens_host, q.device, keep)
+    return int(load_library().gdn_cache_attn_workspace_size(t, c, _attn(scale, d, causal, window,
+                                                                        max_kv)))
 
 
 def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True, window=0,
@@ -359,78 +299,70 @@ def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True,
     sum.  A token that sees no key gets 0 (lse -inf)."""
     lib = load_library()
     keep = []
-    like, Hq = _first("q", q)
+    rq = _n.first("q", q)
+    B, T, Hq, d = q.shape
     dev = q.device
-    n = like.B if cu_seqlens is None else cu_seqlens.numel() - 1
-    c, Hk = _cache(like, k_pages, v_pages, table, kv_lens, n)
-    t, _ = _tokens(like, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
+    n = B if cu_seqlens is None else cu_seqlens.shape[0] - 1
+    c = _n.cache("q", q, k_pages, v_pages, table, kv_lens, n)
+    t = _tokens(q, Hq, k_pages.shape[1], cu_seqlens, cu_seqlens_host, dev, keep)
     if o is None:
-        o = torch.empty_like(q)
-    if lse is not None and (lse.dtype is not torch.float32 or lse.get_device() != like.dev
+        o, ro = _n.like(q)
+    else:
+        ro = _n.rows("o", o, "q", q, Hq)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.device != dev
                             or not lse.is_contiguous() or lse.shape != q.shape[:3]):
         raise ValueError("lse must be contiguous float32 [B, T, Hq] on q's device")
-    a = _attn(scale, like.d, causal, window, max_kv)
+    a = _attn(scale, d, causal, window, max_kv)
     need = lib.gdn_cache_attn_workspace_size(t, c, a)
     ws, size = None, 0
     if need:
         if workspace is None or workspace.numel() < need:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        elif (workspace.get_device() != like.dev or workspace.dtype is not torch.uint8
+        elif (workspace.device != dev or workspace.dtype is not torch.uint8
               or not workspace.is_contiguous()):
             raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
         ws, size = workspace.data_ptr(), workspace.numel()
-    _check(lib.gdn_cache_attn(t, a, _rows("q", q, like), c, _rows("o", o, like, Hq), _ptr(lse), ws,
-                              size, _stream(dev)))
+    _check(lib.gdn_cache_attn(t, a, rq, c, ro, _ptr(lse), ws, size, _stream(dev)))
     return o
 
 
 # ------------------------------------------------------------------ pages
 
 
-def _book(table, lens, refs, page_size, out, with_lens, extra, extra_shape):
+def _book(table, lens, refs, page_size, out, with_lens, extra):
     """gdn_book of tensors, the output tensors (``out``: the caller's, where given), the pointer of
-    the one named ``extra``, the device."""
+    the one named ``extra`` (shaped as refs: "map", or as lens)."""
     if not isinstance(table, _Tensor) or table.dim() != 2:
         raise ValueError("table must be int32 [sequences, blocks]")
     if not isinstance(refs, _Tensor) or refs.dim() != 1:
         raise ValueError("refs must be int32 [pages]")
-    dev, shape = table.get_device(), table.shape
-    if dev < 0:
+    if table.get_device() < 0:
         raise ValueError("table must be on the GPU")
-    S = shape[:1]
-    pt, pl, pr = _ints("table", table, dev), _ints("lens", lens, dev, S), _ints("refs", refs, dev)
+    S, blocks = table.shape
+    num, ints = refs.shape[0], _n.ints
+    pt, pl = ints("table", table, table), ints("lens", lens, table, S)
+    pr = ints("refs", refs, table)
+    like = refs if extra == "map" else lens
     if out is None:
-        got = {"table": torch.empty_like(table)}
+        got = {"table": _n.fresh(table), "refs": _n.fresh(refs),
+               extra: _n.fresh(like)}
         if with_lens:
-            got["lens"] = torch.empty_like(lens)
-        got["refs"] = torch.empty_like(refs)
-        got[extra] = torch.empty_like(refs if extra == "map" else lens)
+            got["lens"] = _n.fresh(lens)
     else:
         got = dict(out)
         for name, x in (("table", table), ("refs", refs), ("lens", lens if with_lens else None),
-                        (extra, refs if extra == "map" else lens)):
+                        (extra, like)):
             if x is not None and got.get(name) is None:
-                got[name] = torch.empty_like(x)
-    b = _BOOK.pack(S[0], shape[1], refs.numel(), page_size, pt, pl, pr,
-                   _ints("out table", got["table"], dev, shape),
-                   _ints("out lens", got["lens"], dev, S) if with_lens else 0,
-                   _ints("out refs", got["refs"], dev, refs.shape))
-    return b, got, _ints("out " + extra, got[extra], dev, extra_shape), dev
+                got[name] = _n.fresh(x)
+    b = _BOOK.pack(S, blocks, num, page_size, pt, pl, pr,
+                   ints("out table", got["table"], table, S, blocks),
+                   ints("out lens", got["lens"], table, S) if with_lens else 0,
+                   ints("out refs", got["refs"], table, num))
+    return b, got, ints("out " + extra, got[extra], table, like.shape[0])
 
 
-def _pool(pool, dev):
-    """gdn_pool of a [parts, num_pages, ...] tensor whose pages are contiguous."""
-    if pool is None:
-        return None
-    if not isinstance(pool, _Tensor) or pool.dim() < 3 or pool.get_device() != dev or dev < 0:
-        raise ValueError("pool must be a [parts, pages, ...] tensor on the GPU of the call")
-    shape, stride, inner = pool.shape, pool.stride(), 1
-    for i in range(len(shape) - 1, 1, -1):
-        if shape[i] != 1 and stride[i] != inner:
-            raise ValueError("pool must be contiguous within a page")
-        inner *= shape[i]
-    e = pool.element_size()
-    return _POOL.pack(pool.data_ptr(), shape[0], shape[1], stride[0] * e, stride[1] * e, inner * e)
+def _pool(pool, table):
+    return None if pool is None else _n.pool(pool, table)
 
 
 def _work(lib, b, workspace, device):
@@ -457,10 +389,10 @@ def gdn_pages_extend(table, lens, refs, add, page_size, out=None, workspace=None
     free).  short[s] > 0: there was no room for the pages it needs, and sequence s is as it was.
     ``out``: dict of tensors to write; the inputs themselves update in place."""
     lib = load_library()
-    b, got, short, dev = _book(table, lens, refs, page_size, out, True, "short", lens.shape)
+    b, got, short = _book(table, lens, refs, page_size, out, True, "short")
     device = table.device
     ws, p, n = _work(lib, b, workspace, device)
-    _check(lib.gdn_pages_extend(b, _ints("add", add, dev, lens.shape), short, p, n,
+    _check(lib.gdn_pages_extend(b, _n.ints("add", add, table, lens.shape[0]), short, p, n,
                                 _stream(device)))
     return got
 
@@ -472,11 +404,11 @@ def gdn_pages_select(table, lens, refs, parents, page_size, pool=None, out=None,
     page is copied for every row but the lowest of its parent, in ``pool`` [parts, pages, ...].
     short[i] == 1: no page was left and row i is empty."""
     lib = load_library()
-    b, got, short, dev = _book(table, lens, refs, page_size, out, True, "short", lens.shape)
+    b, got, short = _book(table, lens, refs, page_size, out, True, "short")
     device = table.device
     ws, p, n = _work(lib, b, workspace, device)
-    _check(lib.gdn_pages_select(b, _ints("parents", parents, dev, lens.shape), _pool(pool, dev),
-                                short, p, n, _stream(device)))
+    _check(lib.gdn_pages_select(b, _n.ints("parents", parents, table, lens.shape[0]),
+                                _pool(pool, table), short, p, n, _stream(device)))
     return got
 
 
@@ -484,10 +416,10 @@ def gdn_pages_compact(table, lens, refs, page_size, pool=None, out=None, workspa
     """Moves the pages in use into the lowest indexes: dict table, refs, map (new index of each
     page, -1 if it was free).  The data moves in ``pool`` [parts, pages, ...]."""
     lib = load_library()
-    b, got, to, dev = _book(table, lens, refs, page_size, out, False, "map", refs.shape)
+    b, got, to = _book(table, lens, refs, page_size, out, False, "map")
     device = table.device
     ws, p, n = _work(lib, b, workspace, device)
-    _check(lib.gdn_pages_compact(b, _pool(pool, dev), to, p, n, _stream(device)))
+    _check(lib.gdn_pages_compact(b, _pool(pool, table), to, p, n, _stream(device)))
     return got
 
 
@@ -496,9 +428,9 @@ def gdn_pages_copy(pool, src, dst):
     or a pool of recurrent states; pairs out of range are skipped."""
     if not isinstance(pool, _Tensor):
         raise TypeError("pool must be a tensor")
-    dev = pool.get_device()
-    p = _pool(pool, dev)
+    p = _n.pool(pool, pool)
     if not isinstance(src, _Tensor) or src.dim() != 1:
         raise ValueError("src must be int32 [pairs]")
-    _check(load_library().gdn_pages_copy(p, _ints("src", src, dev), _ints("dst", dst, dev, src.shape),
-                                         src.numel(), _stream(pool.device)))
+    n = src.shape[0]
+    _check(load_library().gdn_pages_copy(p, _n.ints("src", src, pool),
+                                         _n.ints("dst", dst, pool, n), n, _stream(pool.device)))
