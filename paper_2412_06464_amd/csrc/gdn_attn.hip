@@ -101,17 +101,17 @@ template <> struct Piece<float> {
   }
 };
 
-template <class E> __device__ inline bool finite4(const uint4& x) {
-  const unsigned w[4] = {x.x, x.y, x.z, x.w};
-  bool ok = true;
+// x without its infinities and NaN; true if there were any.
+template <class E> __device__ inline bool clear_odd(uint4& x) {
+  unsigned* w = reinterpret_cast<unsigned*>(&x);
+  bool odd = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(E) == 4)
-      ok = ok && (w[i] & 0x7f800000u) != 0x7f800000u;
-    else
-      ok = ok && (w[i] & 0x7f80u) != 0x7f80u && (w[i] & 0x7f800000u) != 0x7f800000u;
+    const unsigned u = w[i];
+    if ((u & 0x7f800000u) == 0x7f800000u) w[i] &= sizeof(E) == 4 ? 0u : 0xffffu, odd = true;
+    if (sizeof(E) == 2 && (u & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u, odd = true;
   }
-  return ok;
+  return odd;
 }
 
 // Over the four lanes (16 apart) of a column: the largest value, the sum.
@@ -262,7 +262,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
       lds0 + C::TILE + (kw * NK + vr) * RB +
       (sizeof(E) == 4 ? (((c16 >> 2) ^ v_swz<E, NP>(vr)) << 4) + (c16 & 3) * 4
                       : ((((c16 >> 1) & 1) ^ v_swz<E, NP>(vr)) << 4) + (c16 & 1) * 8);
-  auto step = [&](auto edge, int kw0, unsigned buf, unsigned gone, bool odd) {
+  auto step = [&](auto edge, int kw0, unsigned buf, unsigned gone) {
     constexpr bool EDGE = decltype(edge)::value;
     unsigned kaddr = kaddr0 + buf, vaddr = vaddr0 + buf;
     // opaque, or all the addresses below are kept in registers across the loop
@@ -337,23 +337,20 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
     // O^T
     if (PRIO) __builtin_amdgcn_s_setprio(1);
     if constexpr (sizeof(E) == 4) {
-      if (!EDGE || !odd) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              const float x = *(LDS_AS const float*)((vaddr ^ (d << 6)) + (16 * t + e) * RB);
+          for (int d = 0; d < DT; ++d) {
+            const float x = *(LDS_AS const float*)((vaddr ^ (d << 6)) + (16 * t + e) * RB);
 #pragma unroll
-              for (int u = 0; u < QT; ++u) o[d][u] = Mfma<float>::mma(x, s[t][u][e], o[d][u]);
-            }
+            for (int u = 0; u < QT; ++u) o[d][u] = Mfma<float>::mma(x, s[t][u][e], o[d][u]);
           }
-      }
     } else {
-      // p is rounded to bf16 for this product alone; l sums it unrounded
-      // lane i of 16 points at 4 channels of key row i / 4 and receives one
-      // channel (its own, i) of the 4 rows
+      // p is rounded to bf16 for this product alone; l sums it unrounded.
+      // Lane i of 16 points at 4 channels of key row i / 4 and receives one
+      // channel (its own, i) of the 4 rows.
       auto turned = [&](int t, int d) {
         return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (LDS_AS s16x4*)((vaddr ^ (d << 5)) + t * 16 * RB));
@@ -365,14 +362,12 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
           const bf16x4 x = {(bf16)s[0][u][0], (bf16)s[0][u][1], (bf16)s[0][u][2], (bf16)s[0][u][3]};
           p[u] = *reinterpret_cast<const s16x4*>(&x);
         }
-        if (!EDGE || !odd) {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const s16x4 x = turned(0, d);
+        for (int d = 0; d < DT; ++d) {
+          const s16x4 x = turned(0, d);
 #pragma unroll
-            for (int u = 0; u < QT; ++u)
-              o[d][u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p[u], o[d][u], 0, 0, 0);
-          }
+          for (int u = 0; u < QT; ++u)
+            o[d][u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p[u], o[d][u], 0, 0, 0);
         }
       } else {
 #pragma unroll
@@ -385,52 +380,18 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
               p[u][e] = (bf16)s[t][u][e];
               p[u][4 + e] = (bf16)s[t + 1][u][e];
             }
-          if (!EDGE || !odd) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              const s16x4 x0 = turned(t, d), x1 = turned(t + 1, d);
-              const s16x8 x = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
+          for (int d = 0; d < DT; ++d) {
+            const s16x4 x0 = turned(t, d), x1 = turned(t + 1, d);
+            const s16x8 x = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-              for (int u = 0; u < QT; ++u)
-                o[d][u] = Mfma<bf16>::mma(*reinterpret_cast<const bf16x8*>(&x), p[u], o[d][u]);
-            }
+            for (int u = 0; u < QT; ++u)
+              o[d][u] = Mfma<bf16>::mma(*reinterpret_cast<const bf16x8*>(&x), p[u], o[d][u]);
           }
         }
       }
     }
     if (PRIO) __builtin_amdgcn_s_setprio(0);
-    if constexpr (EDGE) {
-      if (odd) {  // key by key, only the rows that see it
-        const unsigned char* const vw = smem + buf + C::TILE + kw * NK * RB;
-#pragma unroll 1
-        for (int k = 0; k < NK; ++k) {
-          const int key = kw0 + k;
-          float p[QT];
-#pragma unroll
-          for (int u = 0; u < QT; ++u) {
-            float x = 0.f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (16 * t + e == (k & ~12)) x = s[t][u][e];
-            p[u] = __shfl(x, ((k >> 2) & 3) * 16 + c16);
-          }
-          const bool held = !(gone >> (k >> 4) & 1);
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const int ch = (16 * d + 4 * g) * (int)sizeof(E);
-            const f32x4 x = load4<E>(reinterpret_cast<const E*>(
-                vw + k * RB + (((ch >> 4) ^ v_swz<E, NP>(k)) << 4) + (ch & 15)));
-#pragma unroll
-            for (int u = 0; u < QT; ++u)
-              if (held && key < last[u] && key >= first[u])
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[d][u][e] = fmaf(p[u], x[e], o[d][u][e]);
-          }
-        }
-      }
-    }
   };
 
   // The copies of tile `it` are there and the other buffer is no longer read;
@@ -452,6 +413,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
     }
     return now;
   };
+  bool odd = false;
   int it = 0;
   while (it < tiles) {
     unsigned now;
@@ -462,32 +424,35 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
       now = next_tile(it);
       const int f0 = begin + it * KT + kw * NK;
       if (f0 + NK > all_hi || f0 < all_lo || now) break;
-      step(std::false_type{}, f0, (it & 1) * 2 * C::TILE, 0u, false);
+      step(std::false_type{}, f0, (it & 1) * 2 * C::TILE, 0u);
       if (++it == tiles) break;
     }
     if (it == tiles) break;
     // Keys that no row sees may hold anything: their v is cleared.  Where some
     // rows see a key and others do not, an infinity or NaN in its v must not
-    // meet a p of zero: those tiles take the product key by key.
+    // meet a p of zero: it is taken out too, and added to the rows that do see it
+    // after the end.
     const unsigned buf = (it & 1) * 2 * C::TILE;
     const int kw0 = begin + it * KT + kw * NK;  // this wave's keys
-    bool bad = false, odd;
-    const int tid = KW == 1 ? (int)threadIdx.x : lane;
 #pragma unroll 1
-    for (int i = tid; i < NK * NP; i += KW == 1 ? C::NTH : 64) {
+    for (int i = KW == 1 ? (int)threadIdx.x : lane; i < NK * NP; i += KW == 1 ? C::NTH : 64) {
       const int r = i / NP, key = kw0 + r;
       uint4* p = reinterpret_cast<uint4*>(smem + buf + C::TILE + kw * NK * RB + i * 16);
-      if (key >= end || key < b.seen || (now >> (r >> 4) & 1))
+      if (key >= end || key < b.seen || (now >> (r >> 4) & 1)) {
         *p = make_uint4(0, 0, 0, 0);
-      else
-        bad = bad || !finite4<E>(*p);
+      } else {
+        uint4 x = *p;
+        if (clear_odd<E>(x)) {
+          *p = x;
+          odd = true;
+        }
+      }
     }
     if (KW == 1)
-      odd = __syncthreads_or(bad);
+      lds_barrier();
     else
-      odd = __ballot(bad) != 0;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (!idle && kw0 < w_end && kw0 + NK > w_begin) step(std::true_type{}, kw0, buf, now, odd);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (!idle && kw0 < w_end && kw0 + NK > w_begin) step(std::true_type{}, kw0, buf, now);
     ++it;
   }
 
@@ -564,6 +529,50 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
         for (int e = 0; e < 4; ++e) x[e] += al * y[e];
       }
       put(b.r0 + r, ch, x, mx, ll);
+    }
+  }
+
+  // The infinities and NaN that were taken out: a thread owns 16 bytes of channels
+  // of all rows, reads them again of every key of those tiles, and adds what it
+  // finds to the rows that see the key (whatever their weight and scale, it makes
+  // them infinite or NaN).
+  if (!__syncthreads_or(odd)) return;
+  if (threadIdx.x >= NP) return;
+  constexpr int N = 16 / (int)sizeof(E);
+#pragma unroll 1
+  for (int f0 = begin; f0 < end; f0 += NK) {
+    bool gap = false;
+#pragma unroll 1
+    for (int k = f0; k < min(f0 + NK, end); k += 16) gap = gap || !there(pages[k >> shift]);
+    if (f0 + NK <= all_hi && f0 >= all_lo && f0 + NK <= end && !gap) continue;
+#pragma unroll 1
+    for (int key = max(f0, b.seen); key < min(f0 + NK, end); ++key) {
+      const int page = pages[key >> shift];
+      if (!there(page)) continue;
+      uint4 x = *reinterpret_cast<const uint4*>(vbase + (int64_t)page * a.cache.page +
+                                                (int64_t)(key & mask) * a.cache.slot +
+                                                threadIdx.x * 16);
+      const uint4 was = x;
+      if (!clear_odd<E>(x)) continue;
+      const E* v = reinterpret_cast<const E*>(&was);
+#pragma unroll 1
+      for (int r = b.r0; r < b.r1; ++r) {
+        const int i = r / a.G, h = b.hk * a.G + r - i * a.G;
+        if (key < b.first(a, i) || key >= b.last(a, i)) continue;
+        const int64_t at = (int64_t)(b.q0 + i) * a.Hq + h;
+        float* w = a.part + (split * rows + at) * D + threadIdx.x * N;
+        E* y = reinterpret_cast<E*>(a.o.data + (int64_t)(b.q0 + i) * a.o.ts + h * a.o.hs) +
+               threadIdx.x * N;
+#pragma unroll 1
+        for (int e = 0; e < N; ++e) {
+          const float z = to_f(v[e]);
+          if (z - z == 0.f) continue;
+          if (a.splits > 1)
+            w[e] += z;
+          else
+            y[e] = to_e<E>(to_f(y[e]) + z);
+        }
+      }
     }
   }
 }
