@@ -13,7 +13,7 @@
 // permuted contraction order of gdn_device.h).
 //
 // Two kernels from one body:
-//   k_attn_tile  many rows: 4 waves with 32 rows each share a tile of keys;
+//   k_attn_tile  many rows: 4 waves with 32 (or 16) rows each share a tile of keys;
 //   k_attn_few   few rows (at most 32): 4 waves share the rows, each walks its
 //                own keys of a tile and the results are joined in LDS.
 // Where the row blocks do not fill the GPU, a block's keys are split over
@@ -590,8 +590,8 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;
   b.r0 = 0;
+  if (b.m == 0 || (int64_t)b.m * a.G > C::ROWS) return;
   b.r1 = b.m * a.G;
-  if (b.m == 0 || b.r1 > C::ROWS) return;
   b.kv = cached(a.cache, b.n);
   b.range(a);
   // a range past the keys: no partial result is read there
@@ -603,11 +603,11 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
 // block of a slot follow from the boundaries: sequence n's slots begin at
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
 // the next one's.
-template <class E, int D, int KT>
+template <class E, int D, int QT, int KT>
 __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile(AttnArgs a,
                                                                                 int slots) {
-  using C = AttnCfg<E, D, 2, 4, 1, KT>;
-  static_assert(C::ROWS == TILE_ROWS, "row block");
+  using C = AttnCfg<E, D, QT, 4, 1, KT>;
+  constexpr int R = C::ROWS;
   __shared__ __align__(1024) unsigned char smem[C::LDS];
   Block b;
   b.hk = blockIdx.x % a.Hk;
@@ -620,97 +620,116 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
     int lo = 0, hi = a.tok.N;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if ((int)(a.tok.cu[mid] * G / TILE_ROWS) + mid <= slot) lo = mid; else hi = mid;
+      if ((int)(a.tok.cu[mid] * G / R) + mid <= slot) lo = mid; else hi = mid;
     }
     b.n = lo;
-    tile = slot - ((int)(a.tok.cu[lo] * G / TILE_ROWS) + lo);
+    tile = slot - ((int)(a.tok.cu[lo] * G / R) + lo);
   } else {
-    const int per = (int)(((int64_t)a.tok.T * a.G + TILE_ROWS - 1) / TILE_ROWS);
+    const int per = (int)(((int64_t)a.tok.T * a.G + R - 1) / R);
     b.n = slot / per;
     tile = slot - b.n * per;
   }
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;
   const int64_t rows = (int64_t)b.m * a.G;
-  if ((int64_t)tile * TILE_ROWS >= rows || rows <= FEW_ROWS) return;
-  b.r0 = tile * TILE_ROWS;
-  b.r1 = (int)min(rows, (int64_t)b.r0 + TILE_ROWS);
+  if ((int64_t)tile * R >= rows) return;
+  b.r0 = tile * R;
+  b.r1 = (int)min(rows, (int64_t)b.r0 + R);
   b.kv = cached(a.cache, b.n);
   b.range(a);
   if (split > 0 && b.lo + split * a.len >= b.hi) return;
-  attn_block<E, D, 2, 4, 1, KT>(a, b, split, smem);
+  attn_block<E, D, QT, 4, 1, KT>(a, b, split, smem);
 }
 
-// Joins the splits' sums: a workgroup to a row.  The threads first turn the
-// splits' maxima into weights, then 256 / (D / 4) groups of them add up the
-// weighted sums of every so many-th split, four loads in flight each.
-template <class E, int D> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  constexpr int TPR = D / 4, NG = 256 / TPR;
-  __shared__ float weight[MAX_SPLITS];
-  __shared__ float red[8];
-  __shared__ f32x4 sums[256];
-  const int64_t rows = (int64_t)a.tok.total * a.Hq, at = blockIdx.x;
-  const int tid = threadIdx.x;
+// Joins the splits' sums of a row by T threads: they turn the splits' maxima into
+// weights, then T / (D / 4) groups of them add up the weighted sums of every so
+// many-th split, four loads in flight each.  T = 256 where a row has many splits;
+// T = D / 4, so several rows to a workgroup and no exchange between threads, where it
+// has few (16000 rows of 3 splits: 25 us with 256 threads a row).
+template <class E, int D, int T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
+  constexpr int TPR = D / 4, NG = T / TPR, PER = 256 / T;
+  const int64_t rows = (int64_t)a.tok.total * a.Hq;
+  const int64_t at = (int64_t)blockIdx.x * PER + (PER > 1 ? threadIdx.x / T : 0);
+  if (at >= rows) return;
+  const int tid = PER > 1 ? threadIdx.x % T : threadIdx.x;
   const int t = (int)(at / a.Hq), h = (int)(at - (int64_t)t * a.Hq);
   Block b;
   b.n = seq_of(a.tok, t);
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;
   const int64_t all = (int64_t)b.m * a.G;
-  if ((all <= FEW_ROWS) != (a.few != 0)) return;
   const int r = (t - b.q0) * a.G + h % a.G;
-  const int R = a.few ? FEW_ROWS : TILE_ROWS;
-  b.r0 = r / R * R;
-  b.r1 = (int)min(all, (int64_t)b.r0 + R);
+  b.r0 = r / a.block * a.block;
+  b.r1 = (int)min(all, (int64_t)b.r0 + a.block);
   b.kv = cached(a.cache, b.n);
   b.range(a);
   const int live = min(a.splits, max(1, (b.hi - b.lo + a.len - 1) / a.len));
 
-  float m[(MAX_SPLITS + 255) / 256], l[(MAX_SPLITS + 255) / 256], mx = -INFINITY, ll = 0.f;
-#pragma unroll
-  for (int j = 0; j < (MAX_SPLITS + 255) / 256; ++j) {
-    const int s = tid + 256 * j;
-    const float2 x = s < live ? *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * rows + at))
-                              : make_float2(-INFINITY, 0.f);
-    m[j] = x.x;
-    l[j] = x.y;
-    mx = fmaxf(mx, x.x);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-  if (lane_id() == 0) red[wave_id()] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float ref = mx == -INFINITY ? 0.f : mx;
-#pragma unroll
-  for (int j = 0; j < (MAX_SPLITS + 255) / 256; ++j) {
-    const float w = __builtin_amdgcn_exp2f(m[j] - ref);
-    if (tid + 256 * j < live) weight[tid + 256 * j] = w;
-    ll += w * l[j];
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) ll += __shfl_xor(ll, d);
-  if (lane_id() == 0) red[4 + wave_id()] = ll;
-  __syncthreads();
-  ll = (red[4] + red[5]) + (red[6] + red[7]);
-
-  const int grp = tid / TPR, ch = (tid % TPR) * 4;
+  const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
+  float mx = -INFINITY, ll = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  const int grp = tid / TPR, ch = (tid % TPR) * 4;
+  if constexpr (PER > 1) {
+    static_assert(NG == 1, "one group of threads a row");
 #pragma unroll 4
-  for (int s = grp; s < live; s += NG) {
-    const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * D + ch);
-    const float w = weight[s];
+    for (int s = 0; s < live; ++s) mx = fmaxf(mx, ml[s * rows + at].x);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll 4
+    for (int s = 0; s < live; ++s) {
+      const float2 z = ml[s * rows + at];
+      const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * D + ch);
+      const float w = __builtin_amdgcn_exp2f(z.x - ref);
+      ll += w * z.y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = fmaf(w, y[e], x[e]);
-  }
-  sums[tid] = x;
-  __syncthreads();
-  if (tid >= TPR) return;
+      for (int e = 0; e < 4; ++e) x[e] = fmaf(w, y[e], x[e]);
+    }
+  } else {
+    __shared__ float weight[MAX_SPLITS];
+    __shared__ float red[8];
+    __shared__ f32x4 sums[256];
+    constexpr int J = (MAX_SPLITS + 255) / 256;
+    float m[J], l[J];
 #pragma unroll
-  for (int j = 1; j < NG; ++j) {
-    const f32x4 y = sums[tid + j * TPR];
+    for (int j = 0; j < J; ++j) {
+      const int s = tid + 256 * j;
+      const float2 z = s < live ? ml[s * rows + at] : make_float2(-INFINITY, 0.f);
+      m[j] = z.x;
+      l[j] = z.y;
+      mx = fmaxf(mx, z.x);
+    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] += y[e];
+    for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+    if (lane_id() == 0) red[wave_id()] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const float w = __builtin_amdgcn_exp2f(m[j] - ref);
+      if (tid + 256 * j < live) weight[tid + 256 * j] = w;
+      ll += w * l[j];
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) ll += __shfl_xor(ll, d);
+    if (lane_id() == 0) red[4 + wave_id()] = ll;
+    __syncthreads();
+    ll = (red[4] + red[5]) + (red[6] + red[7]);
+#pragma unroll 4
+    for (int s = grp; s < live; s += NG) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * D + ch);
+      const float w = weight[s];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = fmaf(w, y[e], x[e]);
+    }
+    sums[tid] = x;
+    __syncthreads();
+    if (tid >= TPR) return;
+#pragma unroll
+    for (int j = 1; j < NG; ++j) {
+      const f32x4 y = sums[tid + j * TPR];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e];
+    }
   }
   const float inv = ll == 0.f ? 0.f : 1.f / ll;
   E* p = reinterpret_cast<E*>(a.o.data + (int64_t)t * a.o.ts + h * a.o.hs) + ch;
@@ -756,13 +775,13 @@ int attn_few_keys(Dt dt, int d) {
 }
 int attn_tile_keys(Dt dt, int d) { return d * (dt == Dt::F32 ? 4 : 2) >= 512 ? 32 : 64; }
 
-hipError_t launch_attn_few(Dt dt, int d, bool rows16, const AttnArgs& a, hipStream_t s) {
+hipError_t launch_attn_few(Dt dt, int d, const AttnArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)a.tok.N * a.splits * a.Hk);
   return by_dim(dt, d, [&](auto e, auto dim) {
     using E = decltype(e);
     constexpr int D = decltype(dim)::value;
     using F = Few<E, D>;
-    if (rows16)
+    if (a.block == 16)
       hipLaunchKernelGGL((k_attn_few<E, D, 1, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
     else
       hipLaunchKernelGGL((k_attn_few<E, D, 2, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
@@ -775,7 +794,10 @@ hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStrea
   return by_dim(dt, d, [&](auto e, auto dim) {
     using E = decltype(e);
     constexpr int D = decltype(dim)::value;
-    hipLaunchKernelGGL((k_attn_tile<E, D, Tile<E, D>::KT>), dim3(grid), dim3(256), 0, s, a, slots);
+    if (a.block == 64)
+      hipLaunchKernelGGL((k_attn_tile<E, D, 1, Tile<E, D>::KT>), dim3(grid), dim3(256), 0, s, a, slots);
+    else
+      hipLaunchKernelGGL((k_attn_tile<E, D, 2, Tile<E, D>::KT>), dim3(grid), dim3(256), 0, s, a, slots);
     return hipGetLastError();
   });
 }
@@ -784,8 +806,12 @@ hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.tok.total * a.Hq;
   return by_dim(dt, d, [&](auto e, auto dim) {
     using E = decltype(e);
-    hipLaunchKernelGGL((k_attn_join<E, decltype(dim)::value>), dim3((unsigned)rows), dim3(256), 0, s,
-                       a);
+    constexpr int D = decltype(dim)::value, T = D / 4, PER = 256 / T;
+    if (a.splits <= 16)
+      hipLaunchKernelGGL((k_attn_join<E, D, T>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(256),
+                         0, s, a);
+    else
+      hipLaunchKernelGGL((k_attn_join<E, D, 256>), dim3((unsigned)rows), dim3(256), 0, s, a);
     return hipGetLastError();
   });
 }

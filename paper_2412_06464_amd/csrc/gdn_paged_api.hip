@@ -129,25 +129,13 @@ gdn_status rotate(const gdn_tokens* t, const gdn_rotary* r, const gdn_rows* q, c
   return done(gdn::launch_rotate(type_of(t->dtype), a, (hipStream_t)stream));
 }
 
-// How a call's work is cut: row blocks of the two kernels, splits of their keys.
+// How a call's work is cut: which kernel, its row blocks, splits of their keys.
 struct Plan {
-  bool few = false, tile = false;  // which kernels have sequences
-  bool rows16 = true;              // no few-rows sequence has more than 16 rows
-  int slots = 0;                   // of the tile kernel
-  int few_splits = 1, few_len = 0, tile_splits = 1, tile_len = 0;
-  size_t part = 0, bytes = 0;      // workspace: offset of {maximum, sum}; size
+  bool few = false;
+  int block = 0, slots = 0;    // rows of a block; blocks of the tile kernel's grid
+  int splits = 1, len = 0;     // key ranges
+  size_t part = 0, bytes = 0;  // workspace: offset of {maximum, sum}; size
 };
-
-// Splits so that about `want` workgroups have keys, no range shorter than `least`.
-void split(int64_t units, int64_t keys, int step, int64_t want, int64_t least, int* splits,
-           int* len) {
-  int64_t s = units >= want / 2 ? 1 : (want + units - 1) / units;
-  s = std::max<int64_t>(1, std::min({s, keys / least, (int64_t)gdn::MAX_SPLITS}));
-  int64_t l = (keys + s - 1) / s;
-  l = (l + step - 1) / step * step;
-  *len = (int)l;
-  *splits = (int)((keys + l - 1) / l);
-}
 
 gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cache* c,
                      const gdn_attn* a, Plan* out) {
@@ -158,52 +146,91 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
   if (t->Hq % t->Hk) return GDN_ERR_SHAPE;
   Plan p;
   const int64_t G = t->Hq / t->Hk;
-  int64_t most_few = 0, most = 0, n_few = 0;  // new tokens of a sequence
+  const Dt dt = type_of(t->dtype);
+  int64_t seqs = 0, most = 0;           // sequences with new tokens; the most of one
+  int64_t blocks64 = 0, blocks128 = 0;  // row blocks
   auto see = [&](int64_t m) {
-    if (m * G <= gdn::FEW_ROWS) {
-      if (m == 0) return;
-      ++n_few;
-      most_few = std::max(most_few, m);
-    } else {
-      p.tile = true;
-      most = std::max(most, m);
-    }
+    if (m == 0) return;
+    ++seqs;
+    most = std::max(most, m);
+    blocks64 += (m * G + 63) / 64;
+    blocks128 += (m * G + 127) / 128;
   };
-  if (tok.cu)
+  if (tok.cu) {
     for (int n = 0; n < tok.N; ++n) see(t->cu_seqlens_host[n + 1] - t->cu_seqlens_host[n]);
-  else
+  } else {
     see(tok.T);
-  if (!tok.cu && n_few) n_few = tok.N;
-  p.few = n_few > 0;
-  p.rows16 = most_few * G <= 16;
-  const int R = gdn::TILE_ROWS;
-  p.slots = tok.cu ? (int)((int64_t)tok.total * G / R) + tok.N
-                   : tok.N * (int)(((int64_t)tok.T * G + R - 1) / R);
+    seqs *= tok.N;
+    blocks64 *= tok.N;
+    blocks128 *= tok.N;
+  }
   const int64_t room = (int64_t)c->max_blocks * c->page_size;
   const int64_t kv = std::max<int64_t>(1, a->max_kv > 0 ? std::min<int64_t>(a->max_kv, room) : room);
-  const Dt dt = type_of(t->dtype);
   // A block of m tokens sees at most window + m - 1 keys, and its range begins
   // at a multiple of 16.
   auto keys = [&](int64_t m) { return a->window > 0 ? std::min(kv, a->window + m + 14) : kv; };
-  // A workgroup of the few-rows kernel has a CU to itself (128 KB of LDS at most
-  // head dims): 256 of them are wanted; more cost more partial sums than they
-  // balance (two sequences of 131072 keys, 4 cache heads: 97 us, with 512 100,
-  // with 2048 113; 12 of up to 3000 keys in fp32, 8 heads: 22.4 and 26.4).  Two
-  // of the other kernel share a CU: 512, in ranges of 256 keys or more.
-  if (p.few)
-    split(n_few * t->Hk, keys(most_few), gdn::attn_few_keys(dt, t->d), 256,
-          gdn::attn_few_keys(dt, t->d), &p.few_splits, &p.few_len);
-  if (p.tile)
-    split((int64_t)p.slots * t->Hk, keys(std::min<int64_t>(most, R / G + 2)),
-          gdn::attn_tile_keys(dt, t->d), 512, 256, &p.tile_splits, &p.tile_len);
-  const int64_t splits = std::max(p.few_splits, p.tile_splits);
-  if ((int64_t)tok.N * p.few_splits * t->Hk >= (int64_t)1 << 31 ||
-      (int64_t)p.slots * p.tile_splits * t->Hk >= (int64_t)1 << 31)
+  auto cut = [&](int64_t range, int64_t splits, int step) {
+    p.len = (int)(((range + splits - 1) / splits + step - 1) / step * step);
+    p.splits = (int)((range + p.len - 1) / p.len);
+  };
+
+  // Where every sequence has few rows, their kernel: bf16 single tokens at d = 128
+  // take the same in both (a batch of 256 in a 2K window 149 and 147 us), 8 tokens of 4
+  // heads 57 and 84, fp32 94 and 146.  With larger ones beside them, all in one
+  // launch of the other: 127 single tokens and 512 of one sequence over up to 4000
+  // keys 123 us, in a launch each 150.
+  p.few = most * G <= gdn::FEW_ROWS;
+  if (p.few) {
+    p.block = most * G <= 16 ? 16 : 32;
+    // A workgroup of this kernel has a CU to itself (128 KB of LDS at most head
+    // dims): 256 of them are wanted; more cost more partial sums than they
+    // balance (two sequences of 131072 keys, 4 cache heads: 97 us, with 512 100,
+    // with 2048 113; 12 of up to 3000 keys in fp32, 8 heads: 22.4 and 26.4).
+    const int step = gdn::attn_few_keys(dt, t->d);
+    const int64_t units = std::max<int64_t>(1, seqs * t->Hk), range = keys(most);
+    const int64_t s = units >= 128 ? 1 : std::min((256 + units - 1) / units, range / step);
+    cut(range, std::max<int64_t>(1, s), step);
+  } else {
+    // Two workgroups share a CU.  Blocks of 128 rows halve what is read of LDS and
+    // of the cache for a product; blocks of 64 take half as long where all run at
+    // once and keys are not many, or where sequences are so short that blocks of 128
+    // were half empty (156 sequences, 175 tokens in one and one in the others, d = 256:
+    // 29 and 20 us; 86 of up to 18 tokens of 4 heads, d = 128: 32 and 16; but 32 of 100
+    // tokens of 4 heads, 500 keys: 32 and 38).
+    const bool small =
+        (blocks64 * t->Hk <= 512 && keys(most) <= 4096) || 5 * blocks64 <= 8 * blocks128;
+    p.block = small ? 64 : 128;
+    p.slots = tok.cu ? (int)((int64_t)tok.total * G / p.block) + tok.N
+                     : tok.N * (int)(((int64_t)tok.T * G + p.block - 1) / p.block);
+    // Splits, by what each number would take: rounds of 512 workgroups, each its
+    // tiles (us for 64 keys, measured alone: bf16 0.7 at d = 64, fp32 6 times that)
+    // and a start of 3 us; and, for more than one, the partial sums' way through
+    // memory and the join's launch (1000 tokens of 16 heads, 4 cache heads: 1 split
+    // 23 us, 3 46; 56 tokens of 32 heads over 95000 keys: 128 us, with 8 splits).
+    const int step = gdn::attn_tile_keys(dt, t->d);
+    const int64_t units = (small ? blocks64 : blocks128) * t->Hk;
+    const int64_t range = keys(std::min<int64_t>(most, p.block / G + 2));
+    const double tile = (dt == Dt::F32 ? 4.2 : 0.7) * t->d / 64 * (small ? 0.6 : 1.0);
+    double best = 0;
+    int64_t at = 1;
+    for (int64_t s = 1; s <= gdn::MAX_SPLITS; s += s < 4 ? 1 : s / 4) {
+      cut(range, s, step);
+      const double us = (double)((units * p.splits + 511) / 512) * (p.len / 64.0 * tile + 3) +
+                        (p.splits > 1 ? 5 + 8.0 * p.splits * tok.total * t->Hq * t->d / 4e6 : 0);
+      if (s == 1 || us < best) {
+        best = us;
+        at = s;
+      }
+      if (p.len == step) break;
+    }
+    cut(range, at, step);
+  }
+  if ((int64_t)(p.few ? tok.N : p.slots) * p.splits * t->Hk >= (int64_t)1 << 31)
     return GDN_ERR_SHAPE;
-  if (splits > 1) {
+  if (p.splits > 1) {
     const int64_t rows = (int64_t)tok.total * t->Hq;
-    p.part = up((size_t)(splits * rows * t->d * 4));
-    p.bytes = p.part + up((size_t)(splits * rows * 8));
+    p.part = up((size_t)(p.splits * rows * t->d * 4));
+    p.bytes = p.part + up((size_t)(p.splits * rows * 8));
   }
   *out = p;
   return GDN_OK;
@@ -385,21 +412,13 @@ gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_row
   a.c = at->scale * 1.4426950408889634f;
   const Dt dt = type_of(t->dtype);
   hipStream_t s = (hipStream_t)stream;
-  if (p.few) {
-    a.few = 1;
-    a.splits = p.few_splits;
-    a.len = p.few_len;
-    if (gdn::launch_attn_few(dt, t->d, p.rows16, a, s) != hipSuccess) return GDN_ERR_HIP;
-    if (a.splits > 1 && gdn::launch_attn_join(dt, t->d, a, s) != hipSuccess) return GDN_ERR_HIP;
-  }
-  if (p.tile) {
-    a.few = 0;
-    a.splits = p.tile_splits;
-    a.len = p.tile_len;
-    if (gdn::launch_attn_tile(dt, t->d, p.slots, a, s) != hipSuccess) return GDN_ERR_HIP;
-    if (a.splits > 1 && gdn::launch_attn_join(dt, t->d, a, s) != hipSuccess) return GDN_ERR_HIP;
-  }
-  return GDN_OK;
+  a.block = p.block;
+  a.splits = p.splits;
+  a.len = p.len;
+  hipError_t e = p.few ? gdn::launch_attn_few(dt, t->d, a, s)
+                       : gdn::launch_attn_tile(dt, t->d, p.slots, a, s);
+  if (e == hipSuccess && p.splits > 1) e = gdn::launch_attn_join(dt, t->d, a, s);
+  return done(e);
 }
 
 size_t gdn_pages_workspace_size(const gdn_book* b) {

@@ -51,20 +51,20 @@ struct AttnArgs {
   int Hq, Hk, G;    // G = Hq / Hk
   int causal, window;
   float c;          // scale * log2(e)
-  int few;          // 1: sequences of at most FEW_ROWS rows, 0: the others
+  int block;        // rows of a block
   int splits, len;  // key ranges of `len` keys (the last: all that follow)
 };
-// Sequences whose rows (new tokens x query heads of a cache head) are at most
-// this many take the kernel whose waves share the rows and split the keys.
+// Calls whose sequences have at most this many rows (new tokens x query heads of a
+// cache head) take the kernel whose waves share the rows and split the keys.
 constexpr int FEW_ROWS = 32;
-constexpr int TILE_ROWS = 128;  // rows of a workgroup of the other kernel
 constexpr int MAX_SPLITS = 512;
 
 // keys of a tile: the unit of `len`
 int attn_few_keys(Dt dt, int d);
 int attn_tile_keys(Dt dt, int d);
-// rows16: no sequence of the class has more than 16 rows; slots: row blocks
-hipError_t launch_attn_few(Dt dt, int d, bool rows16, const AttnArgs& a, hipStream_t s);
+// a.block: 16 or 32 rows, no sequence more
+hipError_t launch_attn_few(Dt dt, int d, const AttnArgs& a, hipStream_t s);
+// a.block: 64 or 128 rows; slots: row blocks
 hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s);
 
