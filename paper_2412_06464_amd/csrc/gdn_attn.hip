@@ -746,7 +746,8 @@ namespace {
 // of k and v (most bytes in flight), four waves where that leaves each a group
 // of 16.  The other: as many as let two workgroups share a CU (64 KB of buffers),
 // so that one's products run beside the other's softmax: at d = 256 in bf16 32
-// keys, prompts in a 2K window 284 us, with 64 and one workgroup 317.
+// keys, prompts in a 2K window 284 us, with 64 and one workgroup 317; at d = 64 in bf16
+// 64 keys leave room for three or four (a prompt of 8192 tokens 170 us, with 128 205).
 template <class E, int D> struct Few {
   static constexpr int RB = D * (int)sizeof(E);
   static constexpr int KW = RB >= 1024 ? 2 : 4;

@@ -174,12 +174,19 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
     p.splits = (int)((range + p.len - 1) / p.len);
   };
 
-  // Where every sequence has few rows, their kernel: bf16 single tokens at d = 128
-  // take the same in both (a batch of 256 in a 2K window 149 and 147 us), 8 tokens of 4
-  // heads 57 and 84, fp32 94 and 146.  With larger ones beside them, all in one
-  // launch of the other: 127 single tokens and 512 of one sequence over up to 4000
-  // keys 123 us, in a launch each 150.
-  p.few = most * G <= gdn::FEW_ROWS;
+  // Where every sequence has few rows, their kernel, whose waves take different
+  // keys: 8 tokens of 4 heads over up to 4000 keys, 64 sequences, 57 us, in the
+  // other 84; fp32 single tokens over 2000 keys 94 and 146.  Bf16 single tokens that
+  // fill the GPU take the same in both (a batch of 256 in a 2K window 149 and 147
+  // us), and where their keys are so few that a workgroup's start counts, two of the
+  // other to a CU are the faster (212 sequences, 8 cache heads: 70 keys 43 and 27
+  // us, 500 100 and 89, 1000 163 and 162; 176 in fp32, 2 cache heads: 317 keys 26
+  // and 45, 836 units of 3 keys 22 and 15).  With larger sequences beside them, all
+  // in one launch of the other: 127 single tokens and 512 of one sequence over up to
+  // 4000 keys 123 us, in a launch each 150.
+  const int64_t few_units = std::max<int64_t>(1, seqs * t->Hk), few_keys = keys(most);
+  p.few = most * G <= gdn::FEW_ROWS &&
+          (few_units <= 256 || few_keys * (dt == Dt::F32 ? 8 : 1) > 1024);
   if (p.few) {
     p.block = most * G <= 16 ? 16 : 32;
     // A workgroup of this kernel has a CU to itself (128 KB of LDS at most head
@@ -187,43 +194,50 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
     // balance (two sequences of 131072 keys, 4 cache heads: 97 us, with 512 100,
     // with 2048 113; 12 of up to 3000 keys in fp32, 8 heads: 22.4 and 26.4).
     const int step = gdn::attn_few_keys(dt, t->d);
-    const int64_t units = std::max<int64_t>(1, seqs * t->Hk), range = keys(most);
-    const int64_t s = units >= 128 ? 1 : std::min((256 + units - 1) / units, range / step);
-    cut(range, std::max<int64_t>(1, s), step);
+    const int64_t s = few_units >= 128 ? 1 : std::min((255 + few_units) / few_units, few_keys / step);
+    cut(few_keys, std::max<int64_t>(1, s), step);
   } else {
-    // Two workgroups share a CU.  Blocks of 128 rows halve what is read of LDS and
-    // of the cache for a product; blocks of 64 take half as long where all run at
-    // once and keys are not many, or where sequences are so short that blocks of 128
-    // were half empty (156 sequences, 175 tokens in one and one in the others, d = 256:
-    // 29 and 20 us; 86 of up to 18 tokens of 4 heads, d = 128: 32 and 16; but 32 of 100
-    // tokens of 4 heads, 500 keys: 32 and 38).
-    const bool small =
-        (blocks64 * t->Hk <= 512 && keys(most) <= 4096) || 5 * blocks64 <= 8 * blocks128;
-    p.block = small ? 64 : 128;
+    // Rows of a block and splits of its keys, by what each choice would take: a
+    // start of 5 us; for 64 keys of 128 rows 0.8, 1.3 and 2.9 us at d = 64, 128 and
+    // 256 in bf16 where a workgroup is alone on its CU, 4.7, 8.2 and 18 in fp32, 0.62 of
+    // that with 64 rows (0.9 at d = 64, where it is the copies' latency); 1.5 (fp32 1.9)
+    // times as long where two share it, 1.25 with three at d = 64; no less than half
+    // of what the cache would take from HBM at its longest; with splits, the partial
+    // sums' way through memory and the join's launch.  (1000 tokens of 16 heads, 4 cache
+    // heads: 1 split 23 us, 3 46.  32 sequences of 100 tokens, 500 keys: blocks of 128
+    // 32 us, of 64 38; 156 sequences, 175 tokens in one and one in the others, d = 256:
+    // 29 and 20.)
+    const int step = gdn::attn_tile_keys(dt, t->d);
+    const bool f32 = dt == Dt::F32, thin = !f32 && t->d == 64;
+    const double alone = t->d == 64 ? (f32 ? 4.7 : 0.8) : t->d == 128 ? (f32 ? 8.2 : 1.3)
+                                                                     : (f32 ? 18. : 2.9);
+    const double hbm = 1.0 * seqs * t->Hk * keys(most) * t->d * size_of(t->dtype) / 5.3e6;
+    const double fit = thin ? 768 : 512, together = thin ? 1.25 : f32 ? 1.9 : 1.5;
+    double best = 0;
+    int64_t at = 0;
+    for (int block : {128, 64}) {
+      const int64_t units = (block == 64 ? blocks64 : blocks128) * t->Hk;
+      const int64_t range = keys(std::min<int64_t>(most, block / G + 2));
+      const double tile = alone * (block == 128 ? 1 : thin ? 0.9 : 0.62);
+      for (int64_t s = 1; s <= gdn::MAX_SPLITS; s += s < 4 ? 1 : s / 4) {
+        cut(range, s, step);
+        const double n = (double)units * p.splits;
+        if (at && p.splits > 1 && n > 1.5 * fit) break;  // far more than run at once: no gain
+        const double share = n <= 256 ? 1 : together * (n <= fit ? 1 : n / fit + 0.5);
+        const double us =
+            std::max(p.len / 64.0 * tile * share, hbm) + 5 +
+            (p.splits > 1 ? 5 + 8.0 * p.splits * tok.total * t->Hq * t->d / 8e6 : 0);
+        if (!at || us < best) {
+          best = us;
+          at = s;
+          p.block = block;
+        }
+        if (p.len == step) break;
+      }
+    }
+    cut(keys(std::min<int64_t>(most, p.block / G + 2)), at, step);
     p.slots = tok.cu ? (int)((int64_t)tok.total * G / p.block) + tok.N
                      : tok.N * (int)(((int64_t)tok.T * G + p.block - 1) / p.block);
-    // Splits, by what each number would take: rounds of 512 workgroups, each its
-    // tiles (us for 64 keys, measured alone: bf16 0.7 at d = 64, fp32 6 times that)
-    // and a start of 3 us; and, for more than one, the partial sums' way through
-    // memory and the join's launch (1000 tokens of 16 heads, 4 cache heads: 1 split
-    // 23 us, 3 46; 56 tokens of 32 heads over 95000 keys: 128 us, with 8 splits).
-    const int step = gdn::attn_tile_keys(dt, t->d);
-    const int64_t units = (small ? blocks64 : blocks128) * t->Hk;
-    const int64_t range = keys(std::min<int64_t>(most, p.block / G + 2));
-    const double tile = (dt == Dt::F32 ? 4.2 : 0.7) * t->d / 64 * (small ? 0.6 : 1.0);
-    double best = 0;
-    int64_t at = 1;
-    for (int64_t s = 1; s <= gdn::MAX_SPLITS; s += s < 4 ? 1 : s / 4) {
-      cut(range, s, step);
-      const double us = (double)((units * p.splits + 511) / 512) * (p.len / 64.0 * tile + 3) +
-                        (p.splits > 1 ? 5 + 8.0 * p.splits * tok.total * t->Hq * t->d / 4e6 : 0);
-      if (s == 1 || us < best) {
-        best = us;
-        at = s;
-      }
-      if (p.len == step) break;
-    }
-    cut(range, at, step);
   }
   if ((int64_t)(p.few ? tok.N : p.slots) * p.splits * t->Hk >= (int64_t)1 << 31)
     return GDN_ERR_SHAPE;
