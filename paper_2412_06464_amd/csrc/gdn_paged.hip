@@ -48,7 +48,8 @@ constexpr int ROT_TABLE = 1024;  // angles it holds
 // v) go through it.
 //   WIDE: a unit is one 16-byte piece (interleaved pairs lie inside one) or, in
 //   the layout of halves, the two pieces that hold the two sides of its pairs,
-//   where those start at multiples of 16 bytes; else a unit is one pair.
+//   where those start at multiples of 16 bytes; else a unit is one piece, and the
+//   other side of its pairs is read element by element.
 template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
   constexpr int N = Pc<E>::N;
   __shared__ float2 cs[ROT_TABLE];
@@ -88,38 +89,33 @@ template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(Ro
   __syncthreads();
 
   const bool halves = a.layout == 0;
-  // units of a row that is turned, and those of it that pass unchanged
-  const int turn = WIDE && halves ? half / N : (WIDE ? a.d / N : half);
-  const int rest = WIDE ? (halves ? (a.d - a.rot) / N : 0) : a.d - a.rot;
-  const int units = turn + rest;
+  // units of a row, the first `turn` of them the two sides of pairs
+  const int turn = WIDE && halves ? half / N : 0, units = a.d / N - turn;
 
   // A thread keeps its unit p and steps through the rows (of q and k, or of v) of
   // the workgroup's tokens, four at a time, loaded ahead of their stores (f gets
   // the token and row of each; a token nt or past it: none).
   constexpr int BATCH = 4;
   auto stream = [&](int tid, int H, int per_row, auto&& f) {
-    const int step = max(1, 256 / per_row);  // rows a pass; the threads left over idle
+    const int step = 256 / per_row;  // rows a pass; the threads left over idle
+    const int p = tid % per_row, row = tid / per_row;
+    if (row >= step) return;
     const int dt = step / H, dh = step - dt * H;
-    // (a row of more units than threads: units p, p + 256, ...)
-    for (int p = per_row > 256 ? tid : tid % per_row; p < per_row; p += 256) {
-      const int row = per_row > 256 ? 0 : tid / per_row;
-      if (row >= step) return;
-      int tt = row / H, h = row - tt * H;
-      while (tt < nt) {
-        int ts[BATCH], hs[BATCH];
+    int tt = row / H, h = row - tt * H;
+    while (tt < nt) {
+      int ts[BATCH], hs[BATCH];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-          ts[j] = tt;
-          hs[j] = h;
-          tt += dt;
-          h += dh;
-          if (h >= H) {
-            h -= H;
-            ++tt;
-          }
+      for (int j = 0; j < BATCH; ++j) {
+        ts[j] = tt;
+        hs[j] = h;
+        tt += dt;
+        h += dh;
+        if (h >= H) {
+          h -= H;
+          ++tt;
         }
-        f(ts, hs, p);
       }
+      f(ts, hs, p);
     }
   };
   const int nq = a.q.data ? a.Hq : 0, nk = a.k.data ? a.Hk : 0;
@@ -188,20 +184,41 @@ template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(Ro
               store_piece(r + at1, u);
             }
           }
-      } else {  // halves that do not start at multiples of 16 bytes
+      } else {
+        // halves that do not start at multiples of 16 bytes: a piece of the result, its
+        // partners one by one.  In place this holds because the units of a row lie in
+        // one wave (d / N divides 64), which reads all of it before it writes any.
+        uint4 x[BATCH];
+        E other[BATCH][N];
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+          x[j] = make_uint4(0, 0, 0, 0);
+          if (there(ts[j], hs[j])) {
+            const unsigned char* r = from(ts[j], hs[j]);
+            x[j] = *reinterpret_cast<const uint4*>(r + p * 16);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+              const int c = p * N + e;
+              other[j][e] = c < a.rot
+                                ? reinterpret_cast<const E*>(r)[c < half ? c + half : c - half]
+                                : to_e<E>(0.f);
+            }
+          }
+        }
 #pragma unroll
         for (int j = 0; j < BATCH; ++j)
           if (there(ts[j], hs[j])) {
-            const E* x = reinterpret_cast<const E*>(from(ts[j], hs[j]));
-            E* y = reinterpret_cast<E*>(to(ts[j], hs[j]));
-            if (p < turn) {
-              const float2 c = cs[ts[j] * half + p];
-              const float u1 = to_f(x[p]), u2 = to_f(x[p + half]);
-              y[p] = to_e<E>(u1 * c.x - u2 * c.y);
-              y[p + half] = to_e<E>(u2 * c.x + u1 * c.y);
-            } else {
-              y[half + p] = x[half + p];
+            Pc<E> u = *reinterpret_cast<const Pc<E>*>(&x[j]);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+              const int c = p * N + e;
+              if (c < a.rot) {
+                const float2 w = cs[ts[j] * half + (c < half ? c : c - half)];
+                const float sin = c < half ? -w.y : w.y;
+                u.e[e] = to_e<E>(to_f(u.e[e]) * w.x + to_f(other[j][e]) * sin);
+              }
             }
+            store_piece(to(ts[j], hs[j]) + p * 16, u);
           }
       }
     });
@@ -347,8 +364,23 @@ inline unsigned move_groups(const Pool* p, int64_t n) {
   return (unsigned)std::min<int64_t>(n * p->parts * per, MOVE_GROUPS);
 }
 
+// Block i of row s of the extended table; a new block's page is marked held.
+__device__ inline void extend_block(const Book& b, const PageWork& w, int s, int i) {
+  const int first = w.rank[s], old = blocks_of(w.lens[s], b);
+  const int64_t at = (int64_t)s * b.max_blocks + i;
+  if (first >= 0 && i >= old && i < blocks_of(b.lens_out[s], b)) {
+    const int p = w.dst[first + i - old];
+    b.table_out[at] = p;
+    b.refs_out[p] = 1;
+  } else if (b.table_out != b.table) {
+    b.table_out[at] = b.table[at];
+  }
+}
+
 // rank[s] = the place, among the pages given out, of sequence s's first (-1:
-// it gets none); dst[i] = the i-th free page; refs_out: with those given out.
+// it gets none); dst[i] = the i-th free page; refs_out, lens_out, short_of.
+// ROWS: the table too, where it is small.
+template <bool ROWS>
 __global__ __launch_bounds__(PLAN) void k_extend_plan(Book b, const int32_t* add,
                                                       int32_t* short_of, PageWork w) {
   const int found = ranked(
@@ -386,27 +418,27 @@ __global__ __launch_bounds__(PLAN) void k_extend_plan(Book b, const int32_t* add
     }
     base = min(base, found + 1) + total;
   }
+  if constexpr (ROWS) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < b.S * b.max_blocks; i += PLAN)
+      extend_block(b, w, i / b.max_blocks, i % b.max_blocks);
+  }
 }
 
-// Rows of the table, one workgroup each; the new blocks' pages are marked held.
+// Rows of the table, one workgroup each.
 __global__ __launch_bounds__(256) void k_extend_rows(Book b, PageWork w) {
-  const int s = blockIdx.x, first = w.rank[s], old = blocks_of(w.lens[s], b);
-  const int now = first >= 0 ? blocks_of(b.lens_out[s], b) : old;
-  for (int i = threadIdx.x; i < b.max_blocks; i += 256) {
-    const int64_t at = (int64_t)s * b.max_blocks + i;
-    if (i >= old && i < now) {
-      const int p = w.dst[first + i - old];
-      b.table_out[at] = p;
-      b.refs_out[p] = 1;
-    } else if (b.table_out != b.table) {
-      b.table_out[at] = b.table[at];
-    }
-  }
+  for (int i = threadIdx.x; i < b.max_blocks; i += 256) extend_block(b, w, blockIdx.x, i);
 }
 
 hipError_t launch_extend(const Book& b, const int32_t* add, int32_t* short_of, const PageWork& w,
                          hipStream_t s) {
-  hipLaunchKernelGGL(k_extend_plan, dim3(1), dim3(PLAN), 0, s, b, add, short_of, w);
+  // A small table goes along in the one workgroup, which saves a launch (55 rows of up
+  // to 6 blocks: 13.4 us a call with two, 10.6 with one).
+  if ((int64_t)b.S * b.max_blocks <= 8192) {
+    hipLaunchKernelGGL(k_extend_plan<true>, dim3(1), dim3(PLAN), 0, s, b, add, short_of, w);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(k_extend_plan<false>, dim3(1), dim3(PLAN), 0, s, b, add, short_of, w);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_extend_rows, dim3(b.S), dim3(256), 0, s, b, w);

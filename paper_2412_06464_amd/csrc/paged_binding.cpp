@@ -5,6 +5,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <string.h>
+
 #include <ATen/Functions.h>
 #include <ATen/core/Tensor.h>
 #include <torch/csrc/Exceptions.h>
@@ -139,6 +141,86 @@ PyObject* fresh(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const Tensor* x = tensor("x", args[0]);
   if (!x) return nullptr;
   return THPVariable_Wrap(at::empty(x->sizes(), x->options().requires_grad(false)));
+  END_HANDLE_TH_ERRORS
+}
+
+// book(table, lens, refs, page_size, out or None, with_lens, extra) -> (gdn_book, dict of the
+// outputs: those of `out`, the missing ones new, the pointer of the one named extra, which is
+// shaped as refs ("map") or as lens)
+PyObject* book(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7) return fail(PyExc_TypeError, "book takes 7 arguments");
+  const Tensor* table = tensor("table", args[0]);
+  const Tensor* lens = table ? tensor("lens", args[1]) : nullptr;
+  const Tensor* refs = lens ? tensor("refs", args[2]) : nullptr;
+  if (!refs) return nullptr;
+  const long page_size = PyLong_AsLong(args[3]);
+  const int with_lens = PyObject_IsTrue(args[5]);
+  const char* extra = NAME(6);
+  if (table->dim() != 2) return fail(PyExc_ValueError, "table must be int32 [sequences, blocks]");
+  if (refs->dim() != 1) return fail(PyExc_ValueError, "refs must be int32 [pages]");
+  if (table->get_device() < 0) return fail(PyExc_ValueError, "table must be on the GPU");
+  if (!ints_of("table", *table, *table) || !ints_of("lens", *lens, *table) ||
+      !ints_of("refs", *refs, *table))
+    return nullptr;
+  if (lens->dim() != 1 || lens->size(0) != table->size(0))
+    return fail(PyExc_ValueError, "lens must be int32 [sequences]");
+  const int64_t most = 0x7fffffff;
+  if (table->size(0) > most || table->size(1) > most || refs->size(0) > most ||
+      page_size < INT32_MIN || page_size > most)
+    return fail(PyExc_ValueError, "the table is too large");
+  gdn_book b = {};
+  b.S = (int32_t)table->size(0);
+  b.max_blocks = (int32_t)table->size(1);
+  b.num_pages = (int32_t)refs->size(0);
+  b.page_size = (int32_t)page_size;
+  b.table = table->data_ptr<int32_t>();
+  b.lens = lens->data_ptr<int32_t>();
+  b.refs = refs->data_ptr<int32_t>();
+  PyObject* got = PyDict_New();
+  if (!got) return nullptr;
+  if (args[4] != Py_None && PyDict_Update(got, args[4]) < 0) {
+    Py_DECREF(got);
+    return nullptr;
+  }
+  const Tensor* like_extra = strcmp(extra, "map") == 0 ? refs : lens;
+  struct Out {
+    const char* name;
+    const Tensor* like;
+    int32_t* ptr;
+  } outs[] = {{"table", table, nullptr}, {"refs", refs, nullptr}, {extra, like_extra, nullptr},
+              {"lens", lens, nullptr}};
+  for (int i = 0; i < (with_lens ? 4 : 3); ++i) {
+    Out& o = outs[i];
+    PyObject* have = PyDict_GetItemString(got, o.name);  // borrowed
+    if (!have || have == Py_None) {
+      PyObject* fresh = THPVariable_Wrap(at::empty(o.like->sizes(), o.like->options()));
+      if (!fresh || PyDict_SetItemString(got, o.name, fresh) < 0) {
+        Py_XDECREF(fresh);
+        Py_DECREF(got);
+        return nullptr;
+      }
+      Py_DECREF(fresh);
+      have = fresh;  // held by the dict
+    }
+    const Tensor* x = tensor(o.name, have);
+    if (!x || !ints_of(o.name, *x, *table) || x->sizes() != o.like->sizes()) {
+      if (!PyErr_Occurred()) fail(PyExc_ValueError, "out: %s has the wrong shape", o.name);
+      Py_DECREF(got);
+      return nullptr;
+    }
+    o.ptr = x->data_ptr<int32_t>();
+  }
+  b.table_out = outs[0].ptr;
+  b.refs_out = outs[1].ptr;
+  b.lens_out = outs[3].ptr;
+  PyObject* image = bytes(b);
+  PyObject* ptr = image ? PyLong_FromVoidPtr(outs[2].ptr) : nullptr;
+  PyObject* out = ptr ? PyTuple_Pack(3, image, got, ptr) : nullptr;
+  Py_XDECREF(image);
+  Py_XDECREF(ptr);
+  Py_DECREF(got);
+  return out;
   END_HANDLE_TH_ERRORS
 }
 
@@ -299,6 +381,7 @@ PyMethodDef methods[] = {
     {"rows", (PyCFunction)(void*)rows, METH_FASTCALL, nullptr},
     {"like", (PyCFunction)(void*)like, METH_FASTCALL, nullptr},
     {"fresh", (PyCFunction)(void*)fresh, METH_FASTCALL, nullptr},
+    {"book", (PyCFunction)(void*)book, METH_FASTCALL, nullptr},
     {"pool", (PyCFunction)(void*)pool, METH_FASTCALL, nullptr},
     {"ints", (PyCFunction)(void*)ints, METH_FASTCALL, nullptr},
     {"tokens", (PyCFunction)(void*)tokens, METH_FASTCALL, nullptr},

@@ -142,7 +142,7 @@ class _Helper:
     def __getattr__(self, name):
         mod = _native()
         for f in ("first", "rows", "like", "fresh", "ints", "tokens", "cache", "rotary",
-                  "pool"):
+                  "pool", "book"):
             setattr(self, f, getattr(mod, f))
         return getattr(self, name)
 
@@ -329,38 +329,6 @@ def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True,
 # ------------------------------------------------------------------ pages
 
 
-def _book(table, lens, refs, page_size, out, with_lens, extra):
-    """gdn_book of tensors, the output tensors (``out``: the caller's, where given), the pointer of
-    the one named ``extra`` (shaped as refs: "map", or as lens)."""
-    if not isinstance(table, _Tensor) or table.dim() != 2:
-        raise ValueError("table must be int32 [sequences, blocks]")
-    if not isinstance(refs, _Tensor) or refs.dim() != 1:
-        raise ValueError("refs must be int32 [pages]")
-    if table.get_device() < 0:
-        raise ValueError("table must be on the GPU")
-    S, blocks = table.shape
-    num, ints = refs.shape[0], _n.ints
-    pt, pl = ints("table", table, table), ints("lens", lens, table, S)
-    pr = ints("refs", refs, table)
-    like = refs if extra == "map" else lens
-    if out is None:
-        got = {"table": _n.fresh(table), "refs": _n.fresh(refs),
-               extra: _n.fresh(like)}
-        if with_lens:
-            got["lens"] = _n.fresh(lens)
-    else:
-        got = dict(out)
-        for name, x in (("table", table), ("refs", refs), ("lens", lens if with_lens else None),
-                        (extra, like)):
-            if x is not None and got.get(name) is None:
-                got[name] = _n.fresh(x)
-    b = _BOOK.pack(S, blocks, num, page_size, pt, pl, pr,
-                   ints("out table", got["table"], table, S, blocks),
-                   ints("out lens", got["lens"], table, S) if with_lens else 0,
-                   ints("out refs", got["refs"], table, num))
-    return b, got, ints("out " + extra, got[extra], table, like.shape[0])
-
-
 def _pool(pool, table):
     return None if pool is None else _n.pool(pool, table)
 
@@ -389,7 +357,7 @@ def gdn_pages_extend(table, lens, refs, add, page_size, out=None, workspace=None
     free).  short[s] > 0: there was no room for the pages it needs, and sequence s is as it was.
     ``out``: dict of tensors to write; the inputs themselves update in place."""
     lib = load_library()
-    b, got, short = _book(table, lens, refs, page_size, out, True, "short")
+    b, got, short = _n.book(table, lens, refs, page_size, out, True, "short")
     device = table.device
     ws, p, n = _work(lib, b, workspace, device)
     _check(lib.gdn_pages_extend(b, _n.ints("add", add, table, lens.shape[0]), short, p, n,
@@ -404,7 +372,7 @@ def gdn_pages_select(table, lens, refs, parents, page_size, pool=None, out=None,
     page is copied for every row but the lowest of its parent, in ``pool`` [parts, pages, ...].
     short[i] == 1: no page was left and row i is empty."""
     lib = load_library()
-    b, got, short = _book(table, lens, refs, page_size, out, True, "short")
+    b, got, short = _n.book(table, lens, refs, page_size, out, True, "short")
     device = table.device
     ws, p, n = _work(lib, b, workspace, device)
     _check(lib.gdn_pages_select(b, _n.ints("parents", parents, table, lens.shape[0]),
@@ -416,7 +384,7 @@ def gdn_pages_compact(table, lens, refs, page_size, pool=None, out=None, workspa
     """Moves the pages in use into the lowest indexes: dict table, refs, map (new index of each
     page, -1 if it was free).  The data moves in ``pool`` [parts, pages, ...]."""
     lib = load_library()
-    b, got, to = _book(table, lens, refs, page_size, out, False, "map")
+    b, got, to = _n.book(table, lens, refs, page_size, out, False, "map")
     device = table.device
     ws, p, n = _work(lib, b, workspace, device)
     _check(lib.gdn_pages_compact(b, _pool(pool, table), to, p, n, _stream(device)))
