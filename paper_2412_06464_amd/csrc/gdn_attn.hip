@@ -599,6 +599,63 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
   attn_block<E, D, QT, 1, KW, KT>(a, b, split, smem);
 }
 
+// The row block that comes at `rank` when all sequences' blocks are ordered by the
+// keys they see, longest first, for at most 64 sequences: a lane holds one.  Block
+// t of a sequence whose first new token has `base` row blocks' worth of keys before
+// it sees depth = min(base + t, cap) of them, so count(K), the blocks with
+// depth >= K, is a sum over the sequences, and the block at `rank` has the largest K
+// with count(K) > rank: 64 values of K are tried at a time, one a lane.  False past
+// the last block.
+__device__ inline bool longest_first(const AttnArgs& a, int R, int rank, int* seq, int* tile) {
+  const int lane = lane_id(), N = a.tok.N;
+  int base = 0, blocks = 0;
+  if (lane < N) {
+    const int m = seq_start(a.tok, lane + 1) - seq_start(a.tok, lane);
+    base = (int)min((int64_t)1 << 29, (int64_t)max(0, cached(a.cache, lane) - m) * a.G / R);
+    blocks = (int)(((int64_t)m * a.G + R - 1) / R);
+  }
+  const int cap = a.window > 0 ? (int)min((int64_t)1 << 30, (int64_t)a.window * a.G / R + 1) : 1 << 30;
+  int top = 0, total = 0;
+#pragma unroll 1
+  for (int n = 0; n < N; ++n) {
+    const int bn = __builtin_amdgcn_readlane(base, n), tn = __builtin_amdgcn_readlane(blocks, n);
+    top = max(top, bn + tn);
+    total += tn;
+  }
+  if (rank >= total) return false;
+  int k = 0, next = 0;  // count(k) > rank; next: count(k + 1)
+  int step = min(top, cap + 1) / 63 + 1;
+  for (;;) {
+    const int K = k + lane * step;
+    int count = 0;
+#pragma unroll 1
+    for (int n = 0; n < N; ++n) {
+      const int bn = __builtin_amdgcn_readlane(base, n), tn = __builtin_amdgcn_readlane(blocks, n);
+      count += max(0, tn - max(0, K - bn));
+    }
+    if (K > cap) count = 0;
+    const int at = 63 - __clzll(__ballot(count > rank));
+    k += at * step;
+    next = __builtin_amdgcn_readlane(count, at + 1);
+    if (step == 1) break;
+    step = (step + 62) / 63;
+  }
+  // of the blocks with depth k, the one at rank - next
+  int j = rank - next;
+  const int mine = max(0, blocks - max(0, k - base)) - (k < cap ? max(0, blocks - max(0, k + 1 - base)) : 0);
+#pragma unroll 1
+  for (int n = 0; n < N; ++n) {
+    const int x = __builtin_amdgcn_readlane(mine, n);
+    if (j < x) {
+      *seq = n;
+      *tile = k < cap ? k - __builtin_amdgcn_readlane(base, n) : __builtin_amdgcn_readlane(blocks, n) - 1 - j;
+      return true;
+    }
+    j -= x;
+  }
+  return false;
+}
+
 // Many rows.  Grid: ((slot * splits + split) * Hk + hk); the sequence and row
 // block of a slot follow from the boundaries: sequence n's slots begin at
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
@@ -612,22 +669,26 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
   Block b;
   b.hk = blockIdx.x % a.Hk;
   const int rest = blockIdx.x / a.Hk, split = rest % a.splits;
-  // the last row blocks see the most keys: they go first
-  const int slot = slots - 1 - rest / a.splits;
   int tile;
-  if (a.tok.cu) {
-    const int64_t G = a.G;
-    int lo = 0, hi = a.tok.N;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if ((int)(a.tok.cu[mid] * G / R) + mid <= slot) lo = mid; else hi = mid;
-    }
-    b.n = lo;
-    tile = slot - ((int)(a.tok.cu[lo] * G / R) + lo);
+  if (a.longest) {
+    if (!longest_first(a, R, rest / a.splits, &b.n, &tile)) return;
   } else {
-    const int per = (int)(((int64_t)a.tok.T * a.G + R - 1) / R);
-    b.n = slot / per;
-    tile = slot - b.n * per;
+    // the last row blocks of a sequence see the most keys: they go first
+    const int slot = slots - 1 - rest / a.splits;
+    if (a.tok.cu) {
+      const int64_t G = a.G;
+      int lo = 0, hi = a.tok.N;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((int)(a.tok.cu[mid] * G / R) + mid <= slot) lo = mid; else hi = mid;
+      }
+      b.n = lo;
+      tile = slot - ((int)(a.tok.cu[lo] * G / R) + lo);
+    } else {
+      const int per = (int)(((int64_t)a.tok.T * a.G + R - 1) / R);
+      b.n = slot / per;
+      tile = slot - b.n * per;
+    }
   }
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;

@@ -134,6 +134,7 @@ struct Plan {
   bool few = false;
   int block = 0, slots = 0;    // rows of a block; blocks of the tile kernel's grid
   int splits = 1, len = 0;     // key ranges
+  bool longest = false;        // longest row blocks of all sequences first
   size_t part = 0, bytes = 0;  // workspace: offset of {maximum, sum}; size
 };
 
@@ -236,6 +237,14 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
       }
     }
     cut(keys(std::min<int64_t>(most, p.block / G + 2)), at, step);
+    // Several sequences' blocks that do not all run at once start in the order of their
+    // keys, or a long one begins when most of the GPU is done: 8 prompts in a 2K
+    // window, d = 256, 166 us, in the sequences' order 205; 60 sequences of up to 300
+    // tokens over up to 3000 keys 110 and 143; 8 of 2048 tokens 158 and 174 (2 of 4000
+    // 140 and 135).  The bf16 blocks of d = 64 are too short for the search that finds
+    // each its place (40 sequences in a window of 512: 66 and 59).
+    p.longest = a->causal && !thin && tok.N > 1 && tok.N <= 64 &&
+                (p.block == 64 ? blocks64 : blocks128) * t->Hk * p.splits > fit;
     p.slots = tok.cu ? (int)((int64_t)tok.total * G / p.block) + tok.N
                      : tok.N * (int)(((int64_t)tok.T * G + p.block - 1) / p.block);
   }
@@ -429,6 +438,7 @@ gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_row
   a.block = p.block;
   a.splits = p.splits;
   a.len = p.len;
+  a.longest = p.longest;
   hipError_t e = p.few ? gdn::launch_attn_few(dt, t->d, a, s)
                        : gdn::launch_attn_tile(dt, t->d, p.slots, a, s);
   if (e == hipSuccess && p.splits > 1) e = gdn::launch_attn_join(dt, t->d, a, s);

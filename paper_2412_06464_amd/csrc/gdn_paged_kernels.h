@@ -53,6 +53,7 @@ struct AttnArgs {
   float c;          // scale * log2(e)
   int block;        // rows of a block
   int splits, len;  // key ranges of `len` keys (the last: all that follow)
+  int longest;      // row blocks of all sequences in the order of their keys
 };
 // Calls whose sequences have at most this many rows (new tokens x query heads of a
 // cache head) take the kernel whose waves share the rows and split the keys.
