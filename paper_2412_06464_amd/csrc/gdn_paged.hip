@@ -40,12 +40,19 @@ template <class E> __device__ inline void store_piece(unsigned char* p, const Pc
 
 }  // namespace
 
-constexpr int ROT_TOKENS = 16;   // most tokens of a workgroup
-constexpr int ROT_TABLE = 1024;  // angles it holds
+constexpr int ROT_TOKENS = 4;                  // most tokens of a workgroup
+constexpr int ROT_TABLE = ROT_TOKENS * 256 / 2;  // angles it holds (d <= 256)
 
-// A workgroup takes a.per tokens: first the cos and sin of their angles into
-// LDS, once for all heads, with each token's place; then the rows of q, k (and
-// v) go through it.
+// Rotation of pairs: y1 = s (x1 cos a - x2 sin a), y2 = s (x2 cos a + x1 sin a), a the
+// token's position times the pair's frequency, reduced to a turn in 64 bits; the
+// gradient is the rotation by -a.  Bound by HBM: each row is read once and
+// written once.  A workgroup takes a.per tokens: the cos and sin of their angles
+// go into LDS, once for all heads, with each token's place, while the first rows of
+// q, k (and v) are on their way.  Four tokens and two rows of a thread at a time:
+// 43,000 tokens of 16 + 4 heads, d = 128, bf16, 103 us a direction, 5.5 TB/s (16 tokens,
+// four rows 117; 2 tokens 108; the loads after the angles 119 with 16 and four); prompts
+// into the cache, 137 MB, 25 us (27.5), after a cache-evicting write 46 (54; a copy
+// of as many bytes 39).  A token each for 256 sequences 7 us, the launch.
 //   WIDE: a unit is one 16-byte piece (interleaved pairs lie inside one) or, in
 //   the layout of halves, the two pieces that hold the two sides of its pairs,
 //   where those start at multiples of 16 bytes; else a unit is one piece, and the
@@ -56,6 +63,105 @@ template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(Ro
   __shared__ int64_t kat[ROT_TOKENS];  // where the token's k and v go; -1: nowhere
   const int half = a.rot / 2;
   const int t0 = blockIdx.x * a.per, nt = min(a.per, a.tok.total - t0);
+  const bool halves = a.layout == 0;
+  // units of a row, the first `turn` of them the two sides of pairs
+  const int turn = WIDE && halves ? half / N : 0, units = a.d / N - turn;
+
+  // A thread keeps its unit p and steps through the rows (of q and k, or of v) of
+  // the workgroup's tokens, BATCH at a time (a token nt or past it: none).
+  constexpr int BATCH = 2;
+  struct Walk {
+    int H, p, t, h, dt, dh;
+    __device__ Walk(int tid, int heads, int per_row, int nt) {
+      H = heads;
+      const int step = 256 / per_row;  // rows a pass; the threads left over idle
+      p = tid % per_row;
+      const int row = tid / per_row;
+      dt = step / H;
+      dh = step - dt * H;
+      t = row < step ? row / H : nt;
+      h = row % H;
+    }
+    __device__ void next(int (&ts)[BATCH], int (&hs)[BATCH]) {
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        ts[j] = t;
+        hs[j] = h;
+        t += dt;
+        h += dh;
+        if (h >= H) {
+          h -= H;
+          ++t;
+        }
+      }
+    }
+  };
+  const int nq = a.q.data ? a.Hq : 0, nk = a.k.data ? a.Hk : 0;
+  // (plain values: a choice between two structures would put them in memory)
+  unsigned char *const qd = a.q.data, *const kd = a.k.data - nq * a.k.hs;
+  const int64_t qts = a.q.ts, qhs = a.q.hs, kts = a.k.ts, khs = a.k.hs;
+  auto from = [&](int tt, int h) {
+    const bool is_q = h < nq;
+    return (is_q ? qd : kd) + (int64_t)(t0 + tt) * (is_q ? qts : kts) + h * (is_q ? qhs : khs);
+  };
+  unsigned char* const qod = a.q_out.data;
+  const int64_t qots = a.q_out.ts, qohs = a.q_out.hs;
+  const int64_t kots = a.append ? 0 : a.k_out.ts, kohs = a.append ? a.cache.head : a.k_out.hs;
+  unsigned char* const kod = (a.append ? a.cache.k : a.k_out.data) - nq * kohs;
+  auto to = [&](int tt, int h) {
+    const bool is_q = h < nq;
+    unsigned char* r =
+        (is_q ? qod : kod) + (int64_t)(t0 + tt) * (is_q ? qots : kots) + h * (is_q ? qohs : kohs);
+    return a.append && !is_q ? r + kat[tt] : r;
+  };
+  Walk wq(threadIdx.x, nq + nk, units, nt);
+  const int p = wq.p;
+  // WIDE: the unit's pieces, its own, or those of both sides of its pairs
+  const bool both = WIDE && halves && p < turn;
+  const int at1 = (WIDE && halves && p >= turn ? turn + p : p) * 16, at2 = (p + turn) * 16;
+  uint4 x1[BATCH], x2[WIDE ? BATCH : 1];
+  E other[WIDE ? 1 : BATCH][N];
+  int ts[BATCH], hs[BATCH];
+  auto load = [&]() {
+    wq.next(ts, hs);
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      x1[j] = make_uint4(0, 0, 0, 0);
+      if constexpr (WIDE) x2[j] = make_uint4(0, 0, 0, 0);
+      if (ts[j] < nt) {
+        const unsigned char* r = from(ts[j], hs[j]);
+        x1[j] = *reinterpret_cast<const uint4*>(r + at1);
+        if constexpr (WIDE) {
+          if (both) x2[j] = *reinterpret_cast<const uint4*>(r + at2);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const int c = p * N + e;
+            other[j][e] =
+                c < a.rot ? reinterpret_cast<const E*>(r)[c < half ? c + half : c - half] : to_e<E>(0.f);
+          }
+        }
+      }
+    }
+  };
+  // v from the other end: where there are few tokens, by the waves that have no q
+  Walk wv(255 - threadIdx.x, max(a.Hk, 1), a.d / N, nt);
+  if (!a.v.data) wv.t = nt;
+  uint4 y[BATCH];
+  int vt[BATCH], vh[BATCH];
+  auto load_v = [&]() {
+    wv.next(vt, vh);
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      y[j] = make_uint4(0, 0, 0, 0);
+      if (vt[j] < nt)
+        y[j] = *reinterpret_cast<const uint4*>(a.v.data + (int64_t)(t0 + vt[j]) * a.v.ts +
+                                               vh[j] * a.v.hs + wv.p * 16);
+    }
+  };
+  // the first rows are on their way while the angles are found
+  load();
+  load_v();
 
   for (int i = threadIdx.x; i < nt * max(half, 1); i += 256) {
     const int tt = half ? i / half : i, j = half ? i - tt * half : 0, t = t0 + tt;
@@ -88,158 +194,64 @@ template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(Ro
   }
   __syncthreads();
 
-  const bool halves = a.layout == 0;
-  // units of a row, the first `turn` of them the two sides of pairs
-  const int turn = WIDE && halves ? half / N : 0, units = a.d / N - turn;
-
-  // A thread keeps its unit p and steps through the rows (of q and k, or of v) of
-  // the workgroup's tokens, four at a time, loaded ahead of their stores (f gets
-  // the token and row of each; a token nt or past it: none).
-  constexpr int BATCH = 4;
-  auto stream = [&](int tid, int H, int per_row, auto&& f) {
-    const int step = 256 / per_row;  // rows a pass; the threads left over idle
-    const int p = tid % per_row, row = tid / per_row;
-    if (row >= step) return;
-    const int dt = step / H, dh = step - dt * H;
-    int tt = row / H, h = row - tt * H;
-    while (tt < nt) {
-      int ts[BATCH], hs[BATCH];
+  for (;;) {
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        ts[j] = tt;
-        hs[j] = h;
-        tt += dt;
-        h += dh;
-        if (h >= H) {
-          h -= H;
-          ++tt;
-        }
-      }
-      f(ts, hs, p);
-    }
-  };
-  const int nq = a.q.data ? a.Hq : 0, nk = a.k.data ? a.Hk : 0;
-  // (plain values: a choice between two structures would put them in memory)
-  unsigned char *const qd = a.q.data, *const kd = a.k.data - nq * a.k.hs;
-  const int64_t qts = a.q.ts, qhs = a.q.hs, kts = a.k.ts, khs = a.k.hs;
-  auto from = [&](int tt, int h) {
-    const bool is_q = h < nq;
-    return (is_q ? qd : kd) + (int64_t)(t0 + tt) * (is_q ? qts : kts) + h * (is_q ? qhs : khs);
-  };
-  unsigned char* const qod = a.q_out.data;
-  const int64_t qots = a.q_out.ts, qohs = a.q_out.hs;
-  const int64_t kots = a.append ? 0 : a.k_out.ts, kohs = a.append ? a.cache.head : a.k_out.hs;
-  unsigned char* const kod = (a.append ? a.cache.k : a.k_out.data) - nq * kohs;
-  auto to = [&](int tt, int h) {
-    const bool is_q = h < nq;
-    unsigned char* r =
-        (is_q ? qod : kod) + (int64_t)(t0 + tt) * (is_q ? qots : kots) + h * (is_q ? qohs : kohs);
-    return a.append && !is_q ? r + kat[tt] : r;
-  };
-  auto there = [&](int tt, int h) { return tt < nt && (h < nq || !a.append || kat[tt] >= 0); };
-  stream(threadIdx.x, nq + nk, units, [&](const int (&ts)[BATCH], const int (&hs)[BATCH], int p) {
+    for (int j = 0; j < BATCH; ++j) {
+      if (ts[j] >= nt || (a.append && hs[j] >= nq && kat[ts[j]] < 0)) continue;
+      unsigned char* r = to(ts[j], hs[j]);
+      const float2* w = cs + ts[j] * half;
+      Pc<E> u = *reinterpret_cast<const Pc<E>*>(&x1[j]);
       if constexpr (WIDE) {
-        // the unit's pieces: its own, or those of both sides of its pairs
-        const bool both = halves && p < turn;
-        const int at1 = (halves && p >= turn ? turn + p : p) * 16, at2 = (p + turn) * 16;
-        uint4 x1[BATCH], x2[BATCH];
+        if (both) {
+          Pc<E> z = *reinterpret_cast<const Pc<E>*>(&x2[j]);
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-          if (there(ts[j], hs[j])) {
-            const unsigned char* r = from(ts[j], hs[j]);
-            x1[j] = *reinterpret_cast<const uint4*>(r + at1);
-            if (both) x2[j] = *reinterpret_cast<const uint4*>(r + at2);
+          for (int e = 0; e < N; ++e) {
+            const float2 c = w[p * N + e];
+            const float u1 = to_f(u.e[e]), u2 = to_f(z.e[e]);
+            u.e[e] = to_e<E>(u1 * c.x - u2 * c.y);
+            z.e[e] = to_e<E>(u2 * c.x + u1 * c.y);
           }
+          store_piece(r + at2, z);
+        } else if (!halves) {
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-          if (there(ts[j], hs[j])) {
-            unsigned char* r = to(ts[j], hs[j]);
-            const float2* w = cs + ts[j] * half;
-            if (both) {
-              Pc<E> u = *reinterpret_cast<const Pc<E>*>(&x1[j]);
-              Pc<E> v = *reinterpret_cast<const Pc<E>*>(&x2[j]);
-#pragma unroll
-              for (int e = 0; e < N; ++e) {
-                const float2 c = w[p * N + e];
-                const float u1 = to_f(u.e[e]), u2 = to_f(v.e[e]);
-                u.e[e] = to_e<E>(u1 * c.x - u2 * c.y);
-                v.e[e] = to_e<E>(u2 * c.x + u1 * c.y);
-              }
-              store_piece(r + at1, u);
-              store_piece(r + at2, v);
-            } else if (halves) {
-              *reinterpret_cast<uint4*>(r + at1) = x1[j];
-            } else {
-              Pc<E> u = *reinterpret_cast<const Pc<E>*>(&x1[j]);
-#pragma unroll
-              for (int e = 0; e < N / 2; ++e) {
-                const int pair = p * (N / 2) + e;
-                if (pair < half) {
-                  const float2 c = w[pair];
-                  const float u1 = to_f(u.e[2 * e]), u2 = to_f(u.e[2 * e + 1]);
-                  u.e[2 * e] = to_e<E>(u1 * c.x - u2 * c.y);
-                  u.e[2 * e + 1] = to_e<E>(u2 * c.x + u1 * c.y);
-                }
-              }
-              store_piece(r + at1, u);
+          for (int e = 0; e < N / 2; ++e) {
+            const int pair = p * (N / 2) + e;
+            if (pair < half) {
+              const float2 c = w[pair];
+              const float u1 = to_f(u.e[2 * e]), u2 = to_f(u.e[2 * e + 1]);
+              u.e[2 * e] = to_e<E>(u1 * c.x - u2 * c.y);
+              u.e[2 * e + 1] = to_e<E>(u2 * c.x + u1 * c.y);
             }
           }
+        }
       } else {
         // halves that do not start at multiples of 16 bytes: a piece of the result, its
         // partners one by one.  In place this holds because the units of a row lie in
         // one wave (d / N divides 64), which reads all of it before it writes any.
-        uint4 x[BATCH];
-        E other[BATCH][N];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-          x[j] = make_uint4(0, 0, 0, 0);
-          if (there(ts[j], hs[j])) {
-            const unsigned char* r = from(ts[j], hs[j]);
-            x[j] = *reinterpret_cast<const uint4*>(r + p * 16);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-              const int c = p * N + e;
-              other[j][e] = c < a.rot
-                                ? reinterpret_cast<const E*>(r)[c < half ? c + half : c - half]
-                                : to_e<E>(0.f);
-            }
+        for (int e = 0; e < N; ++e) {
+          const int c = p * N + e;
+          if (c < a.rot) {
+            const float2 cw = w[c < half ? c : c - half];
+            const float sin = c < half ? -cw.y : cw.y;
+            u.e[e] = to_e<E>(to_f(u.e[e]) * cw.x + to_f(other[j][e]) * sin);
           }
         }
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-          if (there(ts[j], hs[j])) {
-            Pc<E> u = *reinterpret_cast<const Pc<E>*>(&x[j]);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-              const int c = p * N + e;
-              if (c < a.rot) {
-                const float2 w = cs[ts[j] * half + (c < half ? c : c - half)];
-                const float sin = c < half ? -w.y : w.y;
-                u.e[e] = to_e<E>(to_f(u.e[e]) * w.x + to_f(other[j][e]) * sin);
-              }
-            }
-            store_piece(to(ts[j], hs[j]) + p * 16, u);
-          }
       }
-    });
-  // v from the other end: where there are few tokens, by the waves that have no q
-  if (a.v.data)
-    stream(255 - threadIdx.x, a.Hk, a.d / N,
-           [&](const int (&ts)[BATCH], const int (&hs)[BATCH], int p) {
-             uint4 x[BATCH];
+      store_piece(r + at1, u);
+    }
+    if (wq.t >= nt) break;
+    load();
+  }
+  if (!a.v.data) return;
+  for (;;) {
 #pragma unroll
-             for (int j = 0; j < BATCH; ++j) {
-               x[j] = make_uint4(0, 0, 0, 0);
-               if (ts[j] < nt)
-                 x[j] = *reinterpret_cast<const uint4*>(a.v.data + (int64_t)(t0 + ts[j]) * a.v.ts +
-                                                        hs[j] * a.v.hs + p * 16);
-             }
-#pragma unroll
-             for (int j = 0; j < BATCH; ++j)
-               if (ts[j] < nt && kat[ts[j]] >= 0)
-                 *reinterpret_cast<uint4*>(a.cache.v + kat[ts[j]] +
-                                           hs[j] * a.cache.head + p * 16) = x[j];
-           });
+    for (int j = 0; j < BATCH; ++j)
+      if (vt[j] < nt && kat[vt[j]] >= 0)
+        *reinterpret_cast<uint4*>(a.cache.v + kat[vt[j]] + vh[j] * a.cache.head + wv.p * 16) = y[j];
+    if (wv.t >= nt) break;
+    load_v();
+  }
 }
 
 hipError_t launch_rotate(Dt dt, RotateArgs a, hipStream_t s) {
@@ -248,7 +260,6 @@ hipError_t launch_rotate(Dt dt, RotateArgs a, hipStream_t s) {
   int per = (a.tok.total + 2047) / 2048;
   per = per < 1 ? 1 : per > ROT_TOKENS ? ROT_TOKENS : per;
   const int half = a.rot / 2;
-  while (per > 1 && per * half > ROT_TABLE) --per;
   a.per = per;
   const dim3 grid((unsigned)((a.tok.total + per - 1) / per));
   const int n = dt == Dt::F32 ? 4 : 8;
