@@ -131,7 +131,8 @@ __device__ inline float col_sum(float x) {
 
 // The running maximum follows only when a score passes it by this much (in
 // base 2): p stays below 2^8, which costs no accuracy (p, l and o keep their
-// relative precision), and o is rescaled a few times instead of in most tiles.
+// relative precision), and o is rescaled a few times instead of in most tiles
+// (a prompt of 8192 tokens, d = 128: 275 us, with 0 304).
 constexpr float SLACK = 8.f;
 
 template <class E, int D, int QT, int RW, int KW, int KT>
@@ -142,8 +143,9 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   constexpr int NK = C::NK, NT = NK / 16, RB = C::RB, NP = C::NP, KB = RB / 64, DT = D / 16;
   constexpr int GROUPS = KT / 16;
   // Where two waves share a SIMD, the one in its products goes first: the other
-  // fills in with its softmax (a prompt of 8192 tokens at d = 128: 282 -> 266 us).
-  constexpr bool PRIO = KW == 1 && RB <= 512;
+  // fills in with its softmax (a prompt of 8192 tokens, d = 128: 275 us, without 290;
+  // 2048 in fp32 272 and 280; in bf16 with three waves, d = 64, 174 and 166, so not there).
+  constexpr bool PRIO = KW == 1 && RB >= 256 && RB <= 512;
   constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;  // groups this wave copies
   const int lane = lane_id(), g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -577,7 +579,10 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   }
 }
 
-// Few rows: one row block per sequence and cache head, its keys split.
+// Few rows: one row block per sequence and cache head, its keys split.  Bound by HBM,
+// each key read once for all heads that share it, with two buffers of a CU's whole LDS
+// in flight: a token each for 256 sequences in a 2K window (797 MB) 149 us, 5.3 TB/s; two
+// with 131072 keys (537 MB) 95 us, 5.6 TB/s; four with 1000 keys 8.5 us, latency.
 // Grid: ((n * splits + split) * Hk + hk).
 template <class E, int D, int QT, int KW, int KT>
 __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
@@ -656,7 +661,12 @@ __device__ inline bool longest_first(const AttnArgs& a, int R, int rank, int* se
   return false;
 }
 
-// Many rows.  Grid: ((slot * splits + split) * Hk + hk); the sequence and row
+// Many rows: 4 d flop for a row and a key it sees.  Bound by the matrix cores and the
+// exponentials of the softmax in turn, one workgroup's beside the other's.  A prompt
+// of 8192 tokens of 16 heads, 4 cache heads, bf16: 166 us at d = 64 (828 TFLOP/s), 271 at
+// 128 (1,015), 539 at 256 (1,020); two of 2048 in fp32, 8 heads, 272 at d = 128 (63), where
+// the longest blocks end last.
+// Grid: ((slot * splits + split) * Hk + hk); the sequence and row
 // block of a slot follow from the boundaries: sequence n's slots begin at
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
 // the next one's.
@@ -667,8 +677,13 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
   constexpr int R = C::ROWS;
   __shared__ __align__(1024) unsigned char smem[C::LDS];
   Block b;
-  b.hk = blockIdx.x % a.Hk;
-  const int rest = blockIdx.x / a.Hk, split = rest % a.splits;
+  // A second workgroup for some CUs, but no third for any: they come in reverse, the
+  // shortest beside the longest (a prompt of 4096 tokens, 16 heads, d = 128: 107 us, in
+  // order 113; of 2048 in fp32, 8 heads, d = 64: 57 and 79).
+  const int id =
+      gridDim.x > 512 || blockIdx.x < 256 ? blockIdx.x : 255 + gridDim.x - blockIdx.x;
+  b.hk = id % a.Hk;
+  const int rest = id / a.Hk, split = rest % a.splits;
   int tile;
   if (a.longest) {
     if (!longest_first(a, R, rest / a.splits, &b.n, &tile)) return;
@@ -702,11 +717,12 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
   attn_block<E, D, QT, 4, 1, KT>(a, b, split, smem);
 }
 
-// Joins the splits' sums of a row by T threads: they turn the splits' maxima into
-// weights, then T / (D / 4) groups of them add up the weighted sums of every so
-// many-th split, four loads in flight each.  T = 256 where a row has many splits;
-// T = D / 4, so several rows to a workgroup and no exchange between threads, where it
-// has few (16000 rows of 3 splits: 25 us with 256 threads a row).
+// Joins the splits' sums of a row by T threads: they turn the splits' maxima m_s into
+// weights 2^(m_s - max m), then T / (D / 4) groups of them add up the weighted sums of
+// every so many-th split, four loads in flight each.  Latency, or HBM where there are
+// many rows.  T = 256 where a row has many splits (32 rows of 32: 5.0 us); T = D / 4, so
+// several rows to a workgroup and no exchange between threads, where it has few (64
+// rows of 8: 3.0 us; 16000 rows of 3 splits: 25 us with 256 threads a row).
 template <class E, int D, int T> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   constexpr int TPR = D / 4, NG = T / TPR, PER = 256 / T;
   const int64_t rows = (int64_t)a.tok.total * a.Hq;
@@ -807,8 +823,8 @@ namespace {
 // of k and v (most bytes in flight), four waves where that leaves each a group
 // of 16.  The other: as many as let two workgroups share a CU (64 KB of buffers),
 // so that one's products run beside the other's softmax: at d = 256 in bf16 32
-// keys, prompts in a 2K window 284 us, with 64 and one workgroup 317; at d = 64 in bf16
-// 64 keys leave room for three or four (a prompt of 8192 tokens 170 us, with 128 205).
+// keys, prompts in a 2K window 166 us, with 64 and one workgroup 237; at d = 64 in bf16
+// 64 keys leave room for three or four (a prompt of 8192 tokens 174 us, with 128 197).
 template <class E, int D> struct Few {
   static constexpr int RB = D * (int)sizeof(E);
   static constexpr int KW = RB >= 1024 ? 2 : 4;
