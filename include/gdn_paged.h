@@ -57,7 +57,8 @@ typedef struct {
   int64_t page_stride, head_stride, token_stride; /* elements, of both       */
   int32_t num_pages;    /* >= 1                                              */
   int32_t page_size;    /* a power of two, 16 to 1024                        */
-  int32_t max_blocks;   /* columns of table, >= 1                            */
+  int32_t max_blocks;   /* columns of table, >= 1; times page_size at most
+                         * 2^31 - 2^18                                       */
   const int32_t *table;   /* device int32[N, max_blocks]                     */
   const int32_t *kv_lens; /* device int32[N]: tokens of each sequence, those
                            * of the call included                            */

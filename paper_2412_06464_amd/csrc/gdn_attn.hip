@@ -51,7 +51,8 @@ struct Block {
   int lo;             // seen, down to a multiple of 16
   // first and one past the last key that token i sees
   __device__ int first(const AttnArgs& a, int i) const {
-    return a.window > 0 ? max(0, kv - m + i - a.window + 1) : 0;
+    // (a token before the cache's first sees nothing; its place may not pass 32 bits)
+    return a.window > 0 ? max(0, max(0, kv - m + i + 1) - a.window) : 0;
   }
   __device__ int last(const AttnArgs& a, int i) const {
     return a.causal ? max(0, kv - m + i + 1) : kv;

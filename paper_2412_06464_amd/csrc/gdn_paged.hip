@@ -49,7 +49,7 @@ constexpr int ROT_TABLE = ROT_TOKENS * 256 / 2;  // angles it holds (d <= 256)
 // written once.  A workgroup takes a.per tokens: the cos and sin of their angles
 // go into LDS, once for all heads, with each token's place, while the first rows of
 // q, k (and v) are on their way.  Four tokens and two rows of a thread at a time:
-// 43,000 tokens of 16 + 4 heads, d = 128, bf16, 103 us a direction, 5.5 TB/s (16 tokens,
+// 55,700 tokens of 16 + 4 heads, d = 128, bf16, 103 us a direction, 5.5 TB/s (16 tokens,
 // four rows 117; 2 tokens 108; the loads after the angles 119 with 16 and four); prompts
 // into the cache, 137 MB, 25 us (27.5), after a cache-evicting write 46 (54; a copy
 // of as many bytes 39).  A token each for 256 sequences 7 us, the launch.

@@ -67,7 +67,8 @@ gdn_status check_cache(const gdn_cache* c, int esz, bool pointers, gdn::Cache* o
   if (c->num_pages < 1 || c->max_blocks < 1 || c->page_size < 16 || c->page_size > 1024 ||
       (c->page_size & (c->page_size - 1)))
     return GDN_ERR_SHAPE;
-  if ((int64_t)c->max_blocks * c->page_size >= (int64_t)1 << 31) return GDN_ERR_SHAPE;
+  // the kernels look a few tiles past a range of keys, and ranges are whole tiles
+  if ((int64_t)c->max_blocks * c->page_size > ((int64_t)1 << 31) - (1 << 18)) return GDN_ERR_SHAPE;
   if (pointers) {
     if (!c->k || !c->v || !c->table || !c->kv_lens) return GDN_ERR_NULL;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->table, 4) ||

@@ -181,3 +181,14 @@ def test_binding_refusals(P):
                 dict(q_out=torch.empty_like(q)[:, :1]), dict(k_out=k.float())):
         with pytest.raises((ValueError, TypeError, RuntimeError)):
             P.gdn_rotary_fwd(q, k, r, **bad)
+
+
+@pytest.mark.parametrize("new,kv", [([40, 3], [25, 90]), ([200], [150])])
+def test_widest_window(P, new, kv):
+    """A window that no cache reaches is no window, also for tokens before the cache's first."""
+    c = Case(new, kv, 4, 2, 128, 16, BF, 0, seed=5)
+    want, lse = run(P, c)
+    check(c, want, lse)
+    c.window = 2 ** 31 - 1
+    got, again = run(P, c)
+    check(c, got, again)

@@ -292,3 +292,14 @@ def test_binding_refuses_cpu_tensors_and_mismatches():
     with pytest.raises(ValueError, match="GPU"):
         paged.gdn_pages_extend(*[torch.zeros(s, dtype=torch.int32) for s in ((2, 3), (2,), (5,))],
                                add=None, page_size=16)
+
+
+def test_longest_cache(lib):
+    """Key positions stay clear of 32 bits: 2^31 - 2^18 tokens of room are the most."""
+    t, a = tokens(), attn(max_kv=1000)
+    most = (2 ** 31 - 2 ** 18) // 16
+    for blocks, code in ((most, ALIGN), (most + 1, SHAPE), (2 ** 27 - 1, SHAPE)):
+        c = cache(page_size=16, max_blocks=blocks)
+        q = rows(ODD)  # what is checked next
+        assert lib.gdn_cache_attn(ref(t), ref(a), ref(q), ref(c), ref(q), None, None, 0,
+                                  None) == code
