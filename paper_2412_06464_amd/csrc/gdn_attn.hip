@@ -145,7 +145,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   constexpr int GROUPS = KT / 16;
   // Where two waves share a SIMD, the one in its products goes first: the other
   // fills in with its softmax (a prompt of 8192 tokens, d = 128: 275 us, without 290;
-  // 2048 in fp32 272 and 280; in bf16 with three waves, d = 64, 174 and 166, so not there).
+  // with three waves, bf16 at d = 64, 174 and 166, so not there).
   constexpr bool PRIO = KW == 1 && RB >= 256 && RB <= 512;
   constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;  // groups this wave copies
   const int lane = lane_id(), g = lane >> 4, c16 = lane & 15;
@@ -665,8 +665,7 @@ __device__ inline bool longest_first(const AttnArgs& a, int R, int rank, int* se
 // Many rows: 4 d flop for a row and a key it sees.  Bound by the matrix cores and the
 // exponentials of the softmax in turn, one workgroup's beside the other's.  A prompt
 // of 8192 tokens of 16 heads, 4 cache heads, bf16: 166 us at d = 64 (828 TFLOP/s), 271 at
-// 128 (1,015), 539 at 256 (1,020); two of 2048 in fp32, 8 heads, 272 at d = 128 (63), where
-// the longest blocks end last.
+// 128 (1,015), 539 at 256 (1,020); two of 2048 in fp32, 8 heads, 166 at d = 128 (104).
 // Grid: ((slot * splits + split) * Hk + hk); the sequence and row
 // block of a slot follow from the boundaries: sequence n's slots begin at
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before

@@ -215,6 +215,14 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
                                                                      : (f32 ? 18. : 2.9);
     const double hbm = 1.0 * seqs * t->Hk * keys(most) * t->d * size_of(t->dtype) / 5.3e6;
     const double fit = thin ? 768 : 512, together = thin ? 1.25 : f32 ? 1.9 : 1.5;
+    // In fp32 the matrix cores alone bind, so a block is slow beside a second one only as
+    // long as that lasts.  Where the new tokens are much of the keys and sequences are
+    // alike, the longest block has the shortest beside it, of `least` of its keys (two
+    // prompts of 2048 tokens, 8 heads, 4 cache heads, d = 128: 164 us, without this term,
+    // in 128 rows, 276; 5 of up to 900 85 and 137; one of 2000, 16 heads 159 and 269).  In
+    // bf16 it would choose 64 rows where 128 are better (d = 256, 4096 tokens: 162 and 141).
+    const bool pairs = f32 && a->causal && a->window == 0 && 2 * (int64_t)tok.total >= seqs * most;
+    const double least = std::max(0., 1 - (double)most / kv);
     double best = 0;
     int64_t at = 0;
     for (int block : {128, 64}) {
@@ -225,7 +233,9 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
         cut(range, s, step);
         const double n = (double)units * p.splits;
         if (at && p.splits > 1 && n > 1.5 * fit) break;  // far more than run at once: no gain
-        const double share = n <= 256 ? 1 : together * (n <= fit ? 1 : n / fit + 0.5);
+        double share = n <= 256 ? 1 : together * (n <= fit ? 1 : n / fit + 0.5);
+        if (pairs && n > 256 && n <= 512 && p.splits == 1)
+          share = std::max(1 + (together - 1) * least, together * (1 + least) / 2);
         const double us =
             std::max(p.len / 64.0 * tile * share, hbm) + 5 +
             (p.splits > 1 ? 5 + 8.0 * p.splits * tok.total * t->Hq * t->d / 8e6 : 0);
