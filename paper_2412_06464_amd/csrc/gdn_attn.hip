@@ -71,7 +71,9 @@ template <class E, int D, int QT, int RW, int KW, int KT> struct AttnCfg {
   static constexpr int NP = RB / 16;                // 16-byte pieces of it
   static constexpr int ROWS = RW * QT * 16;
   static constexpr int TILE = KT * RB;              // bytes of a tile of k (or v)
-  static constexpr int JOIN = KW > 1 ? KW * ROWS * (D + 2) * 4 : 0;
+  // rows of the waves' sums, 4 banks apart: 16 of them are written at a time
+  static constexpr int JR = D + 4;
+  static constexpr int JOIN = KW > 1 ? KW * ROWS * (JR + 2) * 4 : 0;
   static constexpr int LDS = 4 * TILE > JOIN ? 4 * TILE : JOIN;
   static constexpr int RPI = 64 / NP;               // keys of one wave-wide copy
   static_assert(NK % 16 == 0 && KT % 16 == 0, "a wave works on whole groups of 16 keys");
@@ -499,16 +501,16 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
     }
   } else {
     // join the waves' sums in LDS
-    constexpr int R = C::ROWS;
+    constexpr int R = C::ROWS, JR = C::JR;
     float* sum = reinterpret_cast<float*>(smem);
-    float* ml = sum + KW * R * D;
+    float* ml = sum + KW * R * JR;
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
       const int r = u * 16 + c16;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<f32x4*>(sum + ((kw * R + r) * D + 16 * d + 4 * g)) = o[d][u];
+        *reinterpret_cast<f32x4*>(sum + ((kw * R + r) * JR + 16 * d + 4 * g)) = o[d][u];
       if (g == 0) {
         ml[(kw * R + r) * 2] = m[u];
         ml[(kw * R + r) * 2 + 1] = l[u];
@@ -526,7 +528,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const float al = __builtin_amdgcn_exp2f(ml[(w * R + r) * 2] - ref);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(sum + ((w * R + r) * D + ch));
+        const f32x4 y = *reinterpret_cast<const f32x4*>(sum + ((w * R + r) * JR + ch));
         ll += al * ml[(w * R + r) * 2 + 1];
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] += al * y[e];
