@@ -584,8 +584,8 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
 
 // Few rows: one row block per sequence and cache head, its keys split.  Bound by HBM,
 // each key read once for all heads that share it, with two buffers of a CU's whole LDS
-// in flight: a token each for 256 sequences in a 2K window (797 MB) 149 us, 5.3 TB/s; two
-// with 131072 keys (537 MB) 95 us, 5.6 TB/s; four with 1000 keys 8.5 us, latency.
+// in flight: a token each for 256 sequences in a 2K window (797 MB) 147 us, 5.4 TB/s; two
+// with 131072 keys (537 MB) 95 us, 5.6 TB/s; four with 1000 keys 7.2 us, latency.
 // Grid: ((n * splits + split) * Hk + hk).
 template <class E, int D, int QT, int KW, int KT>
 __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
@@ -666,8 +666,8 @@ __device__ inline bool longest_first(const AttnArgs& a, int R, int rank, int* se
 
 // Many rows: 4 d flop for a row and a key it sees.  Bound by the matrix cores and the
 // exponentials of the softmax in turn, one workgroup's beside the other's.  A prompt
-// of 8192 tokens of 16 heads, 4 cache heads, bf16: 166 us at d = 64 (828 TFLOP/s), 271 at
-// 128 (1,015), 539 at 256 (1,020); two of 2048 in fp32, 8 heads, 166 at d = 128 (104).
+// of 8192 tokens of 16 heads, 4 cache heads, bf16: 165 us at d = 64 (834 TFLOP/s), 269 at
+// 128 (1,020), 531 at 256 (1,036); two of 2048 in fp32, 8 heads, 159 at d = 128 (108).
 // Grid: ((slot * splits + split) * Hk + hk); the sequence and row
 // block of a slot follow from the boundaries: sequence n's slots begin at
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
