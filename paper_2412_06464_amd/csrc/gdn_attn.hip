@@ -37,7 +37,8 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 // at lds + lane * 16; base and lds are the same for the whole wave.  As
 // dma_frag: the caller waits.
 __device__ inline void dma_rows(const unsigned char* base, unsigned off, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
+               "v"(off), "s"(base)
                : "memory");
 }
 

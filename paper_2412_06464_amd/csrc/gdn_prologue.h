@@ -129,8 +129,8 @@ __device__ inline void pro_warm(const E* X, int D, int H, int h, int start, int 
   for (int i = tid; i < n; i += nth) {
     const int r = i / lpr;
     const unsigned off = (unsigned)r * rowb + (unsigned)(i - r * lpr) * 128u;
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off),
-                 "s"(base)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds),
+                 "v"(off), "s"(base)
                  : "memory");
   }
 }

@@ -39,8 +39,8 @@ __device__ inline void warm_l2(const unsigned char* const (&base)[NB], const int
 #pragma unroll
   for (int b = 0; b < NB; ++b)
     if (idx < bytes[b] / WL)
-      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off),
-                   "s"(base[b])
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds),
+                   "v"(off), "s"(base[b])
                    : "memory");
 }
 
