@@ -130,8 +130,12 @@ gdn_status gdn_cache_append(const gdn_tokens *t, const gdn_rotary *r, const gdn_
  * (causal only) also j > its position - window.  Query head h reads cache head
  * h / (Hq / Hk).  A token that sees nothing gets o = 0 and lse = -infinity.
  * What is not seen has no influence, whatever bits it holds (infinities and
- * NaN among them).  Scores, the softmax and the sums over keys are in 32 bits;
- * in bfloat16 problems p is rounded to bfloat16 for its product with v.
+ * NaN among them).  Scores, the softmax and the sums over keys are in 32 bits.
+ * In bfloat16 problems p is rounded to bfloat16 for its product with v (2^-8 of
+ * each p v at most; over many keys about as much as the rounding of o); where
+ * every sequence has few rows (new tokens x Hq / Hk at most 32; not in batches of
+ * over 256 sequences x Hk with at most 1024 keys), it enters as two bfloat16
+ * values (2^-16).
  *   lse      fp32 [B * T, Hq] or NULL: log of the sum of exp(scale q k)
  *   max_kv   how many tokens kv_lens is expected to hold at most: the launches
  *            are sized by it (a longer cache costs time, not results); 0:

@@ -150,6 +150,14 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   // fills in with its softmax (a prompt of 8192 tokens, d = 128: 275 us, without 290;
   // with three waves, bf16 at d = 64, 174 and 166, so not there).
   constexpr bool PRIO = KW == 1 && RB >= 256 && RB <= 512;
+  // The bf16 values that stand for a weight p in its product with v.  Two (p's rounding, and
+  // what that left over: 2^-16 of p is lost) make o exact but for its own rounding; one
+  // leaves its error, against 64 bits, at 1.3 to 1.4 times that.  With few rows the keys'
+  // way from HBM hides the second product (256 single tokens in a 2K window 147.2 us, with
+  // one 147.4; two with 131072 keys 96.7 and 96.6; 8 tokens a sequence, up to 4000 keys,
+  // 55.3 and 55.8).  With many it is matrix cores' time that binds (a prompt of 8192 tokens
+  // 345 us, with one 269; d = 64 245 and 165; prompts in a 2K window, d = 256, 201 and 164).
+  constexpr int PARTS = KW == 1 ? 1 : 2;
   constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;  // groups this wave copies
   const int lane = lane_id(), g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -354,45 +362,58 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
             for (int u = 0; u < QT; ++u) o[d][u] = Mfma<float>::mma(x, s[t][u][e], o[d][u]);
           }
     } else {
-      // p is rounded to bf16 for this product alone; l sums it unrounded.
+      // l sums p in fp32; here it is an operand in bf16 (see PARTS)
       // Lane i of 16 points at 4 channels of key row i / 4 and receives one
       // channel (its own, i) of the 4 rows.
       auto turned = [&](int t, int d) {
         return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (LDS_AS s16x4*)((vaddr ^ (d << 5)) + t * 16 * RB));
       };
+      auto part = [&](int i, float p) {
+        const bf16 hi = (bf16)p;
+        return i == 0 ? hi : (bf16)(p - (float)hi);
+      };
       if constexpr (NT == 1) {
-        s16x4 p[QT];
+        s16x4 p[QT][PARTS];
 #pragma unroll
-        for (int u = 0; u < QT; ++u) {
-          const bf16x4 x = {(bf16)s[0][u][0], (bf16)s[0][u][1], (bf16)s[0][u][2], (bf16)s[0][u][3]};
-          p[u] = *reinterpret_cast<const s16x4*>(&x);
-        }
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int i = 0; i < PARTS; ++i) {
+            const bf16x4 x = {part(i, s[0][u][0]), part(i, s[0][u][1]), part(i, s[0][u][2]),
+                              part(i, s[0][u][3])};
+            p[u][i] = *reinterpret_cast<const s16x4*>(&x);
+          }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const s16x4 x = turned(0, d);
 #pragma unroll
-          for (int u = 0; u < QT; ++u)
-            o[d][u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p[u], o[d][u], 0, 0, 0);
+          for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+              o[d][u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p[u][i], o[d][u], 0, 0, 0);
         }
       } else {
 #pragma unroll
         for (int t = 0; t < NT; t += 2) {
-          bf16x8 p[QT];
+          bf16x8 p[QT][PARTS];
 #pragma unroll
           for (int u = 0; u < QT; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              p[u][e] = (bf16)s[t][u][e];
-              p[u][4 + e] = (bf16)s[t + 1][u][e];
-            }
+            for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                p[u][i][e] = part(i, s[t][u][e]);
+                p[u][i][4 + e] = part(i, s[t + 1][u][e]);
+              }
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             const s16x4 x0 = turned(t, d), x1 = turned(t + 1, d);
             const s16x8 x = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-            for (int u = 0; u < QT; ++u)
-              o[d][u] = Mfma<bf16>::mma(*reinterpret_cast<const bf16x8*>(&x), p[u], o[d][u]);
+            for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+              for (int u = 0; u < QT; ++u)
+                o[d][u] = Mfma<bf16>::mma(*reinterpret_cast<const bf16x8*>(&x), p[u][i], o[d][u]);
           }
         }
       }
