@@ -764,7 +764,8 @@ template <class E, int D, int T> __global__ __launch_bounds__(256) void k_attn_j
   b.r1 = (int)min(all, (int64_t)b.r0 + a.block);
   b.kv = cached(a.cache, b.n);
   b.range(a);
-  const int live = min(a.splits, max(1, (b.hi - b.lo + a.len - 1) / a.len));
+  // (as a quotient that stays within 32 bits at the longest caches)
+  const int live = b.hi > b.lo ? min(a.splits, (b.hi - b.lo - 1) / a.len + 1) : 1;
 
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
   float mx = -INFINITY, ll = 0.f;
