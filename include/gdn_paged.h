@@ -22,7 +22,18 @@
  * its keys, nothing is stored there and nothing of it is read, so pages that
  * have left a window can be freed and their entries set to -1.  kv_lens and
  * table live in device memory and are read when the kernels run; values
- * outside [0, max_blocks * page_size] are taken as the nearest bound.
+ * outside [0, max_blocks * page_size] are taken as the nearest bound, so a
+ * longer length would put new tokens over the last ones: lengths come from
+ * gdn_pages_extend, which does not let them pass the table's room.
+ *
+ * Where pages may run out, skip (or NULL) is the short_of of the
+ * gdn_pages_extend before: a sequence with a non-zero entry there did not get
+ * the room for the call's tokens, its kv_lens does not count them, and the
+ * places that its length gives them are those of older tokens, perhaps in
+ * pages that other sequences share.  It is taken as one that holds no tokens:
+ * nothing of it is stored, its tokens see nothing (o = 0, lse = -infinity) and
+ * its queries are rotated as the tokens before position 0.  Without skip, the
+ * caller has to see to it that no such sequence is in the call.
  *
  * Alignment.  Device pointers are 16-byte aligned and every row (a head of a
  * token, a slot of a page) starts at a multiple of 16 bytes (GDN_ERR_ALIGN).
@@ -62,6 +73,7 @@ typedef struct {
   const int32_t *table;   /* device int32[N, max_blocks]                     */
   const int32_t *kv_lens; /* device int32[N]: tokens of each sequence, those
                            * of the call included                            */
+  const int32_t *skip;    /* device int32[N] or NULL: sequences to leave alone */
 } gdn_cache;
 
 /* ---- rotary positions
@@ -191,7 +203,9 @@ size_t gdn_pages_workspace_size(const gdn_book *b);
  * was free, or whose blocks exceed max_blocks, keeps its row and length and
  * gets short_of[s] = the new pages it asked for (0: served).  Sequences past
  * max_blocks take no pages from those behind them; those that need no new
- * page are always served. */
+ * page are always served.  The cache calls that follow take short_of as the
+ * cache's skip, or leave the refused sequences out: what they stored for them
+ * would go over older tokens. */
 gdn_status gdn_pages_extend(const gdn_book *b, const int32_t *add, int32_t *short_of,
                             void *workspace, size_t workspace_bytes, void *stream);
 

@@ -72,7 +72,7 @@ gdn_status check_cache(const gdn_cache* c, int esz, bool pointers, gdn::Cache* o
   if (pointers) {
     if (!c->k || !c->v || !c->table || !c->kv_lens) return GDN_ERR_NULL;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->table, 4) ||
-        !aligned(c->kv_lens, 4) || c->page_stride * esz % 16 || c->head_stride * esz % 16 ||
+        !aligned(c->kv_lens, 4) || !aligned(c->skip, 4) || c->page_stride * esz % 16 || c->head_stride * esz % 16 ||
         c->token_stride * esz % 16)
       return GDN_ERR_ALIGN;
     if (c->token_stride < 0 || c->token_stride * esz >= MAX_STRIDE) return GDN_ERR_SHAPE;
@@ -84,6 +84,7 @@ gdn_status check_cache(const gdn_cache* c, int esz, bool pointers, gdn::Cache* o
   out->slot = c->token_stride * esz;
   out->table = c->table;
   out->lens = c->kv_lens;
+  out->skip = c->skip;
   out->num_pages = c->num_pages;
   out->shift = 0;
   while ((1 << out->shift) < c->page_size) ++out->shift;

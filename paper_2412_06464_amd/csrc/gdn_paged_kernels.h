@@ -26,6 +26,7 @@ struct Cache {
   int64_t page, head, slot;  // strides in bytes
   const int32_t* table;      // [N, max_blocks]
   const int32_t* lens;       // [N]
+  const int32_t* skip;       // [N] or nullptr: non-zero: taken as holding no tokens
   int num_pages, shift, max_blocks;  // page_size = 1 << shift
 };
 
@@ -115,6 +116,7 @@ __device__ inline int seq_of(const Tokens& k, int t) {
 __device__ inline int seq_start(const Tokens& k, int n) { return k.cu ? k.cu[n] : n * k.T; }
 // Tokens a sequence holds in the cache, within what its row of the table can.
 __device__ inline int cached(const Cache& c, int n) {
+  if (c.skip && c.skip[n] != 0) return 0;
   const int64_t most = (int64_t)c.max_blocks << c.shift;
   const int x = c.lens[n];
   return x < 0 ? 0 : (x > most ? (int)most : x);

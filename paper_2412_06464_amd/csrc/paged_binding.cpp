@@ -305,10 +305,11 @@ PyObject* tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// cache(first's name, first, k_pages, v_pages, table, kv_lens or None, sequences) -> gdn_cache
+// cache(first's name, first, k_pages, v_pages, table, kv_lens or None, sequences, skip or None) ->
+// gdn_cache
 PyObject* cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 7) return fail(PyExc_TypeError, "cache takes 7 arguments");
+  if (n != 8) return fail(PyExc_TypeError, "cache takes 8 arguments");
   const char* other = NAME(0);
   const Tensor* x = tensor(other, args[1]);
   const Tensor* k = x ? tensor("k_pages", args[2]) : nullptr;
@@ -343,13 +344,19 @@ PyObject* cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
   c.page_size = (int32_t)k->size(2);
   c.max_blocks = (int32_t)table->size(1);
   c.table = table->data_ptr<int32_t>();
-  if (args[5] != Py_None) {
-    const Tensor* lens = tensor("kv_lens", args[5]);
-    if (!lens || !ints_of("kv_lens", *lens, *x)) return nullptr;
-    if (lens->dim() != 1 || lens->size(0) != seqs)
-      return PyErr_Format(PyExc_ValueError, "kv_lens must be int32 [%lld sequences]",
+  const struct {
+    const char* name;
+    PyObject* arg;
+    const int32_t** to;
+  } per_seq[] = {{"kv_lens", args[5], &c.kv_lens}, {"skip", args[7], &c.skip}};
+  for (const auto& p : per_seq) {
+    if (p.arg == Py_None) continue;
+    const Tensor* y = tensor(p.name, p.arg);
+    if (!y || !ints_of(p.name, *y, *x)) return nullptr;
+    if (y->dim() != 1 || y->size(0) != seqs)
+      return PyErr_Format(PyExc_ValueError, "%s must be int32 [%lld sequences]", p.name,
                           (long long)seqs);
-    c.kv_lens = lens->data_ptr<int32_t>();
+    *p.to = y->data_ptr<int32_t>();
   }
   return bytes(c);
   END_HANDLE_TH_ERRORS

@@ -50,7 +50,7 @@ class Cache(ctypes.Structure):
                 ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("max_blocks", ctypes.c_int32), ("table", ctypes.c_void_p),
-                ("kv_lens", ctypes.c_void_p)]
+                ("kv_lens", ctypes.c_void_p), ("skip", ctypes.c_void_p)]
 
 
 class RotaryStruct(ctypes.Structure):
@@ -242,12 +242,15 @@ def gdn_rotary_bwd(dq_out, dk_out, rotary, positions=None, cu_seqlens=None, cu_s
 
 
 def gdn_cache_append(q, k, v, k_pages, v_pages, table, kv_lens, rotary=None, cu_seqlens=None,
-                     cu_seqlens_host=None, q_out=None):
+                     cu_seqlens_host=None, q_out=None, skip=None):
     """Stores the new tokens' k (rotated) and v in their sequences' pages; returns q, rotated.
 
     q [B, T, Hq, d] or None, k and v [B, T, Hk, d]; table int32 [sequences, blocks], kv_lens int32
     [sequences]: the tokens of each sequence with the new ones, which are its last.  ``rotary``
-    None: nothing is rotated.  Tokens whose page is a hole are not stored."""
+    None: nothing is rotated.  Tokens whose page is a hole are not stored.  ``skip`` int32
+    [sequences]: the ``short`` of the gdn_pages_extend before; nothing is stored for a sequence with
+    a non-zero entry.  Without it, a sequence that was refused room must not be in the call: its
+    new tokens would go over its last ones, in pages that others may share."""
     lib = load_library()
     keep = []
     rk = _n.first("k", k)
@@ -260,7 +263,7 @@ def gdn_cache_append(q, k, v, k_pages, v_pages, table, kv_lens, rotary=None, cu_
         else:
             ro = _n.rows("q_out", q_out, "k", k, Hq)
     n = B if cu_seqlens is None else cu_seqlens.shape[0] - 1
-    c = _n.cache("k", k, k_pages, v_pages, table, kv_lens, n)
+    c = _n.cache("k", k, k_pages, v_pages, table, kv_lens, n, skip)
     if k_pages.shape[1] != Hk:
         raise ValueError("k_pages must have k's heads")
     t = _tokens(k, Hq, Hk, cu_seqlens, cu_seqlens_host, dev, keep)
@@ -281,7 +284,7 @@ def gdn_cache_attn_workspace_size(q, k_pages, table, scale=None, causal=True, wi
     _n.first("q", q)
     B, _, Hq, d = q.shape
     n = B if cu_seqlens is None else cu_seqlens.shape[0] - 1
-    c = _n.cache("q", q, k_pages, k_pages, table, None, n)
+    c = _n.cache("q", q, k_pages, k_pages, table, None, n, None)
     t = _tokens(q, Hq, k_pages.shape[1], cu_seqlens, cu_seqlens_host, q.device, keep)
     return int(load_library().gdn_cache_attn_workspace_size(t, c, _attn(scale, d, causal, window,
                                                                         max_kv)))
@@ -289,21 +292,22 @@ def gdn_cache_attn_workspace_size(q, k_pages, table, scale=None, causal=True, wi
 
 def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True, window=0,
                    max_kv=0, cu_seqlens=None, cu_seqlens_host=None, o=None, lse=None,
-                   workspace=None):
+                   workspace=None, skip=None):
     """Attention of the new tokens q [B, T, Hq, d] over their sequences' cached keys; returns o.
 
     The new tokens are the last of the kv_lens[n] that sequence n holds (gdn_cache_append has
     stored them).  ``scale`` None: 1 / sqrt(d); ``window`` > 0: a token sees itself and the window - 1
     before it; ``max_kv``: how long a sequence may be at most (0: what the table has room for),
     which the launches are sized by.  ``lse`` float32 [B, T, Hq] receives the log of each softmax's
-    sum.  A token that sees no key gets 0 (lse -inf)."""
+    sum.  A token that sees no key gets 0 (lse -inf), and so do those of a sequence with a non-zero
+    entry in ``skip`` (as in gdn_cache_append)."""
     lib = load_library()
     keep = []
     rq = _n.first("q", q)
     B, T, Hq, d = q.shape
     dev = q.device
     n = B if cu_seqlens is None else cu_seqlens.shape[0] - 1
-    c = _n.cache("q", q, k_pages, v_pages, table, kv_lens, n)
+    c = _n.cache("q", q, k_pages, v_pages, table, kv_lens, n, skip)
     t = _tokens(q, Hq, k_pages.shape[1], cu_seqlens, cu_seqlens_host, dev, keep)
     if o is None:
         o, ro = _n.like(q)
@@ -354,7 +358,8 @@ def gdn_pages_extend(table, lens, refs, add, page_size, out=None, workspace=None
     """Room for add[s] more tokens in each sequence: dict table, lens, refs, short.
 
     table int32 [S, blocks], lens and add int32 [S], refs int32 [pages] (holders of each page; 0:
-    free).  short[s] > 0: there was no room for the pages it needs, and sequence s is as it was.
+    free).  short[s] > 0: there was no room for the pages it needs, and sequence s is as it was: pass
+    ``short`` on as ``skip`` of the calls on the cache, or leave such sequences out of them.
     ``out``: dict of tensors to write; the inputs themselves update in place."""
     lib = load_library()
     b, got, short = _n.book(table, lens, refs, page_size, out, True, "short")
