@@ -82,9 +82,12 @@ class Server:
         self.lens = out.get("lens", self.lens)
 
     def _grow(self, add):
+        """Pages for add[s] more tokens a row; if they do not last, nothing has changed."""
         out = paged.gdn_pages_extend(self.table, self.lens, self.refs, add, page_size=self.page)
+        short = torch.nonzero(out["short"])[:, 0].tolist()
+        if short:
+            raise RuntimeError("no pages left for rows %s" % short)
         self._book(out)
-        return out["short"]
 
     def _state(self, layer):
         return self.states[layer, self.side * self.S:(self.side + 1) * self.S]
@@ -112,7 +115,7 @@ class Server:
         rows' logits after their last tokens.  Rows that had tokens go on from them."""
         m = self.m
         n = torch.tensor([len(p) for p in prompts], dtype=torch.int32)
-        assert not self._grow(n.to(m.device)).any(), "no pages left"
+        self._grow(n.to(m.device))
         host = torch.cat([torch.zeros(1, dtype=torch.int32), n.cumsum(0).to(torch.int32)])
         cu = dict(cu_seqlens=host.to(m.device), cu_seqlens_host=host)
         ids = torch.tensor([t for p in prompts for t in p], device=m.device)
@@ -128,7 +131,7 @@ class Server:
     def decode(self, ids):
         """One token a row (ids [S], a row without a sequence takes one too); logits [S, vocab]."""
         m = self.m
-        assert not self._grow(torch.ones_like(self.lens)).any(), "no pages left"
+        self._grow(torch.ones_like(self.lens))
 
         def rule(i, x):
             state = self._state(i)
