@@ -89,6 +89,16 @@ class Server:
             raise RuntimeError("no pages left for rows %s" % short)
         self._book(out)
 
+    def _release(self):
+        """Drops the pages that lie whole before every later token's window: their entries become
+        holes, which later calls neither read nor store to.  On the device, with no copy back."""
+        first = self.lens + 1 - self.m.window  # the first key that a row's next token sees
+        end = torch.arange(1, self.blocks + 1, dtype=torch.int32, device=first.device) * self.page
+        gone = (self.table >= 0) & (end <= first[:, None])
+        page = self.table.clamp(min=0).flatten().long()
+        self.refs = self.refs.scatter_add(0, page, -gone.flatten().to(torch.int32))
+        self.table = torch.where(gone, -1, self.table)
+
     def _state(self, layer):
         return self.states[layer, self.side * self.S:(self.side + 1) * self.S]
 
@@ -108,6 +118,7 @@ class Server:
             o = paged.gdn_cache_attn(q, k_pages, v_pages, self.table, self.lens, window=m.window,
                                      **cu)
             x = x + o.flatten(2) @ w["out"]
+        self._release()
         return m.norm(x).to(m.dtype) @ m.head
 
     def prefill(self, prompts):

@@ -35,3 +35,25 @@ def test_no_pages_left(server, monkeypatch, call):
     with pytest.raises(RuntimeError, match=r"no pages left for rows \[1\]"):
         call(server)
     assert all(torch.equal(x, y) for x, y in zip(before, (server.table, server.lens, server.refs)))
+
+
+def test_pages_behind_the_window_are_released(server):
+    """A page goes when its last token is one that no row's next token sees; shared ones when
+    their last holder lets go; holes stay holes."""
+    P = server.page
+    server.table[0, :4] = torch.tensor([7, 3, 9, 5])
+    server.table[1, :4] = torch.tensor([7, 3, -1, 2])
+    server.table[2, :2] = torch.tensor([7, 1])
+    server.lens = torch.tensor([4 * P, 4 * P - 9, P + 1], dtype=torch.int32)
+    server.refs[torch.tensor([7, 3, 9, 5, 2, 1])] = torch.tensor([3, 2, 1, 1, 1, 1],
+                                                                 dtype=torch.int32)
+    # the next tokens, at 64, 55 and 17, see from 25, 16 and 0 on
+    server._release()
+    assert server.table[:, :5].tolist() == [[-1, 3, 9, 5, -1], [-1, 3, -1, 2, -1], [7, 1, -1, -1, -1]]
+    assert [server.refs[p].item() for p in (7, 3, 9, 5, 2, 1)] == [1, 2, 1, 1, 1, 1]
+    server.lens[:2] += torch.tensor([7, 16], dtype=torch.int32)  # see from 32 on
+    server._release()
+    assert server.table[:, :5].tolist() == [[-1, -1, 9, 5, -1], [-1, -1, -1, 2, -1],
+                                            [7, 1, -1, -1, -1]]
+    assert [server.refs[p].item() for p in (7, 3, 9, 5, 2, 1)] == [1, 0, 1, 1, 1, 1]
+    assert server.refs.dtype is torch.int32 and server.table.dtype is torch.int32
