@@ -38,14 +38,26 @@ def _compile(src: str, obj: str, extra=()) -> None:
         raise RuntimeError("hipcc failed for %s:\n%s%s" % (src, r.stdout, r.stderr))
 
 
+class MissingTool(RuntimeError):
+    """What the Python side is built with is not there; the C library does not need it."""
+
+
 def build_binding(out: str = BINDING) -> str:
-    """Compile the tensor checks of the attention layer's binding (host code, torch's headers)."""
+    """Compile the tensor checks of the attention layer's binding (host code, torch's headers).
+    MissingTool: torch or the host compiler is not there."""
+    import shutil
     import sysconfig
 
-    import torch
-    from torch.utils import cpp_extension
+    cxx = os.environ.get("CXX", "g++")
+    if shutil.which(cxx.split()[0]) is None:
+        raise MissingTool("no C++ compiler (%s)" % cxx)
+    try:
+        import torch
+        from torch.utils import cpp_extension
+    except ImportError as e:
+        raise MissingTool("no torch (%s)" % e) from e
     tmp = out + ".tmp%d" % os.getpid()
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+    cmd = [*cxx.split(), "-O2", "-std=c++17", "-shared", "-fPIC",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
            *["-I" + d for d in cpp_extension.include_paths()],
            "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "paged_binding.cpp"),
@@ -59,7 +71,9 @@ def build_binding(out: str = BINDING) -> str:
 
 
 def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
-    """Compile every source for gfx950 and link ``out``.  ``defines`` are
+    """Compile every source for gfx950 and link ``out``; with the default ``out``
+    also the binding helper, whose failure is raised once the library is there (and
+    only reported where torch or a C++ compiler is missing).  ``defines`` are
     extra -D flags (tuning experiments; the defaults are the product)."""
     extra = ["-D" + d for d in defines]
     tag = "_".join(d.replace("=", "") for d in defines)
@@ -69,8 +83,6 @@ def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     with cf.ThreadPoolExecutor(len(SOURCES) + 1) as ex:
         binding = ex.submit(build_binding) if out == LIB else None
         list(ex.map(lambda a: _compile(*a, extra), zip(SOURCES, objs)))
-        if binding:
-            binding.result()
     LIBOUT = out
     tmp = LIBOUT + ".tmp%d" % os.getpid()
     cmd = [HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC", *objs, "-o", tmp]
@@ -80,6 +92,12 @@ def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     os.replace(tmp, LIBOUT)
     if verbose:
         print("built", LIBOUT)
+    if binding:
+        try:
+            binding.result()
+        except MissingTool as e:
+            # a C caller's build: the library is whole, and paged.py says what it lacks
+            print("not built: %s: %s" % (BINDING, e), file=sys.stderr)
     return LIBOUT
 
 
