@@ -134,16 +134,6 @@ PyObject* like(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// fresh(x) -> a new contiguous tensor of x's shape, type and device
-PyObject* fresh(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  HANDLE_TH_ERRORS
-  if (n != 1) return fail(PyExc_TypeError, "fresh takes 1 argument");
-  const Tensor* x = tensor("x", args[0]);
-  if (!x) return nullptr;
-  return THPVariable_Wrap(at::empty(x->sizes(), x->options().requires_grad(false)));
-  END_HANDLE_TH_ERRORS
-}
-
 // book(table, lens, refs, page_size, out or None, with_lens, extra) -> (gdn_book, dict of the
 // outputs: those of `out`, the missing ones new, the pointer of the one named extra, which is
 // shaped as refs ("map") or as lens)
@@ -387,7 +377,6 @@ PyMethodDef methods[] = {
     {"first", (PyCFunction)(void*)first, METH_FASTCALL, nullptr},
     {"rows", (PyCFunction)(void*)rows, METH_FASTCALL, nullptr},
     {"like", (PyCFunction)(void*)like, METH_FASTCALL, nullptr},
-    {"fresh", (PyCFunction)(void*)fresh, METH_FASTCALL, nullptr},
     {"book", (PyCFunction)(void*)book, METH_FASTCALL, nullptr},
     {"pool", (PyCFunction)(void*)pool, METH_FASTCALL, nullptr},
     {"ints", (PyCFunction)(void*)ints, METH_FASTCALL, nullptr},

@@ -141,8 +141,7 @@ class _Helper:
 
     def __getattr__(self, name):
         mod = _native()
-        for f in ("first", "rows", "like", "fresh", "ints", "tokens", "cache", "rotary",
-                  "pool", "book"):
+        for f in ("first", "rows", "like", "ints", "tokens", "cache", "rotary", "pool", "book"):
             setattr(self, f, getattr(mod, f))
         return getattr(self, name)
 
