@@ -153,6 +153,9 @@ gdn_status gdn_cache_append(const gdn_tokens *t, const gdn_rotary *r, const gdn_
  *            are sized by it (a longer cache costs time, not results); 0:
  *            max_blocks * page_size
  *   scale    > 0, finite
+ * A launch holds less than 2^24 workgroups (GDN_ERR_SHAPE past that): one for
+ * each sequence and cache head and one for each 64 rows (new tokens x Hq), at
+ * most; keys are split only where those are few.
  * The workspace (gdn_cache_attn_workspace_size bytes, 0 where none is needed)
  * holds partial results of keys split over several workgroups.  The same call
  * gives the same bits. */

@@ -62,7 +62,9 @@ template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(Ro
   __shared__ float2 cs[ROT_TABLE];
   __shared__ int64_t kat[ROT_TOKENS];  // where the token's k and v go; -1: nowhere
   const int half = a.rot / 2;
-  const int t0 = blockIdx.x * a.per, nt = min(a.per, a.tok.total - t0);
+  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.per;
+  if (first >= a.tok.total) return;  // the last row of a grid of several
+  const int t0 = (int)first, nt = min(a.per, a.tok.total - t0);
   const bool halves = a.layout == 0;
   // units of a row, the first `turn` of them the two sides of pairs
   const int turn = WIDE && halves ? half / N : 0, units = a.d / N - turn;
@@ -261,7 +263,10 @@ hipError_t launch_rotate(Dt dt, RotateArgs a, hipStream_t s) {
   per = per < 1 ? 1 : per > ROT_TOKENS ? ROT_TOKENS : per;
   const int half = a.rot / 2;
   a.per = per;
-  const dim3 grid((unsigned)((a.tok.total + per - 1) / per));
+  // (a launch holds less than 2^32 threads in one direction)
+  const int64_t groups = ((int64_t)a.tok.total + per - 1) / per, wide_grid = (int64_t)1 << 22;
+  const dim3 grid((unsigned)std::min(groups, wide_grid),
+                  (unsigned)((groups + wide_grid - 1) / wide_grid));
   const int n = dt == Dt::F32 ? 4 : 8;
   const bool wide = a.layout == 1 || half % n == 0;
   auto go = [&](auto e) {

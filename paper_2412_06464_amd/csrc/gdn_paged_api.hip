@@ -134,7 +134,8 @@ gdn_status rotate(const gdn_tokens* t, const gdn_rotary* r, const gdn_rows* q, c
 // How a call's work is cut: which kernel, its row blocks, splits of their keys.
 struct Plan {
   bool few = false;
-  int block = 0, slots = 0;    // rows of a block; blocks of the tile kernel's grid
+  int block = 0;               // rows of a block
+  int64_t slots = 0;           // blocks of the tile kernel's grid
   int splits = 1, len = 0;     // key ranges
   bool longest = false;        // longest row blocks of all sequences first
   size_t part = 0, bytes = 0;  // workspace: offset of {maximum, sum}; size
@@ -257,10 +258,11 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
     // each its place (40 sequences in a window of 512: 66 and 59).
     p.longest = a->causal && !thin && tok.N > 1 && tok.N <= 64 &&
                 (p.block == 64 ? blocks64 : blocks128) * t->Hk * p.splits > fit;
-    p.slots = tok.cu ? (int)((int64_t)tok.total * G / p.block) + tok.N
-                     : tok.N * (int)(((int64_t)tok.T * G + p.block - 1) / p.block);
+    p.slots = tok.cu ? (int64_t)tok.total * G / p.block + tok.N
+                     : tok.N * (((int64_t)tok.T * G + p.block - 1) / p.block);
   }
-  if ((int64_t)(p.few ? tok.N : p.slots) * p.splits * t->Hk >= (int64_t)1 << 31)
+  // a launch holds less than 2^32 threads, 256 to a workgroup
+  if ((p.few ? tok.N : p.slots) * p.splits * t->Hk >= (int64_t)1 << 24)
     return GDN_ERR_SHAPE;
   if (p.splits > 1) {
     const int64_t rows = (int64_t)tok.total * t->Hq;
@@ -452,7 +454,7 @@ gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_row
   a.len = p.len;
   a.longest = p.longest;
   hipError_t e = p.few ? gdn::launch_attn_few(dt, t->d, a, s)
-                       : gdn::launch_attn_tile(dt, t->d, p.slots, a, s);
+                       : gdn::launch_attn_tile(dt, t->d, (int)p.slots, a, s);
   if (e == hipSuccess && p.splits > 1) e = gdn::launch_attn_join(dt, t->d, a, s);
   return done(e);
 }
