@@ -41,6 +41,7 @@ template <class E> __device__ inline void store_piece(unsigned char* p, const Pc
 }  // namespace
 
 constexpr int ROT_TOKENS = 4;                  // most tokens of a workgroup
+constexpr unsigned ROT_GRID = 1 << 22;         // workgroups in a grid's first direction
 constexpr int ROT_TABLE = ROT_TOKENS * 256 / 2;  // angles it holds (d <= 256)
 
 // Rotation of pairs: y1 = s (x1 cos a - x2 sin a), y2 = s (x2 cos a + x1 sin a), a the
@@ -52,19 +53,25 @@ constexpr int ROT_TABLE = ROT_TOKENS * 256 / 2;  // angles it holds (d <= 256)
 // 55,700 tokens of 16 + 4 heads, d = 128, bf16, 103 us a direction, 5.5 TB/s (16 tokens,
 // four rows 117; 2 tokens 108; the loads after the angles 119 with 16 and four); prompts
 // into the cache, 137 MB, 25 us (27.5), after a cache-evicting write 46 (54; a copy
-// of as many bytes 39).  A token each for 256 sequences 7 us, the launch.
+// of as many bytes 39).  A token each for 256 sequences 7 us a call, 4.6 in a replayed
+// graph.
 //   WIDE: a unit is one 16-byte piece (interleaved pairs lie inside one) or, in
 //   the layout of halves, the two pieces that hold the two sides of its pairs,
 //   where those start at multiples of 16 bytes; else a unit is one piece, and the
 //   other side of its pairs is read element by element.
-template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
+//   LIST: there is a list of sequences to leave alone.  The look at it, one more load of
+//   every thread, takes 0.2 of the 4.6 us above and 0.8 of the prompts' 25, which calls
+//   without one do not pay.
+template <class E, bool WIDE, bool LIST>
+__global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
   constexpr int N = Pc<E>::N;
   __shared__ float2 cs[ROT_TABLE];
   __shared__ int64_t kat[ROT_TOKENS];  // where the token's k and v go; -1: nowhere
   const int half = a.rot / 2;
-  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.per;
-  if (first >= a.tok.total) return;  // the last row of a grid of several
-  const int t0 = (int)first, nt = min(a.per, a.tok.total - t0);
+  // (in a grid of several rows the last may end past the tokens, within 2^31 + 2^24; a
+  // branch there would hold up the loads of the other arguments)
+  const unsigned group = blockIdx.y * ROT_GRID + blockIdx.x, total = a.tok.total;
+  const int t0 = (int)min(group * a.per, total), nt = min(a.per, (int)total - t0);
   const bool halves = a.layout == 0;
   // units of a row, the first `turn` of them the two sides of pairs
   const int turn = WIDE && halves ? half / N : 0, units = a.d / N - turn;
@@ -174,7 +181,7 @@ template <class E, bool WIDE> __global__ __launch_bounds__(256) void k_rotate(Ro
       const int n = seq_of(a.tok, t), q0 = seq_start(a.tok, n);
       pos = t - q0;
       if (a.append) {
-        pos += cached(a.cache, n) - (seq_start(a.tok, n + 1) - q0);
+        pos += cached<LIST>(a.cache, n) - (seq_start(a.tok, n + 1) - q0);
         if (j == 0) {
           int64_t at = -1;
           if (pos >= 0) {
@@ -264,18 +271,21 @@ hipError_t launch_rotate(Dt dt, RotateArgs a, hipStream_t s) {
   const int half = a.rot / 2;
   a.per = per;
   // (a launch holds less than 2^32 threads in one direction)
-  const int64_t groups = ((int64_t)a.tok.total + per - 1) / per, wide_grid = (int64_t)1 << 22;
-  const dim3 grid((unsigned)std::min(groups, wide_grid),
-                  (unsigned)((groups + wide_grid - 1) / wide_grid));
+  const unsigned groups = ((unsigned)a.tok.total + per - 1) / per;
+  const dim3 grid(std::min(groups, ROT_GRID), (groups + ROT_GRID - 1) / ROT_GRID);
   const int n = dt == Dt::F32 ? 4 : 8;
   const bool wide = a.layout == 1 || half % n == 0;
+  using T = std::true_type;
+  using F = std::false_type;
   auto go = [&](auto e) {
     using E = decltype(e);
-    if (wide)
-      hipLaunchKernelGGL((k_rotate<E, true>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_rotate<E, false>), grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    auto run = [&](auto w, auto l) {
+      hipLaunchKernelGGL((k_rotate<E, decltype(w)::value, decltype(l)::value>), grid, dim3(256), 0,
+                         s, a);
+      return hipGetLastError();
+    };
+    if (a.cache.skip) return wide ? run(T{}, T{}) : run(F{}, T{});
+    return wide ? run(T{}, F{}) : run(F{}, F{});
   };
   return dt == Dt::F32 ? go(float{}) : go(bf16{});
 }

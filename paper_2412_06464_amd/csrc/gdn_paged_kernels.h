@@ -114,12 +114,16 @@ __device__ inline int seq_of(const Tokens& k, int t) {
   return lo;
 }
 __device__ inline int seq_start(const Tokens& k, int n) { return k.cu ? k.cu[n] : n * k.T; }
-// Tokens a sequence holds in the cache, within what its row of the table can.
-__device__ inline int cached(const Cache& c, int n) {
-  if (c.skip && c.skip[n] != 0) return 0;
+// Tokens a sequence holds in the cache, within what its row of the table can; none if it
+// is to be left alone (LIST false: there is no list of those).
+template <bool LIST = true> __device__ inline int cached(const Cache& c, int n) {
   const int64_t most = (int64_t)c.max_blocks << c.shift;
   const int x = c.lens[n];
-  return x < 0 ? 0 : (x > most ? (int)most : x);
+  int skip = 0;
+  // (without a list the length once more, a load beside the other: a branch around it
+  // would stand between the loads before and behind it)
+  if (LIST) skip = (c.skip ? c.skip : c.lens)[n];
+  return x < 0 || (LIST && c.skip && skip != 0) ? 0 : (x > most ? (int)most : x);
 }
 
 }  // namespace gdn
