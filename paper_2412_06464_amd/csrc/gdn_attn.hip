@@ -18,6 +18,9 @@
 //                own keys of a tile and the results are joined in LDS.
 // Where the row blocks do not fill the GPU, a block's keys are split over
 // several workgroups, whose unnormalised sums k_attn_join adds.
+//
+// Times in the comments are of the present kernels, both sides of a choice in turn in
+// one process; the same call differs by up to 4% between two runs on one GPU.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -136,7 +139,7 @@ __device__ inline float col_sum(float x) {
 // The running maximum follows only when a score passes it by this much (in
 // base 2): p stays below 2^8, which costs no accuracy (p, l and o keep their
 // relative precision), and o is rescaled a few times instead of in most tiles
-// (a prompt of 8192 tokens, d = 128: 275 us, with 0 304).
+// (a prompt of 8192 tokens, d = 128: 279 us, with 0 306).
 constexpr float SLACK = 8.f;
 
 template <class E, int D, int QT, int RW, int KW, int KT>
@@ -147,7 +150,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   constexpr int NK = C::NK, NT = NK / 16, RB = C::RB, NP = C::NP, KB = RB / 64, DT = D / 16;
   constexpr int GROUPS = KT / 16;
   // Where two waves share a SIMD, the one in its products goes first: the other
-  // fills in with its softmax (a prompt of 8192 tokens, d = 128: 275 us, without 290;
+  // fills in with its softmax (a prompt of 8192 tokens, d = 128: 275 us, without 285;
   // with three waves, bf16 at d = 64, 174 and 166, so not there).
   constexpr bool PRIO = KW == 1 && RB >= 256 && RB <= 512;
   // The bf16 values that stand for a weight p in its product with v.  Two (p's rounding, and
@@ -607,7 +610,8 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
 // Few rows: one row block per sequence and cache head, its keys split.  Bound by HBM,
 // each key read once for all heads that share it, with two buffers of a CU's whole LDS
 // in flight: a token each for 256 sequences in a 2K window (797 MB) 147 us, 5.4 TB/s; two
-// with 131072 keys (537 MB) 95 us, 5.6 TB/s; four with 1000 keys 7.2 us, latency.
+// with 131072 keys (537 MB) 97 us with the join, 5.5 TB/s; four with 1000 keys 10.4 us with
+// the join, latency.
 // Grid: ((n * splits + split) * Hk + hk).
 template <class E, int D, int QT, int KW, int KT>
 __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
@@ -620,6 +624,7 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;
   b.r0 = 0;
+  // (more rows than the plan had: boundaries that have changed on the device since)
   if (b.m == 0 || (int64_t)b.m * a.G > C::ROWS) return;
   b.r1 = b.m * a.G;
   b.kv = cached(a.cache, b.n);
@@ -688,8 +693,8 @@ __device__ inline bool longest_first(const AttnArgs& a, int R, int rank, int* se
 
 // Many rows: 4 d flop for a row and a key it sees.  Bound by the matrix cores and the
 // exponentials of the softmax in turn, one workgroup's beside the other's.  A prompt
-// of 8192 tokens of 16 heads, 4 cache heads, bf16: 165 us at d = 64 (834 TFLOP/s), 269 at
-// 128 (1,020), 531 at 256 (1,036); two of 2048 in fp32, 8 heads, 159 at d = 128 (108).
+// of 8192 tokens of 16 heads, 4 cache heads, bf16: 165 us at d = 64 (832 TFLOP/s), 269 at
+// 128 (1,021), 530 at 256 (1,038); two of 2048 in fp32, 8 heads, 164 at d = 128 (105).
 // Grid: ((slot * splits + split) * Hk + hk); the sequence and row
 // block of a slot follow from the boundaries: sequence n's slots begin at
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
@@ -702,8 +707,8 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
   __shared__ __align__(1024) unsigned char smem[C::LDS];
   Block b;
   // A second workgroup for some CUs, but no third for any: they come in reverse, the
-  // shortest beside the longest (a prompt of 4096 tokens, 16 heads, d = 128: 107 us, in
-  // order 113; of 2048 in fp32, 8 heads, d = 64: 57 and 79).
+  // shortest beside the longest (a prompt of 4096 tokens, 16 heads, d = 128: 111 us, in
+  // order 113; of 2048 in fp32, 8 heads, d = 64: 57 and 79, two at d = 128 166 and 259).
   const int id =
       gridDim.x > 512 || blockIdx.x < 256 ? blockIdx.x : 255 + gridDim.x - blockIdx.x;
   b.hk = id % a.Hk;
@@ -848,8 +853,8 @@ namespace {
 // of k and v (most bytes in flight), four waves where that leaves each a group
 // of 16.  The other: as many as let two workgroups share a CU (64 KB of buffers),
 // so that one's products run beside the other's softmax: at d = 256 in bf16 32
-// keys, prompts in a 2K window 166 us, with 64 and one workgroup 237; at d = 64 in bf16
-// 64 keys leave room for three or four (a prompt of 8192 tokens 174 us, with 128 197).
+// keys, prompts in a 2K window 174 us, with 64 and one workgroup 247; at d = 64 in bf16
+// 64 keys leave room for three or four (a prompt of 8192 tokens 173 us, with 128 200).
 template <class E, int D> struct Few {
   static constexpr int RB = D * (int)sizeof(E);
   static constexpr int KW = RB >= 1024 ? 2 : 4;

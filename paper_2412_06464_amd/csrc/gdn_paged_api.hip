@@ -180,14 +180,15 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
 
   // Where every sequence has few rows, their kernel, whose waves take different
   // keys: 8 tokens of 4 heads over up to 4000 keys, 64 sequences, 57 us, in the
-  // other 84; fp32 single tokens over 2000 keys 94 and 146.  Bf16 single tokens that
+  // other 76; 12 sequences of up to 5 in fp32, 8 cache heads, up to 3000 keys 22 and
+  // 44; fp32 single tokens over 2000 keys 93 and 149.  Bf16 single tokens that
   // fill the GPU take the same in both (a batch of 256 in a 2K window 149 and 147
   // us), and where their keys are so few that a workgroup's start counts, two of the
-  // other to a CU are the faster (212 sequences, 8 cache heads: 70 keys 43 and 27
-  // us, 500 100 and 89, 1000 163 and 162; 176 in fp32, 2 cache heads: 317 keys 26
-  // and 45, 836 units of 3 keys 22 and 15).  With larger sequences beside them, all
+  // other to a CU are the faster (212 sequences, 8 cache heads: 70 keys 39 and 27
+  // us, 500 94 and 87, 1000 156 and 160; 836 units of 3 keys 19 and 11; but 176 in
+  // fp32, 2 cache heads, 317 keys 30 and 45).  With larger sequences beside them, all
   // in one launch of the other: 127 single tokens and 512 of one sequence over up to
-  // 4000 keys 123 us, in a launch each 150.
+  // 4000 keys 123 us, in a launch each (as before that) 150.
   const int64_t few_units = std::max<int64_t>(1, seqs * t->Hk), few_keys = keys(most);
   p.few = most * G <= gdn::FEW_ROWS &&
           (few_units <= 256 || few_keys * (dt == Dt::F32 ? 8 : 1) > 1024);
@@ -220,8 +221,8 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
     // In fp32 the matrix cores alone bind, so a block is slow beside a second one only as
     // long as that lasts.  Where the new tokens are much of the keys and sequences are
     // alike, the longest block has the shortest beside it, of `least` of its keys (two
-    // prompts of 2048 tokens, 8 heads, 4 cache heads, d = 128: 164 us, without this term,
-    // in 128 rows, 276; 5 of up to 900 85 and 137; one of 2000, 16 heads 159 and 269).  In
+    // prompts of 2048 tokens, 8 heads, 4 cache heads, d = 128: 168 us, without this term,
+    // in 128 rows, 276; 5 of up to 900 88 and 139; one of 2000, 16 heads 163 and 270).  In
     // bf16 it would choose 64 rows where 128 are better (d = 256, 4096 tokens: 162 and 141).
     const bool pairs = f32 && a->causal && a->window == 0 && 2 * (int64_t)tok.total >= seqs * most;
     const double least = std::max(0., 1 - (double)most / kv);
@@ -252,9 +253,9 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
     cut(keys(std::min<int64_t>(most, p.block / G + 2)), at, step);
     // Several sequences' blocks that do not all run at once start in the order of their
     // keys, or a long one begins when most of the GPU is done: 8 prompts in a 2K
-    // window, d = 256, 166 us, in the sequences' order 205; 60 sequences of up to 300
-    // tokens over up to 3000 keys 110 and 143; 8 of 2048 tokens 158 and 174 (2 of 4000
-    // 140 and 135).  The bf16 blocks of d = 64 are too short for the search that finds
+    // window, d = 256, 171 us, in the sequences' order 209; 60 sequences of up to 300
+    // tokens over up to 3000 keys 112 and 141; 8 of 2048 tokens 159 and 173 (2 of 4000
+    // 142 and 137).  A lane holds a sequence: more than 64 come in their own order.  The bf16 blocks of d = 64 are too short for the search that finds
     // each its place (40 sequences in a window of 512: 66 and 59).
     p.longest = a->causal && !thin && tok.N > 1 && tok.N <= 64 &&
                 (p.block == 64 ? blocks64 : blocks128) * t->Hk * p.splits > fit;
