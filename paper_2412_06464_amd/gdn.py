@@ -6,6 +6,7 @@ stream.  There is no fallback: if the library is missing, loading fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -323,6 +324,17 @@ def _stream(device):
     if _raw_stream is None or device.type != "cuda" or device.index is None:
         return torch.cuda.current_stream(device).cuda_stream
     return _raw_stream(device.index)
+
+
+_NOWHERE = contextlib.nullcontext()
+
+
+def _on(device):
+    """The device as the current one for a call, where it is not: a launch goes to the current
+    device's code."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return _NOWHERE
+    return torch.cuda.device(device)
 
 
 def _check(code: int):
