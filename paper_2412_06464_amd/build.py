@@ -29,7 +29,8 @@ FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++20", "-fPIC",
 # the general passes gain in fp32 at 256/512 (us, without / with it: forward
 # 321 / 315 at 1 x 1000 x 4 and 646 / 634 at 2 x 2048 x 6, training step 1,389 /
 # 1,373) and are elsewhere the same (bf16 within 1 us of 20 to 700).
-SOURCE_FLAGS = {"gdn_seq.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+SOURCE_FLAGS = {"gdn_seq.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+                "gdn_linear.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src: str, obj: str, extra=()) -> None:

@@ -6,8 +6,7 @@
 // k_linear walks the chunks of a sequence (or of a segment of it) for one head and a
 // slice of dv, with the state slice in fp32 accumulators from the first chunk to
 // the last: HBM sees q, k, v and o once and no chunk's state.  Every wave owns
-// 16 or 32 columns of the slice and needs nothing of the others but the rows of
-// q, k and v in LDS, so a chunk takes two barriers.  All products use the permuted
+// 16 columns of the slice, and the waves share out the tiles of P.  All products use the permuted
 // contraction order of gdn_device.h, in which accumulator tiles are operands as
 // they stand:
 //     P   = K Q^T        (rows s, columns t)  A = K rows, B = Q rows, from LDS
@@ -86,23 +85,40 @@ template <> __device__ inline float operand<float>(const f32x4* t, int stride, i
   return t[(kt >> 2) * stride][kt & 3];
 }
 
-// Operands of a row in LDS (p: the row's element 4 (lane >> 4)), all k-steps of KD.
-template <class E, int KD>
-__device__ inline void row_operands(typename Mfma<E>::frag (&f)[KD / Mfma<E>::K], const E* p) {
+// Matrices in LDS.  In bf16 an operand read takes 8 bytes of each of 16 rows, a transposing one
+// 32 bytes of each of 4: with rows 8 banks apart (of 32) and the four 8-byte units of a 32-byte
+// block exchanged by unit XOR (row / 4) % 4, both meet every bank once, and so do the
+// accumulators' stores.  In fp32 they take 16 bytes of 8 rows, or 64 bytes of 2 rows 4 apart:
+// rows 4 banks apart.
+template <class E> struct Lds {
+  static constexpr int PAD = sizeof(E) == 2 ? 16 : 4;  // DK, NV and 64 are multiples of 32 banks
+};
+__device__ inline int units(int row) { return (row >> 2) & 3; }
+
+// 16-byte piece p of row r (its first element; row stride LD).
+template <class E, int LD> __device__ inline u32x4* piece(E* m, int r, int p) {
+  const int x = sizeof(E) == 2 ? p ^ (units(r) >> 1) : p;
+  return reinterpret_cast<u32x4*>(m + r * LD + x * (16 / (int)sizeof(E)));
+}
+// A piece as it stands there, or back.
+template <class E> __device__ inline u32x4 turned(u32x4 x, int r) {
+  if constexpr (sizeof(E) == 4) return x;
+  return units(r) & 1 ? u32x4{x[2], x[3], x[0], x[1]} : x;
+}
+
+// This lane's part (columns 4 g .. of every 16) of row 16 x + c16: its first element.
+template <class E, int LD> __device__ inline E* row_part(E* m, int x) {
+  const int c16 = lane_id() & 15, g = lane_id() >> 4;
+  return m + (16 * x + c16) * LD + 4 * (sizeof(E) == 2 ? g ^ units(c16) : g);
+}
+// Operand of k-step kt of the row with this part.
+template <class E> __device__ inline typename Mfma<E>::frag row_operand(const E* p, int kt) {
   if constexpr (sizeof(E) == 2) {
-#pragma unroll
-    for (int kt = 0; kt < KD / 32; ++kt) {
-      const bf16x4 x = *reinterpret_cast<const bf16x4*>(p + 32 * kt);
-      const bf16x4 y = *reinterpret_cast<const bf16x4*>(p + 32 * kt + 16);
-      f[kt] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
+    const bf16x4 x = *reinterpret_cast<const bf16x4*>(p + 32 * kt);
+    const bf16x4 y = *reinterpret_cast<const bf16x4*>(p + 32 * kt + 16);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
   } else {
-#pragma unroll
-    for (int i = 0; i < KD / 16; ++i) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(p + 16 * i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[4 * i + e] = x[e];
-    }
+    return p[16 * (kt >> 2) + (kt & 3)];
   }
 }
 
@@ -112,7 +128,8 @@ __device__ inline typename Mfma<E>::frag col_operand(const E* m, int c0, int kt)
   const int c16 = lane_id() & 15, g = lane_id() >> 4;
   if constexpr (sizeof(E) == 2) {
     // lane i of 16 points at 4 columns of row i / 4 and receives column i of the 4 rows
-    const E* p = m + (32 * kt + 4 * g + (c16 >> 2)) * LD + c0 + 4 * (c16 & 3);
+    // (units(row) is g)
+    const E* p = m + (32 * kt + 4 * g + (c16 >> 2)) * LD + c0 + 4 * ((c16 & 3) ^ g);
     const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)p);
     const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(p + 16 * LD));
     const s16x8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -131,26 +148,76 @@ template <class E> __device__ inline bool has_odd(u32x4 w) {
   return odd;
 }
 
-// DK x (64 NC) of the state a workgroup, 16 NC columns of it a wave.
+// Inclusive prefix sums over the 64 lanes: within rows of 16 lanes by shifts of 1, 2, 4 and
+// 8, then each row's last to the row behind it, then the lower half's to the upper.  By DPP: six
+// exchanges of 64 bits through LDS took 4,000 clocks of a chunk's 17,000.
+template <int CTRL, int ROWS> __device__ inline double dpp_or_zero(double x) {
+  const long long b = __double_as_longlong(x);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+  return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
+}
+__device__ inline double wave_sums(double x) {
+  x += dpp_or_zero<0x111, 0xf>(x);  // row_shr 1
+  x += dpp_or_zero<0x112, 0xf>(x);
+  x += dpp_or_zero<0x114, 0xf>(x);
+  x += dpp_or_zero<0x118, 0xf>(x);
+  x += dpp_or_zero<0x142, 0xa>(x);  // row_bcast 15, to rows 1 and 3
+  x += dpp_or_zero<0x143, 0xc>(x);  // row_bcast 31, to rows 2 and 3
+  return x;
+}
+
+// One token's sum G of log2 alphas in a chunk (its value in fp32, and what that leaves
+// over), 2^(G_64 - G) and 2^G.
+struct Gates {
+  float2 G[64];
+  float left[64], grown[64];
+};
+
+// How a workgroup's DK x NV of the state lie over its waves: DK / KS rows and 16 NC
+// columns each.
+template <class E, int DK, int NV> struct LinearCfg;
+template <int DK> struct LinearCfg<bf16, DK, 64> {
+  static constexpr int KS = DK == 256 ? 2 : 1, NC = 1;
+};
+template <int DK> struct LinearCfg<bf16, DK, 128> {
+  static constexpr int KS = DK == 256 ? 2 : 1, NC = 2;
+};
+template <int DK, int NV> struct LinearCfg<float, DK, NV> {
+  static constexpr int KS = DK == 256 ? 2 : 1, NC = 1;
+};
+
 // Grid: groups of 8 units (slot, head) x slices of dv, a unit's slices 8 apart, so that
 // they share the q and k of an XCD's L2.
-template <class E, int DK, int NC, bool OUT>
-__global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
+template <class E, int DK, int NV, int KS, int NC, bool OUT>
+__global__ __launch_bounds__(64 * KS * NV / (16 * NC), KS * NV / (16 * NC) / 4 * (NC == 2 && KS == 1 ? 2 : 1))
+void k_linear(LinearArgs a) {
   using M = Mfma<E>;
-  constexpr int NV = 64 * NC, PAD = sizeof(E) == 2 ? 16 : 4;
-  constexpr int LK = DK + PAD, LV = NV + PAD;  // row strides: operand reads spread over the banks
+  using frag = typename M::frag;
+  constexpr int CW = NV / (16 * NC), W = CW * KS, NTH = 64 * W;
+  constexpr int LK = DK + Lds<E>::PAD, LV = NV + Lds<E>::PAD, LP = 64 + Lds<E>::PAD;  // row strides
   constexpr int EPP = 16 / (int)sizeof(E);     // elements of a piece
   constexpr int PK = DK / EPP, PV = NV / EPP;  // pieces of a row
-  constexpr int RK = 64 * PK / 256, RV = 64 * PV / 256;
-  constexpr int KQ = DK / M::K, KT = 64 / M::K, IT = DK / 16;
+  constexpr int RK = 64 * PK / NTH, RV = 64 * PV / NTH;
+  constexpr int KQ = DK / M::K / KS, KT = 64 / M::K, IT = DK / 16 / KS;
+  constexpr int BP = 64 * LP * (int)sizeof(E), BX = KS > 1 ? W * 2 * NC * 1024 : 0;
+  // where LDS is short, P and the sums that waves exchange take the place of q, at the price
+  // of a barrier
+  constexpr bool OVER = OUT && 64 * (2 * LK + LV) * (int)sizeof(E) + BP + BX > 156 * 1024;
   __shared__ __align__(16) E sq[OUT ? 64 * LK : 16];
   __shared__ __align__(16) E sk[64 * LK];
   __shared__ __align__(16) E sv[64 * LV];
-  __shared__ float2 sg[64];  // G: its value in fp32, and what that leaves over
-  __shared__ int sodd;
+  __shared__ __align__(16) unsigned char more[OUT && !OVER ? BP + BX : 16];
+  __shared__ Gates gates[2];
+  __shared__ int sodd[2];
+  E* const sp = OVER ? sq : (E*)more;                                       // P [t][s]
+  f32x4* const sx = (f32x4*)((OVER ? (unsigned char*)sq : more) + BP);      // sums to add
+  static_assert(!OVER || 64 * LK * (int)sizeof(E) >= BP + BX, "q's place is too small");
 
   const int tid = threadIdx.x, lane = lane_id(), g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int kh = KS == 1 ? 0 : wave / CW, cw = KS == 1 ? wave : wave % CW;
+  constexpr int GATES = W == 8 ? 7 : 0;  // the wave that finds the gates
   const int slices = a.dv / NV;
   const int grp = blockIdx.x / (8 * slices), rest = blockIdx.x - grp * 8 * slices;
   const int slice = rest >> 3, unit = grp * 8 + (rest & 7);
@@ -158,13 +225,14 @@ __global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
   const int slot = unit / a.H, h = unit - slot * a.H;
   const Segment seg = segment(a, slot);
   if (!seg.real || (!OUT && seg.last)) return;
-  const int n0 = slice * NV + wave * 16 * NC;  // this wave's columns
+  const int n0 = slice * NV + cw * 16 * NC;  // this wave's columns
+  const int k0 = kh * (DK / KS);             // and rows
   const E* const Q = (const E*)a.q + (size_t)h * DK;
   const E* const K = (const E*)a.k + (size_t)h * DK;
   const E* const V = (const E*)a.v + (size_t)h * a.dv + slice * NV;
   const size_t rk = (size_t)a.H * DK, rv = (size_t)a.H * a.dv;  // elements between tokens
 
-  // the state: rows 16 i + 4 g + e, column n0 + 16 c + c16
+  // the state: rows k0 + 16 i + 4 g + e, column n0 + 16 c + c16
   f32x4 S[IT][NC];
   const size_t matrix = (size_t)DK * a.dv;
   {
@@ -177,207 +245,346 @@ __global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          S[i][c][e] = from ? from[(size_t)(16 * i + 4 * g + e) * a.dv + n0 + 16 * c + c16] : 0.f;
+          S[i][c][e] =
+              from ? from[(size_t)(k0 + 16 * i + 4 * g + e) * a.dv + n0 + 16 * c + c16] : 0.f;
   }
 
   // the next chunk's rows, on their way
+  // (rows past the segment's last: that one again, cleared where they are stored)
   u32x4 nq[OUT ? RK : 1], nk[RK], nv[RV];
-  float nla = 0.f;
+  const int pk = tid % PK * EPP, pv = tid % PV * EPP;  // NTH is a multiple of PK and PV
   auto fetch = [&](int t) {
-    const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < RK; ++i) {
-      const int x = tid + 256 * i, r = x / PK, p = x - r * PK;
-      const bool in = t + r < seg.t1;
-      const size_t at = (size_t)(t + r) * rk + p * EPP;
-      if (OUT) nq[i] = in ? *reinterpret_cast<const u32x4*>(Q + at) : none;
-      nk[i] = in ? *reinterpret_cast<const u32x4*>(K + at) : none;
+      const size_t at = (size_t)min(t + tid / PK + NTH / PK * i, seg.t1 - 1) * rk + pk;
+      if (OUT) nq[i] = *reinterpret_cast<const u32x4*>(Q + at);
+      nk[i] = *reinterpret_cast<const u32x4*>(K + at);
     }
 #pragma unroll
-    for (int i = 0; i < RV; ++i) {
-      const int x = tid + 256 * i, r = x / PV, p = x - r * PV;
-      nv[i] = t + r < seg.t1 ? *reinterpret_cast<const u32x4*>(V + (size_t)(t + r) * rv + p * EPP)
-                             : none;
-    }
-    nla = 0.f;
-    if (wave == 0 && a.log_alpha && t + lane < seg.t1)
-      nla = a.log_alpha[a.per_head ? h : (size_t)(t + lane) * a.H + h];
+    for (int i = 0; i < RV; ++i)
+      nv[i] = *reinterpret_cast<const u32x4*>(
+          V + (size_t)min(t + tid / PV + NTH / PV * i, seg.t1 - 1) * rv + pv);
   };
-  if (seg.t0 < seg.t1) fetch(seg.t0);
+  float la = 0.f;  // of the chunk whose gates are found next
+  auto fetch_la = [&](int t) {
+    la = 0.f;
+    if (a.log_alpha && t + lane < seg.t1)
+      la = a.log_alpha[a.per_head ? h : (size_t)(t + lane) * a.H + h];
+  };
   double total = 0;  // log2 of the segment's product of alphas
+  auto find_gates = [&](Gates& to) {
+    // summed in 64 bits: the differences of two sums are what weighs
+    const double x = wave_sums((double)finite_log(la) * 1.4426950408889634074);
+    const double end = __shfl(x, 63);
+    const float hi = (float)x;
+    to.G[lane] = make_float2(hi, (float)(x - (double)hi));
+    to.left[lane] = __builtin_amdgcn_exp2f((float)(end - x));
+    to.grown[lane] = __builtin_amdgcn_exp2f((float)x);
+    total += end;
+  };
+  if (seg.t0 < seg.t1) {
+    fetch(seg.t0);
+    if (wave == GATES) {
+      fetch_la(seg.t0);
+      find_gates(gates[0]);
+      fetch_la(seg.t0 + 64);
+    }
+  }
+  if (tid < 2) sodd[tid] = 0;
+  auto put_out = [&](int t, int r, u32x4 x) {
+    if (t + r < seg.t1)
+      *reinterpret_cast<u32x4*>((E*)a.o + (size_t)(t + r) * rv + (size_t)h * a.dv + slice * NV + pv) =
+          turned<E>(x, r);
+  };
 
-  for (int t = seg.t0; t < seg.t1; t += 64) {
-    if (tid == 0) sodd = 0;
-    lds_barrier();  // the rows before are no longer read
+  int buf = 0, t = seg.t0;
+  for (; t < seg.t1; t += 64, buf ^= 1) {
+    lds_barrier();  // what stood there is no longer read; the outputs are in v's place
+    if (t + 64 > seg.t1) {
+#pragma unroll
+      for (int i = 0; i < RK; ++i)
+        if (t + tid / PK + NTH / PK * i >= seg.t1) {
+          if (OUT) nq[i] = u32x4{0, 0, 0, 0};
+          nk[i] = u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+      for (int i = 0; i < RV; ++i)
+        if (t + tid / PV + NTH / PV * i >= seg.t1) nv[i] = u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < RK; ++i) {
+      const int r = tid / PK + NTH / PK * i;
+      if (OUT) *piece<E, LK>(sq, r, tid % PK) = turned<E>(nq[i], r);
+      *piece<E, LK>(sk, r, tid % PK) = turned<E>(nk[i], r);
+    }
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < RK; ++i) {
-      const int x = tid + 256 * i, r = x / PK, p = x - r * PK;
-      if (OUT) *reinterpret_cast<u32x4*>(sq + r * LK + p * EPP) = nq[i];
-      *reinterpret_cast<u32x4*>(sk + r * LK + p * EPP) = nk[i];
-    }
-#pragma unroll
     for (int i = 0; i < RV; ++i) {
-      const int x = tid + 256 * i, r = x / PV, p = x - r * PV;
-      *reinterpret_cast<u32x4*>(sv + r * LV + p * EPP) = nv[i];
-      if (OUT) odd = odd || has_odd<E>(nv[i]);
+      const int r = tid / PV + NTH / PV * i;
+      u32x4* const at = piece<E, LV>(sv, r, tid % PV);
+      // stored here, the outputs are long gone when the next rows are waited for (one
+      // counter holds both)
+      if (OUT && t > seg.t0) put_out(t - 64, r, *at);
+      *at = turned<E>(nv[i], r);
+      odd = odd || has_odd<E>(nv[i]);
     }
-    if (OUT && odd) sodd = 1;
-    if (wave == 0) {
-      // summed in 64 bits: the differences of two sums are what weighs
-      double x = (double)finite_log(nla) * 1.4426950408889634074;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const double y = __shfl_up(x, d, 64);
-        if (lane >= d) x += y;
-      }
-      const float hi = (float)x;
-      sg[lane] = make_float2(hi, (float)(x - (double)hi));
-    }
+    if (odd) sodd[buf] = 1;
     if (t + 64 < seg.t1) fetch(t + 64);
     lds_barrier();
+    const Gates& gt = gates[buf];
+    const bool careful = sodd[buf] != 0;
+    if (tid == 0) sodd[buf ^ 1] = 0;
+    if (wave == GATES) {
+      find_gates(gates[buf ^ 1]);
+      fetch_la(t + 128);
+    }
 
-    float2 G[4][4];  // of tokens 16 s + 4 g + e
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) G[s][e] = sg[16 * s + 4 * g + e];
-    const float2 end = sg[63];
-    total += (double)end.x + (double)end.y;
-
-    typename M::frag vf[KT][NC];
+    frag vf[KT][NC];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-        vf[kt][c] = col_operand<E, LV>(sv, wave * 16 * NC + 16 * c, kt);
+      for (int c = 0; c < NC; ++c) vf[kt][c] = col_operand<E, LV>(sv, cw * 16 * NC + 16 * c, kt);
 
+    constexpr int MINE = KS == 1 ? 4 : 2;  // token tiles whose outputs this wave finishes
+    f32x4 mine[MINE][NC];
     if constexpr (OUT) {
-      typename M::frag sf[KQ][NC];  // the state as an operand
+      // P: rows s, columns t.  Tasks of two tiles side by side, of one
+      auto task = [&](auto count, int tt, int s) {
+        constexpr int CNT = decltype(count)::value;
+        f32x4 p[CNT], r[CNT];  // sums of even and odd steps
 #pragma unroll
-      for (int kt = 0; kt < KQ; ++kt)
+        for (int j = 0; j < CNT; ++j) p[j] = r[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int PART = DK / M::K > 8 ? DK / M::K / 8 : 1;  // (fp32: a part of a row at a time)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) sf[kt][c] = operand<E>(&S[0][c], NC, kt);
-      const bool careful = sodd != 0;
+        for (int x = 0; x < PART; ++x) {
+          constexpr int D = DK / PART;
+          frag q[D / M::K], k[CNT][D / M::K];
+          const E* const pq = row_part<E, LK>(sq, tt) + x * D;
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt) {
-        typename M::frag q[KQ];
-        row_operands<E, DK>(q, sq + (16 * tt + c16) * LK + 4 * g);
-        const float2 Gt = sg[16 * tt + c16];
-        f32x4 o[NC];
+          for (int kt = 0; kt < D / M::K; ++kt) q[kt] = row_operand<E>(pq, kt);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int j = 0; j < CNT; ++j) {
+            const E* const p = row_part<E, LK>(sk, s + j) + x * D;
 #pragma unroll
-        for (int kt = 0; kt < KQ; ++kt)
+            for (int kt = 0; kt < D / M::K; ++kt) k[j][kt] = row_operand<E>(p, kt);
+          }
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c] = M::mma(sf[kt][c], q[kt], o[c]);
-        const float et = __builtin_amdgcn_exp2f(Gt.x + Gt.y);
+          for (int kt = 0; kt < D / M::K; ++kt)
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+            for (int j = 0; j < CNT; ++j) {
+              f32x4& to = kt & 1 ? r[j] : p[j];
+              to = M::mma(k[j][kt], q[kt], to);
+            }
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[c][e] *= et;
-        f32x4 p[4];
+        for (int j = 0; j < CNT; ++j)
 #pragma unroll
-        for (int s = 0; s < 4; ++s) p[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int e = 0; e < 4; ++e) p[j][e] += r[j][e];
+        const float2 Gt = gt.G[16 * tt + c16];
 #pragma unroll
-        for (int s = 0; s <= tt; ++s) {
-          typename M::frag k[KQ];
-          row_operands<E, DK>(k, sk + (16 * s + c16) * LK + 4 * g);
-#pragma unroll
-          for (int kt = 0; kt < KQ; ++kt) p[s] = M::mma(k[kt], q[kt], p[s]);
+        for (int j = 0; j < CNT; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float w = __builtin_amdgcn_exp2f((Gt.x - G[s][e].x) + (Gt.y - G[s][e].y));
-            p[s][e] = s < tt || 4 * g + e <= c16 ? p[s][e] * w : 0.f;
+            const float2 Gs = gt.G[16 * (s + j) + 4 * g + e];
+            float w = __builtin_amdgcn_exp2f((Gt.x - Gs.x) + (Gt.y - Gs.y));
+            asm("" : "+v"(w));  // (or each stands behind a branch of its own)
+            p[j][e] = s + j < tt || 4 * g + e <= c16 ? p[j][e] * w : 0.f;
+          }
+        if constexpr (OVER) lds_barrier();
+#pragma unroll
+        for (int j = 0; j < CNT; ++j) {
+          typename Raw4<E>::type y = {to_e<E>(p[j][0]), to_e<E>(p[j][1]), to_e<E>(p[j][2]),
+                                      to_e<E>(p[j][3])};
+          *reinterpret_cast<typename Raw4<E>::type*>(row_part<E, LP>(sp, tt) + 16 * (s + j)) = y;
+        }
+      };
+      // the entry state's part
+      f32x4 o[4][NC];
+      auto from_state = [&]() {
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[tt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kt = 0; kt < KQ; ++kt) {
+          frag sf[NC];
+#pragma unroll
+          for (int c = 0; c < NC; ++c) sf[c] = operand<E>(&S[0][c], NC, kt);
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt) {
+            const frag q = row_operand<E>(row_part<E, LK>(sq, tt) + k0, kt);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[c], q, o[tt][c]);
           }
         }
-        if (!careful) {
+      };
+      constexpr std::integral_constant<int, 1> one{};
+      constexpr std::integral_constant<int, 2> two{};
+      if constexpr (OVER) {
+        static_assert(!OVER || W == 8, "each wave has one task");
+        from_state();
+        // (a wave without a task meets the others' barrier alone)
+        if (wave < 4) task(two, wave < 2 ? 3 : 4 - wave, wave == 1 ? 2 : 0);
+        else if (wave < 6) task(one, wave == 4 ? 2 : 0, wave == 4 ? 2 : 0);
+        else lds_barrier();
+      } else {
+        if (wave < 4) task(two, wave < 2 ? 3 : 4 - wave, wave == 1 ? 2 : 0);
+        const int x = W == 8 ? wave : wave + 2;
+        if (x == 4 || x == 5) task(one, x == 4 ? 2 : 0, x == 4 ? 2 : 0);
+        from_state();
+      }
+      // two waves of the same columns: each adds up two of the four token tiles
+      if constexpr (KS == 1) {
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            if (kt * M::K >= 16 * (tt + 1)) break;
-            const typename M::frag x = operand<E>(p, 1, kt);
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) o[c] = M::mma(vf[kt][c], x, o[c]);
-          }
-        } else {
-          // an infinity or NaN in v must not meet the zeros of earlier tokens
+          for (int c = 0; c < NC; ++c) mine[j][c] = o[j][c];
+      } else {
 #pragma unroll
-          for (int s = 0; s <= tt; ++s)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll 1
-              for (int x = j; x < 16; x += 4) {
-                const float w = __shfl(p[s][j], (x >> 2) * 16 + c16);
-                if (s == tt && x > c16) continue;
-                const E* from = sv + (16 * s + x) * LV + wave * 16 * NC + 4 * g;
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) o[c][e] += w * to_f(from[16 * c + e]);
-              }
-        }
-        const int row = t + 16 * tt + c16;
-        if (row < seg.t1) {
-          E* to = (E*)a.o + (size_t)row * rv + (size_t)h * a.dv + n0 + 4 * g;
-#pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            typename Raw4<E>::type y = {to_e<E>(o[c][0]), to_e<E>(o[c][1]), to_e<E>(o[c][2]),
-                                        to_e<E>(o[c][3])};
-            *reinterpret_cast<typename Raw4<E>::type*>(to + 16 * c) = y;
-          }
+        for (int c = 0; c < NC; ++c) {
+          mine[0][c] = kh ? o[1][c] : o[0][c];
+          mine[1][c] = kh ? o[2][c] : o[3][c];
+          sx[((wave * 2 + 0) * NC + c) * 64 + lane] = kh ? o[0][c] : o[1][c];
+          sx[((wave * 2 + 1) * NC + c) * 64 + lane] = kh ? o[3][c] : o[2][c];
         }
       }
     }
 
-    // the state: v weighted, in bf16 as two values (2^-17 of it is lost, where one
+    // the state: v weighted, in bf16 as two values (2^-16 of it is lost, where one
     // value would leave the state with eight bits)
-    const float fe = __builtin_amdgcn_exp2f(end.x + end.y);
+    const float fe = gt.grown[63];
 #pragma unroll
     for (int i = 0; i < IT; ++i)
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[i][c][e] *= fe;
-    float w[4][4];
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        w[s][e] = __builtin_amdgcn_exp2f((end.x - G[s][e].x) + (end.y - G[s][e].y));
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      typename M::frag hi[NC], lo[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if constexpr (sizeof(E) == 2) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float x = (float)vf[kt][c][j] * w[2 * kt + (j >> 2)][j & 3];
-            const bf16 y = (bf16)x;
-            const float z = x - (float)y;
-            hi[c][j] = y;
-            lo[c][j] = (bf16)(z - z == 0.f ? z : 0.f);
-          }
-        } else {
-          hi[c] = vf[kt][c] * w[kt >> 2][kt & 3];
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const typename M::frag x = col_operand<E, LK>(sk, 16 * i, kt);
+      frag hi[NC], lo[NC];
+      if constexpr (sizeof(E) == 2) {
+        const f32x4 w0 = *reinterpret_cast<const f32x4*>(gt.left + 32 * kt + 4 * g);
+        const f32x4 w1 = *reinterpret_cast<const f32x4*>(gt.left + 32 * kt + 16 + 4 * g);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          S[i][c] = M::mma(x, hi[c], S[i][c]);
-          if constexpr (sizeof(E) == 2) S[i][c] = M::mma(x, lo[c], S[i][c]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float x = (float)vf[kt][c][j] * (j < 4 ? w0[j & 3] : w1[j & 3]);
+            hi[c][j] = (bf16)x;
+            lo[c][j] = (bf16)(x - (float)hi[c][j]);
+          }
+          if (careful)  // (an infinity less itself)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if ((float)lo[c][j] != (float)lo[c][j]) lo[c][j] = (bf16)0.f;
+        }
+      } else {
+        const float w = gt.left[16 * (kt >> 2) + 4 * g + (kt & 3)];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) hi[c] = vf[kt][c] * w;
+      }
+      // (four row tiles at a time: products that follow each other do not wait for one another)
+#pragma unroll
+      for (int i0 = 0; i0 < IT; i0 += 4) {
+        frag x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = col_operand<E, LK>(sk, k0 + 16 * (i0 + i), kt);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) S[i0 + i][c] = M::mma(x[i], hi[c], S[i0 + i][c]);
+        if constexpr (sizeof(E) == 2)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) S[i0 + i][c] = M::mma(x[i], lo[c], S[i0 + i][c]);
+      }
+    }
+
+    if constexpr (OUT) {
+      lds_barrier();
+      auto tile = [&](int j) { return KS == 1 ? j : kh ? 1 + j : 3 * j; };
+#pragma unroll
+      for (int j = 0; j < MINE; ++j) {
+        const float et = gt.grown[16 * tile(j) + c16];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if constexpr (KS > 1) {
+            const f32x4 y = sx[(((wave ^ CW) * 2 + j) * NC + c) * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine[j][c][e] += y[e];
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mine[j][c][e] *= et;
         }
       }
+      if (!careful) {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+          const int tt = tile(j), most = KS == 1 ? j : 1 + 2 * j;  // (most: at compile time)
+          frag x[KT];
+          const E* const p = row_part<E, LP>(sp, tt);
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) x[kt] = row_operand<E>(p, kt);
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) {
+            // what is past the diagonal tile was not written
+            if constexpr (sizeof(E) == 2) {
+              if (2 * kt > most) continue;
+              const bf16x8 half = __builtin_shufflevector(x[kt], bf16x8{}, 0, 1, 2, 3, 8, 9, 10, 11);
+              x[kt] = 2 * kt < tt ? x[kt] : half;
+            } else {
+              if (kt / 4 > most) continue;
+              x[kt] = kt / 4 <= tt ? x[kt] : 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) mine[j][c] = M::mma(vf[kt][c], x[kt], mine[j][c]);
+          }
+        }
+      } else {
+        // an infinity or NaN in v must not meet the zeros of earlier tokens
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+          const int tt = tile(j);
+#pragma unroll 1
+          for (int s = 0; s <= 16 * tt + c16; ++s) {
+            const bool b = sizeof(E) == 2;
+            const float w = to_f(sp[(16 * tt + c16) * LP + (b ? s ^ 4 * units(c16) : s)]);
+            const E* from = sv + s * LV + cw * 16 * NC + 4 * (b ? g ^ units(s) : g);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) mine[j][c][e] += w * to_f(from[16 * c + e]);
+          }
+        }
+        lds_barrier();
+      }
+      // v is in registers, or read: o takes its place
+#pragma unroll
+      for (int j = 0; j < MINE; ++j)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          *reinterpret_cast<typename Raw4<E>::type*>(row_part<E, LV>(sv, tile(j)) + cw * 16 * NC +
+                                                     16 * c) =
+              typename Raw4<E>::type{to_e<E>(mine[j][c][0]), to_e<E>(mine[j][c][1]),
+                                     to_e<E>(mine[j][c][2]), to_e<E>(mine[j][c][3])};
+    }
+  }
+  if (OUT && t > seg.t0) {
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < RV; ++i) {
+      const int r = tid / PV + NTH / PV * i;
+      put_out(t - 64, r, *piece<E, LV>(sv, r, tid % PV));
     }
   }
 
   float* to = nullptr;
   if (!OUT) {
     to = a.states + ((size_t)slot * a.H + h) * matrix;
-    if (slice == 0 && tid == 0) a.fade[(size_t)slot * a.H + h] = (float)exp2(total);
+    // (the gates of one more chunk are in the total: those past the segment are 0)
+    if (slice == 0 && wave == GATES && lane == 0)
+      a.fade[(size_t)slot * a.H + h] = (float)exp2(total);
   } else if (seg.last && a.ht) {
     to = a.ht + ((size_t)seg.n * a.H + h) * matrix;
   }
@@ -388,7 +595,7 @@ __global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          to[(size_t)(16 * i + 4 * g + e) * a.dv + n0 + 16 * c + c16] = S[i][c][e];
+          to[(size_t)(k0 + 16 * i + 4 * g + e) * a.dv + n0 + 16 * c + c16] = S[i][c][e];
   }
 }
 
@@ -508,14 +715,16 @@ template <bool OUT> hipError_t launch(Dt dt, const LinearArgs& a, hipStream_t s)
   return by_dk(dt, a.dk, [&](auto e, auto dim) {
     using E = decltype(e);
     constexpr int DK = decltype(dim)::value;
-    if constexpr (sizeof(E) == 2 || DK < 256) {
-      if (nv == 128) {
-        hipLaunchKernelGGL((k_linear<E, DK, 2, OUT>), dim3(grid), dim3(256), 0, s, a);
-        return hipGetLastError();
-      }
-    }
-    hipLaunchKernelGGL((k_linear<E, DK, 1, OUT>), dim3(grid), dim3(256), 0, s, a);
-    return hipGetLastError();
+    auto go = [&](auto columns) {
+      constexpr int NV = decltype(columns)::value;
+      using C = LinearCfg<E, DK, NV>;
+      hipLaunchKernelGGL((k_linear<E, DK, NV, C::KS, C::NC, OUT>), dim3(grid),
+                         dim3(64 * C::KS * NV / (16 * C::NC)), 0, s, a);
+      return hipGetLastError();
+    };
+    if constexpr (sizeof(E) == 2 || DK < 256)
+      if (nv == 128) return go(std::integral_constant<int, 128>{});
+    return go(std::integral_constant<int, 64>{});
   });
 }
 
