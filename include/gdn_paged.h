@@ -170,6 +170,25 @@ gdn_status gdn_cache_attn(const gdn_tokens *t, const gdn_attn *a, const gdn_rows
                           const gdn_cache *cache, const gdn_rows *o, float *lse, void *workspace,
                           size_t workspace_bytes, void *stream);
 
+/* The same attention where all sequences of the call begin with the same `prefix`
+ * tokens (answers to one prompt, continuations of one document), whose keys are
+ * computed with once for all of them: key j < prefix is in page
+ * prefix_table[j / page_size] (device int32[ceil(prefix / page_size)], an entry
+ * outside the pool is a hole), whatever the sequences' own rows of the table
+ * hold there; later keys are where the table has them.  kv_lens counts the
+ * prefix; a sequence that holds fewer tokens sees those it holds.  prefix
+ * is at most max_blocks * page_size; with 0 it is gdn_cache_attn.
+ * In bfloat16 p is rounded as there, in the prefix's part as for sequences of many
+ * rows unless the call's new tokens x Hq / Hk are at most 32 in all.
+ * The workspace (gdn_cache_attn_shared_workspace_size bytes) holds the partial
+ * results of the prefix and of the sequences' own keys. */
+size_t gdn_cache_attn_shared_workspace_size(const gdn_tokens *t, const gdn_cache *cache,
+                                            const gdn_attn *a, int32_t prefix);
+gdn_status gdn_cache_attn_shared(const gdn_tokens *t, const gdn_attn *a, const gdn_rows *q,
+                                 const gdn_cache *cache, const int32_t *prefix_table,
+                                 int32_t prefix, const gdn_rows *o, float *lse,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- management of the pages, on the device
  *
  * A book of S sequences: table int32[S, max_blocks], lens int32[S] (tokens of

@@ -15,7 +15,9 @@
 // Two kernels from one body:
 //   k_attn_tile  many rows: 4 waves with 32 (or 16) rows each share a tile of keys;
 //   k_attn_few   few rows (at most 32): 4 waves share the rows, each walks its
-//                own keys of a tile and the results are joined in LDS.
+//                own keys of a tile and the results are joined in LDS;
+// and from the same body k_attn_shared_tile and k_attn_shared_few, for the rows of all
+// sequences at a time over the keys of a prefix that they share.
 // Where the row blocks do not fill the GPU, a block's keys are split over
 // several workgroups, whose unnormalised sums k_attn_join adds.
 //
@@ -45,26 +47,38 @@ __device__ inline void dma_rows(const unsigned char* base, unsigned off, unsigne
                : "memory");
 }
 
-// One row block's place in the problem.
-struct Block {
+// One row block's place in the problem.  SHARED: the block's rows are those of all
+// sequences' new tokens (one sequence as far as q0 and m go), its keys the prefix.
+template <bool SHARED> struct Block {
   int n, hk;          // sequence, cache head
   int q0, m;          // first token row of the sequence, its new tokens
   int kv;             // its cached tokens
   int r0, r1;         // rows [r0, r1) of the m * G
   int seen, hi;       // keys that some row sees lie in [seen, hi)
   int lo;             // seen, down to a multiple of 16
+  int all_lo, all_hi; // SHARED: the keys that all rows see
   // first and one past the last key that token i sees
   __device__ int first(const AttnArgs& a, int i) const {
     // (a token before the cache's first sees nothing; its place may not pass 32 bits)
-    return a.window > 0 ? max(0, max(0, kv - m + i + 1) - a.window) : 0;
+    if constexpr (SHARED) return a.window > 0 ? max(0, max(0, place(a, i) + 1) - a.window) : 0;
+    return max(a.from, a.window > 0 ? max(0, max(0, kv - m + i + 1) - a.window) : 0);
   }
   __device__ int last(const AttnArgs& a, int i) const {
+    if constexpr (SHARED) {
+      if (a.causal) return min(a.prefix, max(0, place(a, i) + 1));
+      return min(a.prefix, cached(a.cache, seq_of(a.tok, i)));
+    }
     return a.causal ? max(0, kv - m + i + 1) : kv;
   }
   __device__ void range(const AttnArgs& a) {
     seen = first(a, r0 / a.G);
     lo = seen & ~15;
     hi = min(kv, last(a, (r1 - 1) / a.G));
+  }
+  // SHARED: position of the call's token i (behind the last sequence: before all keys)
+  __device__ static int place(const AttnArgs& a, int i) {
+    const int s = seq_of(a.tok, i), end = seq_start(a.tok, s + 1);
+    return i < end ? cached(a.cache, s) - end + i : -1;
   }
 };
 
@@ -142,8 +156,8 @@ __device__ inline float col_sum(float x) {
 // (a prompt of 8192 tokens, d = 128: 279 us, with 0 306).
 constexpr float SLACK = 8.f;
 
-template <class E, int D, int QT, int RW, int KW, int KT>
-__device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
+template <class E, int D, int QT, int RW, int KW, int KT, bool SHARED>
+__device__ inline void attn_block(const AttnArgs& a, const Block<SHARED>& b, int split,
                                   unsigned char* smem) {
   using C = AttnCfg<E, D, QT, RW, KW, KT>;
   using P = Piece<E>;
@@ -167,11 +181,14 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   const int rw = KW == 1 ? wave : 0, kw = KW == 1 ? 0 : wave;
 
   // the last range goes to the end, however long the cache has become
-  const int begin = b.lo + split * a.len;
-  const int end = split == a.splits - 1 ? b.hi : min(b.hi, begin + a.len);
+  // (SHARED: the same ranges for all blocks, each as far as the block sees it)
+  const int from = SHARED ? split * a.len : b.lo + split * a.len;
+  const int begin = SHARED ? max(from, b.lo) : from;
+  const int end = split == a.splits - 1 ? b.hi : min(b.hi, from + a.len);
   const int tiles = (end - begin + KT - 1) / KT;
 
-  const CONST_AS int* pages = (const CONST_AS int*)(a.cache.table + (int64_t)b.n * a.cache.max_blocks);
+  const CONST_AS int* pages = (const CONST_AS int*)(
+      SHARED ? a.prefix_table : a.cache.table + (int64_t)b.n * a.cache.max_blocks);
   const int shift = a.cache.shift, mask = (1 << shift) - 1, num_pages = a.cache.num_pages;
   const unsigned char* const kbase = a.cache.k + (int64_t)b.hk * a.cache.head;
   const unsigned char* const vbase = a.cache.v + (int64_t)b.hk * a.cache.head;
@@ -241,10 +258,13 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
     last[t] = real ? min(end, b.last(a, i)) : 0;
   }
   // the keys that all rows of the block see, and that some row of the wave sees
-  const int all_lo = b.first(a, (b.r1 - 1) / a.G), all_hi = min(end, b.last(a, b.r0 / a.G));
+  const int all_lo = SHARED ? b.all_lo : b.first(a, (b.r1 - 1) / a.G);
+  const int all_hi = min(end, SHARED ? b.all_hi : b.last(a, b.r0 / a.G));
   const int we = min(b.r1, wr0 + QT * 16) - 1;
   const bool idle = wr0 >= b.r1;
-  const int w_begin = idle ? 0 : b.first(a, wr0 / a.G), w_end = idle ? 0 : min(end, b.last(a, we / a.G));
+  // (SHARED: of the block)
+  const int w_begin = idle ? 0 : SHARED ? b.seen : b.first(a, wr0 / a.G);
+  const int w_end = idle ? 0 : min(end, SHARED ? b.hi : b.last(a, we / a.G));
 
   f32x4 o[DT][QT];
   float m[QT], l[QT];
@@ -494,7 +514,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
   auto put = [&](int r, int ch, f32x4 x, float mm, float ll) {
     const int i = r / a.G, h = b.hk * a.G + r - i * a.G;
     const int64_t at = (int64_t)(b.q0 + i) * a.Hq + h;
-    if (a.splits > 1) {
+    if (a.partial) {
       const int64_t w = split * rows + at;
       *reinterpret_cast<f32x4*>(a.part + w * D + ch) = x;
       if (ch == 0) {
@@ -597,7 +617,7 @@ __device__ inline void attn_block(const AttnArgs& a, const Block& b, int split,
         for (int e = 0; e < N; ++e) {
           const float z = to_f(v[e]);
           if (z - z == 0.f) continue;
-          if (a.splits > 1)
+          if (a.partial)
             w[e] += z;
           else
             y[e] = to_e<E>(to_f(y[e]) + z);
@@ -617,7 +637,7 @@ template <class E, int D, int QT, int KW, int KT>
 __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
   using C = AttnCfg<E, D, QT, 1, KW, KT>;
   __shared__ __align__(1024) unsigned char smem[C::LDS];
-  Block b;
+  Block<false> b;
   b.hk = blockIdx.x % a.Hk;
   const int rest = blockIdx.x / a.Hk, split = rest % a.splits;
   b.n = rest / a.splits;
@@ -631,7 +651,7 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
   b.range(a);
   // a range past the keys: no partial result is read there
   if (split > 0 && b.lo + split * a.len >= b.hi) return;
-  attn_block<E, D, QT, 1, KW, KT>(a, b, split, smem);
+  attn_block<E, D, QT, 1, KW, KT, false>(a, b, split, smem);
 }
 
 // The row block that comes at `rank` when all sequences' blocks are ordered by the
@@ -705,7 +725,7 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
   using C = AttnCfg<E, D, QT, 4, 1, KT>;
   constexpr int R = C::ROWS;
   __shared__ __align__(1024) unsigned char smem[C::LDS];
-  Block b;
+  Block<false> b;
   // A second workgroup for some CUs, but no third for any: they come in reverse, the
   // shortest beside the longest (a prompt of 4096 tokens, 16 heads, d = 128: 111 us, in
   // order 113; of 2048 in fp32, 8 heads, d = 64: 57 and 79, two at d = 128 166 and 259).
@@ -743,7 +763,81 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
   b.kv = cached(a.cache, b.n);
   b.range(a);
   if (split > 0 && b.lo + split * a.len >= b.hi) return;
-  attn_block<E, D, QT, 4, 1, KT>(a, b, split, smem);
+  attn_block<E, D, QT, 4, 1, KT, false>(a, b, split, smem);
+}
+
+// A prefix that all sequences of the call share, its keys read once for a block of rows of
+// all of them: the rows of a cache head are the query heads of every new token.  Only
+// partial sums leave; k_attn_join adds them to those of the sequences' own keys.
+
+// What the block's rows see of the prefix, by `threads` threads.
+template <int THREADS>
+__device__ inline void shared_range(const AttnArgs& a, Block<true>& b, unsigned char* smem) {
+  int lo = 1 << 30, hi = 0, all_lo = 0, all_hi = 1 << 30;
+  // (a row of heads sees the same: a thread a token)
+  for (int i = b.r0 / a.G + (int)threadIdx.x; i <= (b.r1 - 1) / a.G; i += THREADS) {
+    const int f = b.first(a, i), l = b.last(a, i);
+    if (f < l) lo = min(lo, f);
+    hi = max(hi, l);
+    all_lo = max(all_lo, f);
+    all_hi = min(all_hi, l);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    lo = min(lo, __shfl_xor(lo, d));
+    hi = max(hi, __shfl_xor(hi, d));
+    all_lo = max(all_lo, __shfl_xor(all_lo, d));
+    all_hi = min(all_hi, __shfl_xor(all_hi, d));
+  }
+  int4* const x = reinterpret_cast<int4*>(smem);
+  if (lane_id() == 0) x[wave_id()] = make_int4(lo, hi, all_lo, all_hi);
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    const int4 y = x[w];
+    lo = min(lo, y.x);
+    hi = max(hi, y.y);
+    all_lo = max(all_lo, y.z);
+    all_hi = min(all_hi, y.w);
+  }
+  __syncthreads();
+  b.seen = __builtin_amdgcn_readfirstlane(min(lo, hi));
+  b.lo = b.seen & ~15;
+  b.hi = __builtin_amdgcn_readfirstlane(hi);
+  b.all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  b.all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+}
+
+// Grid: split * Hk + hk.
+template <class E, int D, int QT, int KW, int KT>
+__global__ __launch_bounds__(64 * KW, 1) void k_attn_shared_few(AttnArgs a) {
+  using C = AttnCfg<E, D, QT, 1, KW, KT>;
+  __shared__ __align__(1024) unsigned char smem[C::LDS];
+  Block<true> b;
+  b.hk = blockIdx.x % a.Hk;
+  b.n = b.q0 = b.r0 = 0;
+  b.m = a.tok.total;
+  b.kv = a.prefix;
+  b.r1 = b.m * a.G;  // (at most C::ROWS, by the plan)
+  shared_range<64 * KW>(a, b, smem);
+  attn_block<E, D, QT, 1, KW, KT, true>(a, b, blockIdx.x / a.Hk, smem);
+}
+
+// Grid: (tile * splits + split) * Hk + hk.
+template <class E, int D, int QT, int KT>
+__global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_shared_tile(AttnArgs a) {
+  using C = AttnCfg<E, D, QT, 4, 1, KT>;
+  __shared__ __align__(1024) unsigned char smem[C::LDS];
+  Block<true> b;
+  b.hk = blockIdx.x % a.Hk;
+  const int rest = blockIdx.x / a.Hk, tile = rest / a.splits;
+  b.n = b.q0 = 0;
+  b.m = a.tok.total;
+  b.kv = a.prefix;
+  b.r0 = tile * C::ROWS;
+  b.r1 = (int)min((int64_t)b.m * a.G, (int64_t)b.r0 + C::ROWS);
+  shared_range<256>(a, b, smem);
+  attn_block<E, D, QT, 4, 1, KT, true>(a, b, rest - tile * a.splits, smem);
 }
 
 // Joins the splits' sums of a row by T threads: they turn the splits' maxima m_s into
@@ -759,7 +853,8 @@ template <class E, int D, int T> __global__ __launch_bounds__(256) void k_attn_j
   if (at >= rows) return;
   const int tid = PER > 1 ? threadIdx.x % T : threadIdx.x;
   const int t = (int)(at / a.Hq), h = (int)(at - (int64_t)t * a.Hq);
-  Block b;
+  if (a.lead && t >= seq_start(a.tok, a.tok.N)) return;  // behind the last sequence
+  Block<false> b;
   b.n = seq_of(a.tok, t);
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;
@@ -770,7 +865,7 @@ template <class E, int D, int T> __global__ __launch_bounds__(256) void k_attn_j
   b.kv = cached(a.cache, b.n);
   b.range(a);
   // (as a quotient that stays within 32 bits at the longest caches)
-  const int live = b.hi > b.lo ? min(a.splits, (b.hi - b.lo - 1) / a.len + 1) : 1;
+  const int live = a.lead + (b.hi > b.lo ? min(a.splits, (b.hi - b.lo - 1) / a.len + 1) : 1);
 
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
   float mx = -INFINITY, ll = 0.f;
@@ -910,12 +1005,32 @@ hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStrea
   });
 }
 
+hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& a, hipStream_t s) {
+  const int64_t tiles = ((int64_t)a.tok.total * a.G + a.block - 1) / a.block;
+  const unsigned grid = (unsigned)(tiles * a.splits * a.Hk);
+  return by_dim(dt, d, [&](auto e, auto dim) {
+    using E = decltype(e);
+    constexpr int D = decltype(dim)::value;
+    using F = Few<E, D>;
+    constexpr int KT = Tile<E, D>::KT;
+    if (few && a.block == 16)
+      hipLaunchKernelGGL((k_attn_shared_few<E, D, 1, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
+    else if (few)
+      hipLaunchKernelGGL((k_attn_shared_few<E, D, 2, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
+    else if (a.block == 64)
+      hipLaunchKernelGGL((k_attn_shared_tile<E, D, 1, KT>), dim3(grid), dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_attn_shared_tile<E, D, 2, KT>), dim3(grid), dim3(256), 0, s, a);
+    return hipGetLastError();
+  });
+}
+
 hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.tok.total * a.Hq;
   return by_dim(dt, d, [&](auto e, auto dim) {
     using E = decltype(e);
     constexpr int D = decltype(dim)::value, T = D / 4, PER = 256 / T;
-    if (a.splits <= 16)
+    if (a.lead + a.splits <= 16)
       hipLaunchKernelGGL((k_attn_join<E, D, T>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(256),
                          0, s, a);
     else

@@ -141,8 +141,9 @@ struct Plan {
   size_t part = 0, bytes = 0;  // workspace: offset of {maximum, sum}; size
 };
 
+// from: keys before it are not the plan's (a shared prefix).
 gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cache* c,
-                     const gdn_attn* a, Plan* out) {
+                     const gdn_attn* a, int64_t from, Plan* out) {
   if (!a) return GDN_ERR_NULL;
   if (!(a->scale > 0.f) || !isfinite(a->scale) || a->window < 0 || a->max_kv < 0 ||
       (a->window > 0 && !a->causal))
@@ -169,7 +170,8 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
     blocks128 *= tok.N;
   }
   const int64_t room = (int64_t)c->max_blocks * c->page_size;
-  const int64_t kv = std::max<int64_t>(1, a->max_kv > 0 ? std::min<int64_t>(a->max_kv, room) : room);
+  const int64_t kv =
+      std::max<int64_t>(1, (a->max_kv > 0 ? std::min<int64_t>(a->max_kv, room) : room) - from);
   // A block of m tokens sees at most window + m - 1 keys, and its range begins
   // at a multiple of 16.
   auto keys = [&](int64_t m) { return a->window > 0 ? std::min(kv, a->window + m + 14) : kv; };
@@ -270,6 +272,43 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
     p.part = up((size_t)(p.splits * rows * t->d * 4));
     p.bytes = p.part + up((size_t)(p.splits * rows * 8));
   }
+  *out = p;
+  return GDN_OK;
+}
+
+// How the prefix's part is cut: the rows of all sequences in blocks, its keys in ranges, so
+// that there are about as many workgroups as run at once.
+struct SharedPlan {
+  bool few;
+  int block, splits, len;
+  Plan own;                    // the sequences' own keys
+  size_t part, bytes;          // workspace: offset of {maximum, sum}; size
+};
+
+gdn_status plan_shared(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cache* c,
+                       const gdn_attn* a, int32_t prefix, SharedPlan* out) {
+  if (prefix < 1) return GDN_ERR_VALUE;
+  if (prefix > (int64_t)c->max_blocks * c->page_size) return GDN_ERR_SHAPE;
+  SharedPlan p;
+  const gdn_status st = plan_attn(t, tok, c, a, prefix, &p.own);
+  if (st != GDN_OK) return st;
+  const Dt dt = type_of(t->dtype);
+  const int64_t rows = (int64_t)tok.total * (t->Hq / t->Hk);  // of a cache head
+  if (rows >= (int64_t)1 << 30) return GDN_ERR_SHAPE;
+  p.few = rows <= gdn::FEW_ROWS;
+  p.block = p.few ? (rows <= 16 ? 16 : 32) : rows <= 64 ? 64 : 128;
+  const int step = p.few ? gdn::attn_few_keys(dt, t->d) : gdn::attn_tile_keys(dt, t->d);
+  const int64_t units = (rows + p.block - 1) / p.block * t->Hk;
+  const int64_t want = p.few || size_of(t->dtype) * t->d > 512 ? 256 : 512;
+  const int64_t most = std::min<int64_t>(gdn::MAX_SPLITS - p.own.splits, (prefix + step - 1) / step);
+  const int64_t splits = std::max<int64_t>(1, std::min(want / std::max<int64_t>(1, units), most));
+  p.len = (int)(((prefix + splits - 1) / splits + step - 1) / step * step);
+  p.splits = (int)((prefix - 1) / p.len + 1);
+  // a launch holds less than 2^32 threads, 256 to a workgroup
+  if (units * p.splits >= (int64_t)1 << 24) return GDN_ERR_SHAPE;
+  const int64_t all = (int64_t)tok.total * t->Hq, parts = p.splits + p.own.splits;
+  p.part = up((size_t)(parts * all * t->d * 4));
+  p.bytes = p.part + up((size_t)(parts * all * 8));
   *out = p;
   return GDN_OK;
 }
@@ -416,7 +455,7 @@ size_t gdn_cache_attn_workspace_size(const gdn_tokens* t, const gdn_cache* cache
   gdn::Cache c;
   Plan p;
   if (check_tokens(t, &tok) != GDN_OK || check_cache(cache, 1, false, &c) != GDN_OK ||
-      plan_attn(t, tok, cache, a, &p) != GDN_OK)
+      plan_attn(t, tok, cache, a, 0, &p) != GDN_OK)
     return 0;
   return p.bytes;
 }
@@ -434,7 +473,7 @@ gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_row
   if ((st = check_rows(o, esz, &a.o)) != GDN_OK) return st;
   if (!aligned(lse, 4)) return GDN_ERR_ALIGN;
   Plan p;
-  if ((st = plan_attn(t, a.tok, cache, at, &p)) != GDN_OK) return st;
+  if ((st = plan_attn(t, a.tok, cache, at, 0, &p)) != GDN_OK) return st;
   if (p.bytes) {
     if (!workspace || workspace_bytes < p.bytes) return GDN_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return GDN_ERR_ALIGN;
@@ -454,10 +493,80 @@ gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_row
   a.splits = p.splits;
   a.len = p.len;
   a.longest = p.longest;
+  a.partial = p.splits > 1;
   hipError_t e = p.few ? gdn::launch_attn_few(dt, t->d, a, s)
                        : gdn::launch_attn_tile(dt, t->d, (int)p.slots, a, s);
   if (e == hipSuccess && p.splits > 1) e = gdn::launch_attn_join(dt, t->d, a, s);
   return done(e);
+}
+
+size_t gdn_cache_attn_shared_workspace_size(const gdn_tokens* t, const gdn_cache* cache,
+                                            const gdn_attn* a, int32_t prefix) {
+  if (prefix == 0) return gdn_cache_attn_workspace_size(t, cache, a);
+  gdn::Tokens tok;
+  gdn::Cache c;
+  SharedPlan p;
+  if (check_tokens(t, &tok) != GDN_OK || check_cache(cache, 1, false, &c) != GDN_OK ||
+      plan_shared(t, tok, cache, a, prefix, &p) != GDN_OK)
+    return 0;
+  return p.bytes;
+}
+
+gdn_status gdn_cache_attn_shared(const gdn_tokens* t, const gdn_attn* at, const gdn_rows* q,
+                                 const gdn_cache* cache, const int32_t* prefix_table,
+                                 int32_t prefix, const gdn_rows* o, float* lse, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  if (prefix == 0) return gdn_cache_attn(t, at, q, cache, o, lse, workspace, workspace_bytes, stream);
+  AttnArgs a;
+  memset(&a, 0, sizeof a);
+  gdn_status st = check_tokens(t, &a.tok);
+  if (st != GDN_OK) return st;
+  const int esz = size_of(t->dtype);
+  if ((st = check_cache(cache, esz, true, &a.cache)) != GDN_OK) return st;
+  if ((st = check_rows(q, esz, &a.q)) != GDN_OK) return st;
+  if ((st = check_rows(o, esz, &a.o)) != GDN_OK) return st;
+  if (!prefix_table) return GDN_ERR_NULL;
+  if (!aligned(lse, 4) || !aligned(prefix_table, 4)) return GDN_ERR_ALIGN;
+  SharedPlan p;
+  if ((st = plan_shared(t, a.tok, cache, at, prefix, &p)) != GDN_OK) return st;
+  if (!workspace || workspace_bytes < p.bytes) return GDN_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return GDN_ERR_ALIGN;
+  const Dt dt = type_of(t->dtype);
+  const hipStream_t s = (hipStream_t)stream;
+  const int64_t rows = (int64_t)a.tok.total * t->Hq;
+  a.part = (float*)workspace;
+  a.part_ml = (float*)((unsigned char*)workspace + p.part);
+  a.partial = 1;
+  a.lse = lse;
+  a.Hq = t->Hq;
+  a.Hk = t->Hk;
+  a.G = t->Hq / t->Hk;
+  a.causal = at->causal != 0;
+  a.window = at->window;
+  a.c = at->scale * 1.4426950408889634f;
+  // the prefix
+  AttnArgs b = a;
+  b.prefix_table = prefix_table;
+  b.prefix = prefix;
+  b.block = p.block;
+  b.splits = p.splits;
+  b.len = p.len;
+  hipError_t e = gdn::launch_attn_shared(dt, t->d, p.few, b, s);
+  if (e != hipSuccess) return GDN_ERR_HIP;
+  // the sequences' own keys, their sums behind the prefix's
+  a.from = prefix;
+  a.block = p.own.block;
+  a.splits = p.own.splits;
+  a.len = p.own.len;
+  a.longest = p.own.longest;
+  b = a;
+  b.part += p.splits * rows * t->d;
+  b.part_ml += p.splits * rows * 2;
+  e = p.own.few ? gdn::launch_attn_few(dt, t->d, b, s)
+                : gdn::launch_attn_tile(dt, t->d, (int)p.own.slots, b, s);
+  if (e != hipSuccess) return GDN_ERR_HIP;
+  a.lead = p.splits;
+  return done(gdn::launch_attn_join(dt, t->d, a, s));
 }
 
 size_t gdn_pages_workspace_size(const gdn_book* b) {

@@ -55,6 +55,12 @@ struct AttnArgs {
   int block;        // rows of a block
   int splits, len;  // key ranges of `len` keys (the last: all that follow)
   int longest;      // row blocks of all sequences in the order of their keys
+  int from;         // the sequences' own keys: keys before it are not seen
+  int partial;      // sums go to part
+  // A prefix that the sequences share: keys [0, prefix) are in these pages, for all.
+  const int32_t* prefix_table;
+  int prefix;
+  int lead;         // join: partial sums of the prefix ahead of a row's own
 };
 // Calls whose sequences have at most this many rows (new tokens x query heads of a
 // cache head) take the kernel whose waves share the rows and split the keys.
@@ -68,6 +74,8 @@ int attn_tile_keys(Dt dt, int d);
 hipError_t launch_attn_few(Dt dt, int d, const AttnArgs& a, hipStream_t s);
 // a.block: 64 or 128 rows; slots: row blocks
 hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStream_t s);
+// the rows of all sequences over the prefix (few: at most FEW_ROWS of a cache head, as a.block)
+hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s);
 
 struct Book {

@@ -26,7 +26,8 @@ import torch
 from .gdn import _check, _cu_pair, _ptr, _stream, load_library as _load
 
 EXPORTS = ("gdn_rotary_turns", "gdn_rotary_fwd", "gdn_rotary_bwd", "gdn_cache_append",
-           "gdn_cache_attn", "gdn_cache_attn_workspace_size", "gdn_pages_workspace_size",
+           "gdn_cache_attn", "gdn_cache_attn_workspace_size", "gdn_cache_attn_shared",
+           "gdn_cache_attn_shared_workspace_size", "gdn_pages_workspace_size",
            "gdn_pages_extend", "gdn_pages_select", "gdn_pages_compact", "gdn_pages_copy")
 
 LAYOUTS = {"halves": 0, "interleaved": 1}
@@ -102,6 +103,8 @@ def load_library():
                 ("gdn_cache_append", [P] * 8),
                 ("gdn_cache_attn", [P] * 7 + [S, P]),
                 ("gdn_cache_attn_workspace_size", [P] * 3),
+                ("gdn_cache_attn_shared", [P] * 5 + [I] + [P] * 3 + [S, P]),
+                ("gdn_cache_attn_shared_workspace_size", [P] * 3 + [I]),
                 ("gdn_pages_workspace_size", [P]),
                 ("gdn_pages_extend", [P] * 4 + [S, P]),
                 ("gdn_pages_select", [P] * 5 + [S, P]),
@@ -300,6 +303,12 @@ def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True,
     which the launches are sized by.  ``lse`` float32 [B, T, Hq] receives the log of each softmax's
     sum.  A token that sees no key gets 0 (lse -inf), and so do those of a sequence with a non-zero
     entry in ``skip`` (as in gdn_cache_append)."""
+    return _attend(q, k_pages, v_pages, table, kv_lens, None, 0, scale, causal, window, max_kv,
+                   cu_seqlens, cu_seqlens_host, o, lse, workspace, skip)
+
+
+def _attend(q, k_pages, v_pages, table, kv_lens, prefix_table, prefix, scale, causal, window,
+            max_kv, cu_seqlens, cu_seqlens_host, o, lse, workspace, skip):
     lib = load_library()
     keep = []
     rq = _n.first("q", q)
@@ -316,7 +325,10 @@ def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True,
                             or not lse.is_contiguous() or lse.shape != q.shape[:3]):
         raise ValueError("lse must be contiguous float32 [B, T, Hq] on q's device")
     a = _attn(scale, d, causal, window, max_kv)
-    need = lib.gdn_cache_attn_workspace_size(t, c, a)
+    if prefix_table is None:
+        need = lib.gdn_cache_attn_workspace_size(t, c, a)
+    else:
+        need = lib.gdn_cache_attn_shared_workspace_size(t, c, a, prefix)
     ws, size = None, 0
     if need:
         if workspace is None or workspace.numel() < need:
@@ -325,8 +337,51 @@ def gdn_cache_attn(q, k_pages, v_pages, table, kv_lens, scale=None, causal=True,
               or not workspace.is_contiguous()):
             raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
         ws, size = workspace.data_ptr(), workspace.numel()
-    _check(lib.gdn_cache_attn(t, a, rq, c, ro, _ptr(lse), ws, size, _stream(dev)))
+    if prefix_table is None:
+        _check(lib.gdn_cache_attn(t, a, rq, c, ro, _ptr(lse), ws, size, _stream(dev)))
+        return o
+    pt = _n.ints("prefix_table", prefix_table, q)
+    if prefix > prefix_table.numel() * k_pages.shape[2]:
+        raise ValueError("prefix_table must hold the pages of %d tokens" % prefix)
+    _check(lib.gdn_cache_attn_shared(t, a, rq, c, pt, prefix, ro, _ptr(lse), ws, size,
+                                     _stream(dev)))
     return o
+
+
+def gdn_cache_attn_shared_workspace_size(q, k_pages, table, prefix, scale=None, causal=True,
+                                         window=0, max_kv=0, cu_seqlens=None,
+                                         cu_seqlens_host=None) -> int:
+    """Workspace bytes of gdn_cache_attn_shared with these arguments."""
+    keep = []
+    _n.first("q", q)
+    B, _, Hq, d = q.shape
+    n = B if cu_seqlens is None else cu_seqlens.shape[0] - 1
+    c = _n.cache("q", q, k_pages, k_pages, table, None, n, None)
+    t = _tokens(q, Hq, k_pages.shape[1], cu_seqlens, cu_seqlens_host, q.device, keep)
+    return int(load_library().gdn_cache_attn_shared_workspace_size(
+        t, c, _attn(scale, d, causal, window, max_kv), _prefix(prefix)))
+
+
+def _prefix(prefix):
+    prefix = int(prefix)
+    if not 0 <= prefix <= 0x7fffffff:
+        raise ValueError("prefix must be a number of tokens")
+    return prefix
+
+
+def gdn_cache_attn_shared(q, k_pages, v_pages, table, kv_lens, prefix_table, prefix, scale=None,
+                          causal=True, window=0, max_kv=0, cu_seqlens=None, cu_seqlens_host=None,
+                          o=None, lse=None, workspace=None, skip=None):
+    """gdn_cache_attn where all sequences begin with the same ``prefix`` tokens, whose keys are
+    read and multiplied once for all of them; returns o.
+
+    ``prefix_table`` int32 [blocks]: the prefix's pages (a row of a table that holds it: what
+    gdn_pages_select leaves in every fork of a prompt).  A sequence's own row of ``table`` is read
+    from the prefix's end on; kv_lens counts the prefix.  The rest as in gdn_cache_attn."""
+    if not isinstance(prefix_table, torch.Tensor):
+        raise TypeError("prefix_table must be a tensor")
+    return _attend(q, k_pages, v_pages, table, kv_lens, prefix_table, _prefix(prefix), scale,
+                   causal, window, max_kv, cu_seqlens, cu_seqlens_host, o, lse, workspace, skip)
 
 
 # ------------------------------------------------------------------ pages
