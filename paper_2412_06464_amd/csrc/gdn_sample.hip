@@ -4,9 +4,11 @@
 // One workgroup a row.  All that a draw needs are places in the order of falling
 // logits: the k-th token, the one where the sum of weights reaches top_p of it, the
 // one where it passes u times the sum of what is kept (min_p needs none: what it
-// keeps is a prefix too, and the shortest prefix has the smallest sum).  A histogram over
-// the logarithm of the weight, with counts and sums, says in which bin a place lies;
-// the bin's tokens are gathered, sorted and summed.  No row is sorted.
+// keeps is a prefix too, and the shortest prefix has the smallest sum).  No row is sorted:
+//   - with a top_k of few tokens, the k-th largest of the threads' largest logits is a
+//     bound that the k largest reach; what reaches it is gathered and sorted;
+//   - otherwise a histogram of weights over their logarithm says in which bin a place lies,
+//     and the bin's tokens (or all up to there, where they are few) are gathered.
 //
 // Weights are whole multiples of 2^-42 of the largest (found with an exponential in 64
 // bits), so that sums are exact, whatever their order, atomics included, and two
@@ -24,11 +26,17 @@ namespace {
 using gdn::lane_id;
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
+// (a lambda that is called keeps what it refers to in memory)
+#define INLINE __attribute__((always_inline))
 
 constexpr int NTH = 1024, NW = NTH / 64;
-constexpr int BINS = 2048, CAP = 2048;  // of a histogram; tokens gathered at a time
+constexpr int BINS = 2048, CAP = 2048;  // of a histogram; tokens of the list
+constexpr int FEW = 512;                // top_k up to which the list is tried first
 constexpr double LOWEST = -43;          // log2 of the least weight that counts
 constexpr int SCALE = 42;               // weights are multiples of 2^-SCALE
+// log2 of the weights that have bins of their own: with 16 one draw in 200 from a normal
+// distribution (of 2.5 at T = 1, 128,000 tokens) was from the last bin, and took another histogram
+constexpr double RANGE = 22;
 constexpr unsigned INDEX = (1u << 20) - 1;
 
 struct SampleArgs {
@@ -52,62 +60,64 @@ __device__ inline float value_of(unsigned r) {
 __device__ inline u64 place_of(float x, int i) {
   return (u64)rank_of(x) << 20 | (INDEX - (unsigned)i);
 }
-
-struct Scale {
-  float top;       // the largest logit
-  double per;      // log2(e) / T
-  // log2 of the weight of x; below LOWEST (or NaN): none
-  __device__ double log2w(float x) const {
-    if (isinf(top)) return x == top ? 0.0 : -1e9;
-    return ((double)x - (double)top) * per;
-  }
-};
-
-// 2^y in units of 2^-SCALE, LOWEST <= y <= 0: e^(f ln 2) for |f| <= 1/2 by its Taylor
-// series, whose first term left out is 2e-13, under a unit of the largest weight.
-__device__ inline u64 weight(double y) {
-  const double n = __builtin_rint(y), f = (y - n) * 0.6931471805599453;
-  double p = 1.0 / 3628800;
-  p = __builtin_fma(p, f, 1.0 / 362880);
-  p = __builtin_fma(p, f, 1.0 / 40320);
-  p = __builtin_fma(p, f, 1.0 / 5040);
-  p = __builtin_fma(p, f, 1.0 / 720);
-  p = __builtin_fma(p, f, 1.0 / 120);
-  p = __builtin_fma(p, f, 1.0 / 24);
-  p = __builtin_fma(p, f, 1.0 / 6);
-  p = __builtin_fma(p, f, 0.5);
-  p = __builtin_fma(p, f, 1.0);
-  p = __builtin_fma(p, f, 1.0);
-  // rounded to a whole number by the addition
-  const double v = __builtin_ldexp(p, (int)n + SCALE) + 4503599627370496.0;
-  return (u64)__double_as_longlong(v) & 0xfffffffffffffull;
-}
-
-struct Found {
-  int j;         // bin
-  u64 before;    // sum of what comes before it
-  unsigned n;    // and how many
-};
+__device__ inline float value_at(u64 place) { return value_of((unsigned)(place >> 20)); }
 
 struct Shared {
-  unsigned count[2][BINS];
-  u64 sum[2][BINS];
-  u64 list[CAP];
+  double power[128];  // 2^(SCALE + j / 128)
+  unsigned count[BINS];
+  // (the last bin's, of the many small weights, in a place for each lane)
+  u64 sum[BINS - 1 + 64];
+  u64 list[CAP];  // places
+  u64 run[CAP];   // sums of weights up to each
   u64 part[2][NW];
-  unsigned partc[NW];
+  unsigned votes[16][3];
   unsigned listed;
   int at;
-  u64 before;
-  unsigned nbefore;
-  u64 lo, hi;
+  u64 before, nbefore, lo, hi;
 };
 
-__device__ inline u64 wave_scan(u64 x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 y = __shfl_up(x, d, 64);
-    if (lane_id() >= d) x += y;
+struct Scale {
+  double top;  // the largest logit
+  double per;  // log2(e) / T
+  // (an infinity: so far above all that is finite that nothing of that has weight)
+  __device__ Scale(float x, float T)
+      : top(x == INFINITY ? 1e39 : (double)x),
+        per(x == INFINITY ? 1e300 : 1.4426950408889634074 / (double)T) {}
+  // log2 of the weight; NONE where there is none (NaN, or below LOWEST)
+  __device__ double log2w(float x) const {
+    return __builtin_fmin(__builtin_fmax(((double)x - top) * per, NONE), 0.0);
   }
+  static constexpr double NONE = -64;
+};
+
+// 2^y in units of 2^-SCALE, y <= 0 (0 at NONE), from a table of 2^(j / 128) and the Taylor series
+// of the rest, whose first term left out is 2.2e-12 at most.
+__device__ inline u64 weight(const Shared& s, double y) {
+  // the sum's last bits are round(128 y)
+  const double shift = 0x1.8p45, z = y + shift, f = y - (z - shift);
+  const int i = (int)__double_as_longlong(z);
+  double p = __builtin_fma(f, 0.05550410866482158, 0.2402265069591007);
+  p = __builtin_fma(p, f, 0.6931471805599453);
+  p = __builtin_fma(p, f, 1.0);
+  const long long t = __double_as_longlong(s.power[i & 127]) + ((long long)((i << 13) & 0xfff00000) << 32);
+  // rounded to a whole number by the addition
+  return (u64)__double_as_longlong(__builtin_fma(p, __longlong_as_double(t), 0x1p52)) &
+         0xfffffffffffffull;
+}
+
+// Inclusive prefix sums over the 64 lanes (as in rows of 16 lanes, then across them).
+template <int CTRL, int ROWS> __device__ inline u64 dpp_or_zero(u64 x) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false);
+  return (u64)(unsigned)hi << 32 | (unsigned)lo;
+}
+__device__ inline u64 wave_scan(u64 x) {
+  x += dpp_or_zero<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
+  x += dpp_or_zero<0x112, 0xf>(x);
+  x += dpp_or_zero<0x114, 0xf>(x);
+  x += dpp_or_zero<0x118, 0xf>(x);
+  x += dpp_or_zero<0x142, 0xa>(x);  // row_bcast 15, to rows 1 and 3
+  x += dpp_or_zero<0x143, 0xc>(x);  // row_bcast 31, to rows 2 and 3
   return x;
 }
 
@@ -126,6 +136,17 @@ __device__ inline void block_scan(Shared& s, u64& x, u64& c) {
     x += s.part[0][i];
     c += s.part[1][i];
   }
+}
+// The sum over the workgroup's threads, for all of them.
+__device__ inline u64 block_sum(Shared& s, u64 x) {
+  x = wave_scan(x);
+  __syncthreads();
+  if (lane_id() == 63) s.part[0][threadIdx.x >> 6] = x;
+  __syncthreads();
+  u64 all = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) all += s.part[0][i];
+  return all;
 }
 
 // A row's logits, 16 bytes a thread at a time; what is past its ends is NaN.
@@ -162,13 +183,15 @@ template <class E> struct Row {
   }
 };
 
+// 64 rows of 100,000 in fp32, top_p: bound by the histogram's 64-bit exponentials, an instruction
+// for 64 tokens each; with a small top_k by two passes over the row, the second from cache.
 template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a) {
   constexpr int N = Row<E>::N;
   __shared__ Shared s;
   const int tid = threadIdx.x, wave = tid >> 6, r = blockIdx.x;
   const Row<E> row(a.logits + r * a.stride, a.vocab);
   // f(x, index) for this thread's tokens; two loads ahead.  Whole waves take part.
-  auto each = [&](auto&& f) {
+  auto each = [&](auto&& f) INLINE {
     u32x4 x = row.load(tid), y = row.load(tid + NTH);
 #pragma unroll 1
     for (int j = tid; j - tid < row.pieces; j += NTH) {
@@ -180,21 +203,33 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     }
   };
 
-  // the largest, the lowest index first
+  // the largest, the lowest index first; the smallest
+  float mine = -INFINITY, low = INFINITY;
   u64 best = 0;
   {
-    float top = -INFINITY;
     int at = -1;
-    each([&](float x, int i) {
-      if (x > top) top = x, at = i;
+    each([&](float x, int i) INLINE {
+      low = fminf(low, x);
+      if (x > mine) mine = x, at = i;
     });
-    if (at >= 0) best = place_of(top, at);
+    if (at >= 0) best = place_of(mine, at);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) best = max(best, (u64)__shfl_xor(best, d, 64));
-    if (lane_id() == 0) s.part[0][wave] = best;
+    for (int d = 1; d < 64; d <<= 1) {
+      best = max(best, (u64)__shfl_xor(best, d, 64));
+      low = fminf(low, __shfl_xor(low, d, 64));
+    }
+    if (lane_id() == 0) {
+      s.part[0][wave] = best;
+      s.part[1][wave] = __float_as_uint(low);
+    }
+    if (tid < 128) s.power[tid] = exp2(SCALE + tid / 128.0);
+    if (tid < 48) s.votes[tid / 3][tid % 3] = 0;
     __syncthreads();
-    for (int i = 0; i < NW; ++i) best = max(best, s.part[0][i]);
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      best = max(best, s.part[0][i]);
+      low = fminf(low, __uint_as_float((unsigned)s.part[1][i]));
+    }
   }
   const float T = a.temperature ? a.temperature[r] : 1.f;
   if (best == 0 || !(T > 0.f)) {  // nothing to draw, or no draw
@@ -204,288 +239,362 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     }
     return;
   }
-  const Scale sc{value_of((unsigned)(best >> 20)), 1.4426950408889634074 / (double)T};
+  const Scale sc(value_at(best), T);
   const int k = a.top_k ? a.top_k[r] : 0;
   const double p = a.top_p ? (double)a.top_p[r] : 1.0, mp = a.min_p ? (double)a.min_p[r] : 0.0;
   const float un = a.u ? a.u[r] : 0.f;
   const double u = un > 0.f ? fmin((double)un, 1 - 0x1p-24) : 0.0;
   const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.0, by_m = mp > 0.0;
 
-  const double per_bin = -BINS / (1 - LOWEST);
-  auto bin_of = [&](double y) { return (int)(y * per_bin); };  // y in [LOWEST, 0]
-
-  auto clear = [&](int h) {
-    for (int i = tid; i < BINS; i += NTH) {
-      s.count[h][i] = 0;
-      s.sum[h][i] = 0;
-    }
-    __syncthreads();
-  };
-  // one token into histogram h; what a whole wave has in one bin goes there at once
-  auto add = [&](int h, bool in, int b, bool sums, u64 w) {
-    const u64 who = __ballot(in);
-    if (!who) return;
-    const int first = __builtin_amdgcn_readlane(b, __ffsll(who) - 1);
-    if (__popcll(who) > 8 && __ballot(in && b == first) == who) {
-      u64 x = in ? w : 0;
-      if (sums)
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
-      if (lane_id() == 0) {
-        atomicAdd(&s.count[h][first], (unsigned)__popcll(who));
-        if (sums) atomicAdd(&s.sum[h][first], x);
-      }
-    } else if (in) {
-      atomicAdd(&s.count[h][b], 1u);
-      if (sums) atomicAdd(&s.sum[h][b], w);
-    }
-  };
-  u64 kept_m = 0;  // sum of the weights that min_p keeps
-  auto histogram = [&](bool sums) {
-    clear(0);
-    u64 mine = 0;
-    each([&](float x, int) {
-      const double y = sc.log2w(x);
-      const bool in = y >= LOWEST;
-      u64 w = 0;
-      if (sums && in) {
-        w = weight(y);
-        if (by_m && (double)w >= mp * 0x1p42) mine += w;
-      }
-      add(0, in, in ? bin_of(y) : 0, sums, w);
-    });
-    __syncthreads();
-    if (sums && by_m) {
-      u64 none = 0;
-      block_scan(s, mine, none);
-      __syncthreads();
-      if (tid == NTH - 1) s.before = mine;
-      __syncthreads();
-      kept_m = s.before;
-    }
-  };
-
-  // The first bin of histogram h up to which, `base` and `nbase` before it, test(sum, count)
-  // holds; the last that holds anything if none does.
-  auto find_bin = [&](int h, u64 base, u64 nbase, auto&& test) {
-    u64 x[2], c[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = s.sum[h][2 * tid + i], c[i] = s.count[h][2 * tid + i];
-    u64 sx = x[0] + x[1], scn = c[0] + c[1];
-    block_scan(s, sx, scn);
-    if (tid == 0) s.at = BINS;
-    __syncthreads();
-    u64 before = base + sx - x[0] - x[1], n = nbase + scn - c[0] - c[1];
-    int mine = BINS;
-    u64 mb = 0, mn = 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (mine == BINS && c[i] && test(before + x[i], n + c[i])) mine = 2 * tid + i, mb = before, mn = n;
-      before += x[i];
-      n += c[i];
-    }
-    if (mine < BINS) atomicMin(&s.at, mine);
-    __syncthreads();
-    if (s.at == BINS) {  // (never for a sum that the caller has from the same histogram)
-      __syncthreads();
-      if (tid == 0) s.at = -1;
-      __syncthreads();
-      const int last = c[1] ? 2 * tid + 1 : c[0] ? 2 * tid : -1;
-      if (last >= 0) atomicMax(&s.at, last);
-      __syncthreads();
-      if (last >= 0 && last == s.at) mine = last, mb = before - x[last & 1], mn = n - c[last & 1];
-    }
-    if (mine == s.at) {
-      s.before = mb;
-      s.nbefore = (unsigned)mn;
-    }
-    __syncthreads();
-    const Found f{s.at, s.before, s.nbefore};
-    __syncthreads();
-    return f;
-  };
-
-  // Gathers the tokens for which in(y, place) holds, at most CAP, and sorts them.
-  auto gather = [&](auto&& in) {
+  // Gathers the tokens for which in(x, index) holds; how many they are (they are all in the list
+  // if that is at most CAP).
+  auto gather = [&](auto&& in) INLINE {
     if (tid == 0) s.listed = 0;
     __syncthreads();
-    each([&](float x, int i) {
-      const double y = sc.log2w(x);
-      if (!(y >= LOWEST)) return;
-      const u64 c = place_of(x, i);
-      if (in(y, c)) {
+    each([&](float x, int i) INLINE {
+      if (in(x, i)) {
         const unsigned at = atomicAdd(&s.listed, 1u);
-        if (at < CAP) s.list[at] = c;
+        if (at < CAP) s.list[at] = place_of(x, i);
       }
     });
     __syncthreads();
-    const int n = min((int)s.listed, CAP);
-    if (n <= 512) {  // each finds its place by comparing with all others
-      const u64 mine = tid < n ? s.list[tid] : 0;
-      int at = 0;
-      if (tid < n)
-        for (int i = 0; i < n; ++i) at += s.list[i] > mine;
-      __syncthreads();
-      if (tid < n) s.list[at] = mine;
-      __syncthreads();
-      return n;
-    }
-    const int m = n <= 1024 ? 1024 : 2048;
-    for (int i = n + tid; i < m; i += NTH) s.list[i] = 0;
+    const int n = (int)s.listed;
     __syncthreads();
-    for (int size = 2; size <= m; size <<= 1)
-      for (int step = size >> 1; step > 0; step >>= 1) {
-        if (tid < m / 2) {
-          const int i = 2 * tid - (tid & (step - 1)), j = i + step;
-          const u64 x = s.list[i], y = s.list[j];
-          if ((x < y) == ((i & size) == 0)) s.list[i] = y, s.list[j] = x;
-        }
-        __syncthreads();
-      }
     return n;
   };
-  // The first token of the sorted list up to which test(sum, count) holds (the last if none
-  // does): its place, and the sum with it.
+  // Sorts the list's n tokens, and sums their weights up to each from `base` on.
+  auto sort = [&](int n, u64 base) INLINE {
+    if (n <= 512) {  // each finds its place by comparing with all others
+      const u64 x = tid < n ? s.list[tid] : 0;
+      int at = 0;
+      if (tid < n)
+        for (int i = 0; i < n; ++i) at += s.list[i] > x;
+      __syncthreads();
+      if (tid < n) s.list[at] = x;
+      __syncthreads();
+    } else {
+      const int m = n <= 1024 ? 1024 : 2048;
+      for (int i = n + tid; i < m; i += NTH) s.list[i] = 0;
+      __syncthreads();
+      for (int size = 2; size <= m; size <<= 1)
+        for (int step = size >> 1; step > 0; step >>= 1) {
+          if (tid < m / 2) {
+            const int i = 2 * tid - (tid & (step - 1)), j = i + step;
+            const u64 x = s.list[i], y = s.list[j];
+            if ((x < y) == ((i & size) == 0)) s.list[i] = y, s.list[j] = x;
+          }
+          __syncthreads();
+        }
+    }
+    u64 w[2], none = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w[i] = 2 * tid + i < n ? weight(s, sc.log2w(value_at(s.list[2 * tid + i]))) : 0;
+    u64 x = w[0] + w[1];
+    block_scan(s, x, none);
+    x += base;
+    s.run[2 * tid] = x - w[1];
+    s.run[2 * tid + 1] = x;
+    __syncthreads();
+  };
+  // What is looked for: the token with which the count reaches n, the sum `want`, or passes it.
+  enum Kind { COUNT, REACHES, PASSES };
+  struct Target {
+    Kind kind;
+    u64 n;
+    double want;
+    __device__ bool operator()(u64 sum, u64 count) const {
+      if (kind == COUNT) return count >= n;
+      return kind == REACHES ? (double)sum >= want && sum > 0 : (double)sum > want;
+    }
+  };
+  // The first token of the sorted list up to which the test holds (the last if none does): its
+  // place, and the sum with it.
   u64 got_place = 0, got_sum = 0;
-  auto find_listed = [&](int n, u64 base, u64 nbase, auto&& test) {
-    u64 w[2], c[2];
+  auto find_listed = [&](int n, u64 nbase, const Target& test) INLINE {
+    if (tid == 0) s.at = max(n - 1, 0);
+    __syncthreads();
+    bool was = tid > 0 && 2 * tid <= n && test(s.run[2 * tid - 1], nbase + 2 * tid);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      c[i] = 2 * tid + i < n;
-      w[i] = c[i] ? weight(sc.log2w(value_of((unsigned)(s.list[2 * tid + i] >> 20)))) : 0;
+      const int j = 2 * tid + i;
+      const bool is = j < n && test(s.run[j], nbase + j + 1);
+      if (is && !was) s.at = j;
+      was = is;
     }
-    u64 x = w[0] + w[1], cn = c[0] + c[1];
-    block_scan(s, x, cn);
-    if (tid == 0) s.at = n - 1;
-    __syncthreads();
-    u64 sum = base + x - w[0] - w[1], cnt = nbase + cn - c[0] - c[1];
-    u64 sums[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      sum += w[i];
-      cnt += c[i];
-      sums[i] = sum;
-      if (c[i] && test(sum, cnt)) atomicMin(&s.at, 2 * tid + i);
-    }
-    __syncthreads();
-    if (s.at >> 1 == tid) s.before = sums[s.at & 1];
     __syncthreads();
     got_place = s.list[s.at];
-    got_sum = s.before;
+    got_sum = s.run[s.at];
     __syncthreads();
   };
-  // The same among the tokens of bin f.j, which may be more than the list holds: their places,
-  // which are all different, are cut ever finer.
-  auto find_in_bin = [&](const Found& f, auto&& test) {
-    unsigned n = s.count[0][f.j];
-    u64 lo = 0, hi = ~0ull, base = f.before, nbase = f.n;
+
+  // ---- few tokens, by a bound that the k largest reach
+  int listed = 0;  // tokens of the list, if it holds all that can be kept
+  u64 total = 0, kept_m = 0;
+  const Target reaches_k{COUNT, (u64)max(k, 0), 0};
+  if (by_k && k <= FEW) {
+    // the k-th largest of the threads' largest, two bits at a time (0: fewer have any)
+    const unsigned own = mine > -INFINITY ? rank_of(mine) : 0;
+    unsigned bound = 0;
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i) {
+      const int at = 30 - 2 * i;
+#pragma unroll
+      for (unsigned c = 0; c < 3; ++c) {
+        const int n = __popcll(__ballot(own >= (bound | (c + 1) << at)));
+        if (lane_id() == 0 && n) atomicAdd(&s.votes[i][c], (unsigned)n);
+      }
+      __syncthreads();
+      unsigned digit = 0;
+#pragma unroll
+      for (unsigned c = 0; c < 3; ++c) digit += s.votes[i][c] >= (unsigned)k;
+      bound |= digit << at;
+    }
+    const float least = bound ? value_of(bound) : -INFINITY;
+    const int n = gather([&](float x, int) INLINE { return x >= least; });
+    if (n <= CAP) {
+      listed = n;
+      sort(n, 0);
+      find_listed(n, 0, reaches_k);
+      total = got_sum;
+      if (by_m) {
+        u64 x = 0;
+        for (int i = tid; i < n; i += NTH) {
+          const u64 w = s.run[i] - (i ? s.run[i - 1] : 0);
+          if ((double)w >= mp * 0x1p42) x += w;
+        }
+        kept_m = block_sum(s, x);
+      }
+    }
+  }
+
+  // ---- otherwise by a histogram: bins of equal width in log2 of the weight, from `first` on, as
+  // fine as the row's range has it; the last takes all that is below
+  double first = 0, fine = 0;
+  auto binned = [](double y, double first, double fine) INLINE {
+    return (int)fmax(0.0, fmin((first - y) * fine, BINS - 1.0));
+  };
+  auto bin_of = [&](double y) INLINE { return binned(y, first, fine); };
+  // Sums of the weights for which bin_if(x, index, y) is not negative, and their counts if by_k.
+  auto histogram = [&](auto&& bin_if) INLINE {
+    for (int i = tid; i < BINS - 1 + 64; i += NTH) s.sum[i] = 0;
+    for (int i = tid; i < BINS; i += NTH) s.count[i] = 0;
+    __syncthreads();
+    auto fill = [&](auto counts, auto keeps) INLINE {
+      each([&](float x, int i) INLINE {
+        const double y = sc.log2w(x);
+        const int b = bin_if(x, i, y);
+        const u64 w = weight(s, y);
+        if (b >= 0) atomicAdd(&s.sum[b < BINS - 1 ? b : BINS - 1 + lane_id()], w);
+        if constexpr (decltype(keeps)::value)
+          if ((double)w >= mp * 0x1p42) kept_m += w;
+        if constexpr (decltype(counts)::value)
+          if (b >= 0 && y >= LOWEST) atomicAdd(&s.count[b], 1u);
+      });
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    if (by_k)
+      by_m ? fill(yes, yes) : fill(yes, no);
+    else
+      by_m ? fill(no, yes) : fill(no, no);
+    __syncthreads();
+    if (wave == 0) {
+      const u64 x = wave_scan(s.sum[BINS - 1 + tid]);
+      if (tid == 63) s.sum[BINS - 1] = x;
+    }
+    __syncthreads();
+  };
+  // The first bin up to which, with base and nbase before the first, the test holds (the
+  // last with any weight if none does); s.before and s.nbefore then are before it.
+  auto find_bin = [&](u64 base, u64 nbase, const Target& test) INLINE {
+    u64 x[2], c[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = s.sum[2 * tid + i], c[i] = s.count[2 * tid + i];
+    u64 sx = x[0] + x[1], sn = c[0] + c[1];
+    block_scan(s, sx, sn);
+    if (tid == 0) s.at = -1;
+    __syncthreads();
+    const u64 before = base + sx - x[0] - x[1], n = nbase + sn - c[0] - c[1];
+    const bool was = test(before, n);
+    const bool mid = test(before + x[0], n + c[0]), end = test(before + x[0] + x[1], n + c[0] + c[1]);
+    if (end && !was) s.at = mid ? 2 * tid : 2 * tid + 1;
+    __syncthreads();
+    int at = s.at;
+    __syncthreads();
+    if (at < 0) {
+      if (x[0] + x[1]) atomicMax(&s.at, x[1] ? 2 * tid + 1 : 2 * tid);
+      __syncthreads();
+      at = max(s.at, 0);
+      __syncthreads();
+    }
+    if (at >> 1 == tid) {
+      s.before = before + (at & 1 ? x[0] : 0);
+      s.nbefore = n + (at & 1 ? c[0] : 0);
+    }
+    __syncthreads();
+    return at;
+  };
+  bool fresh = false;  // the histogram of all tokens stands
+  auto whole = [&]() INLINE {
+    first = 0;
+    const double range = fmin(RANGE, fmax(0x1p-20, -sc.log2w(low)));
+    fine = (BINS - 1) / range;
+    kept_m = 0;
+    histogram([&](float, int, double y) INLINE { return bin_of(y); });
+    if (by_m) kept_m = block_sum(s, kept_m);
+    fresh = true;
+  };
+  // The token of bin j that the search is for.
+  auto find_in_bin = [&](int j, const Target& test) INLINE {
+    u64 base = s.before, nbase = s.nbefore, lo = 0, hi = ~0ull;
+    // logits that can be in the bin: a hair beyond its ends
+    float above, below;
+    auto ends = [&]() INLINE {
+      const double top = sc.top, hi = top + (first - j / fine) / sc.per,
+                   lo = top + (first - (j + 1) / fine) / sc.per;
+      above = j == 0 ? INFINITY : (float)(hi + 1e-6 * (1 + fabs(top) + fabs(hi)));
+      below = j == BINS - 1 ? -INFINITY : (float)(lo - 1e-6 * (1 + fabs(top) + fabs(lo)));
+      if (value_at(best) == INFINITY) above = INFINITY, below = -INFINITY;
+    };
+    ends();
+    auto in = [&](float x, int i) INLINE {
+      if (!(x >= below && x <= above)) return false;
+      const double y = sc.log2w(x);
+      if (y < LOWEST || bin_of(y) != j) return false;
+      const u64 c = place_of(x, i);
+      return c >= lo && c <= hi;
+    };
+    int n = gather(in);
     if (n > CAP) {
-      u64 mlo = ~0ull, mhi = 0;
-      each([&](float x, int i) {
-        const double y = sc.log2w(x);
-        if (!(y >= LOWEST) || bin_of(y) != f.j) return;
-        const u64 c = place_of(x, i);
-        mlo = min(mlo, c);
-        mhi = max(mhi, c);
-      });
-      if (tid == 0) s.lo = ~0ull, s.hi = 0;
-      __syncthreads();
-      atomicMin(&s.lo, mlo);
-      atomicMax(&s.hi, mhi);
-      __syncthreads();
-      lo = s.lo;
-      hi = s.hi;
+      const u64 keep = kept_m;
+      fresh = false;
+      // the last bin: its range in finer bins
+      if (j == BINS - 1) {
+        const double from = first - j / fine;
+        histogram([&](float, int, double y) INLINE {
+          if (y < LOWEST || bin_of(y) != j) return -1;
+          return binned(y, from, (BINS - 1) / (0.5 - LOWEST - RANGE));
+        });
+        j = find_bin(base, nbase, test);
+        base = s.before;
+        nbase = s.nbefore;
+        const double old_first = first, old_fine = fine;
+        first = from;
+        fine = (BINS - 1) / (0.5 - LOWEST - RANGE);
+        ends();
+        if (j == 0) above = INFINITY;
+        n = gather([&](float x, int i) INLINE {
+          if (!(x >= below && x <= above)) return false;
+          const double y = sc.log2w(x);
+          return y >= LOWEST && binned(y, old_first, old_fine) == BINS - 1 && bin_of(y) == j;
+        });
+        if (n > CAP) {
+          // (what follows tells the tokens by their places alone)
+          if (tid == 0) s.lo = ~0ull, s.hi = 0;
+          __syncthreads();
+          u64 mlo = ~0ull, mhi = 0;
+          each([&](float x, int i) INLINE {
+            const double y = sc.log2w(x);
+            if (y < LOWEST || binned(y, old_first, old_fine) != BINS - 1 || bin_of(y) != j) return;
+            const u64 c = place_of(x, i);
+            mlo = min(mlo, c);
+            mhi = max(mhi, c);
+          });
+          atomicMin(&s.lo, mlo);
+          atomicMax(&s.hi, mhi);
+          __syncthreads();
+          lo = s.lo;
+          hi = s.hi;
+        }
+      } else {
+        if (tid == 0) s.lo = ~0ull, s.hi = 0;
+        __syncthreads();
+        u64 mlo = ~0ull, mhi = 0;
+        each([&](float x, int i) INLINE {
+          if (!in(x, i)) return;
+          const u64 c = place_of(x, i);
+          mlo = min(mlo, c);
+          mhi = max(mhi, c);
+        });
+        atomicMin(&s.lo, mlo);
+        atomicMax(&s.hi, mhi);
+        __syncthreads();
+        lo = s.lo;
+        hi = s.hi;
+      }
+      // many equal, or nearly so: their places, which are all different, are cut ever finer
+      while (n > CAP) {
+        int shift = 0;
+        while ((hi - lo) >> shift >= BINS) ++shift;
+        histogram([&](float x, int i, double) INLINE {
+          const u64 c = place_of(x, i);
+          return x == x && c >= lo && c <= hi ? (int)((hi - c) >> shift) : -1;
+        });
+        const int g = find_bin(base, nbase, test);
+        base = s.before;
+        nbase = s.nbefore;
+        hi -= (u64)g << shift;
+        const u64 width = ((u64)1 << shift) - 1;
+        if (hi - lo > width) lo = hi - width;
+        __syncthreads();
+        n = gather([&](float x, int i) INLINE {
+          const u64 c = place_of(x, i);
+          return x == x && c >= lo && c <= hi;
+        });
+      }
+      kept_m = keep;
     }
-    while (n > CAP) {
-      int shift = 0;
-      while ((hi - lo) >> shift >= BINS) ++shift;
-      clear(1);
-      each([&](float x, int i) {
-        const double y = sc.log2w(x);
-        const u64 c = place_of(x, i);
-        const bool in = y >= LOWEST && bin_of(y) == f.j && c >= lo && c <= hi;
-        add(1, in, in ? (int)((hi - c) >> shift) : 0, true, in ? weight(y) : 0);
-      });
-      __syncthreads();
-      const Found g = find_bin(1, base, nbase, test);
-      n = s.count[1][g.j];
-      base = g.before;
-      nbase = g.n;
-      hi -= (u64)g.j << shift;
-      const u64 width = ((u64)1 << shift) - 1;
-      if (hi - lo > width) lo = hi - width;
-      __syncthreads();
+    sort(n, base);
+    find_listed(n, nbase, test);
+  };
+  // the same for all tokens, as a list where those up to there are few
+  auto find = [&](auto&& test, bool list) INLINE {
+    if (!fresh) whole();
+    const int j = find_bin(0, 0, test);
+    if (list && j < BINS - 1) {
+      // how many that are: a bin's tokens weigh alike
+      double n = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (2 * tid + i <= j) n += (double)s.sum[2 * tid + i] * exp2((2 * tid + i + 0.5) / fine - SCALE);
+      if (block_sum(s, (u64)(n * 1024)) < (u64)CAP * 1000) {
+        const int n = gather([&](float x, int) INLINE { return bin_of(sc.log2w(x)) <= j; });
+        if (n <= CAP) {
+          listed = n;
+          sort(n, 0);
+          find_listed(n, 0, test);
+          return;
+        }
+      }
     }
-    const int m = gather([&](double y, u64 c) { return bin_of(y) == f.j && c >= lo && c <= hi; });
-    find_listed(m, base, nbase, test);
+    find_in_bin(j, test);
   };
 
-  // Where top_k leaves few tokens, counts alone say in which bin the last of them lies, and
-  // the list of all tokens up to there is all that is looked at from then on.
-  const bool counts = by_k && k <= CAP / 2;
-  histogram(!counts);
-  int listed = 0;  // tokens of the list, if it holds all that can be kept
-  auto reaches_k = [&](u64, u64 n) { return n >= (u64)k; };
-  if (counts) {
-    const Found f = find_bin(0, 0, 0, reaches_k);
-    if (f.n + s.count[0][f.j] <= CAP)
-      listed = gather([&](double y, u64) { return bin_of(y) <= f.j; });
+  if (!listed) {
+    whole();
+    if (!by_k) total = block_sum(s, s.sum[2 * tid] + s.sum[2 * tid + 1]);
+  }
+  // the k-th, the one that reaches top_p, the drawn one
+#pragma unroll 1
+  for (int step = 0; step < 3; ++step) {
+    if (step == 0 ? !by_k || listed : step == 1 ? !by_p : false) continue;
+    Target t = reaches_k;
+    if (step == 1) t = {REACHES, 0, p * (double)total};
+    if (step == 2) {
+      if (by_m) total = min(total, max(kept_m, (u64)1 << SCALE));  // (at least the first)
+      t = {PASSES, 0, u * (double)total};
+    }
+    if (listed)
+      find_listed(listed, 0, t);
     else
-      histogram(true);
+      find(t, step == 1);
+    if (step < 2) total = step == 0 ? got_sum : min(total, got_sum);
   }
-  u64 total;
-  if (listed) {
-    find_listed(listed, 0, 0, reaches_k);
-    total = got_sum;
-  } else if (by_k) {
-    const Found f = find_bin(0, 0, 0, reaches_k);
-    find_in_bin(f, reaches_k);
-    total = got_sum;
-  } else {
-    // (all: the bin past the last)
-    const Found f = find_bin(0, 0, 0, [&](u64, u64) { return false; });
-    total = f.before + s.sum[0][f.j];
-  }
-  if (by_p) {
-    const double want = p * (double)total;
-    auto reaches = [&](u64 x, u64) { return (double)x >= want; };
-    if (!listed) {
-      const Found f = find_bin(0, 0, 0, reaches);
-      if (f.n + s.count[0][f.j] <= CAP)
-        listed = gather([&](double y, u64) { return bin_of(y) <= f.j; });
-      else
-        find_in_bin(f, reaches);
-    }
-    if (listed) find_listed(listed, 0, 0, reaches);
-    total = min(total, got_sum);
-  }
-  if (by_m) {
-    if (counts && kept_m == 0) {
-      // (no sums over all: the list's)
-      u64 x = 0, none = 0;
-      for (int i = tid; i < listed; i += NTH) {
-        const u64 w = weight(sc.log2w(value_of((unsigned)(s.list[i] >> 20))));
-        if ((double)w >= mp * 0x1p42) x += w;
-      }
-      block_scan(s, x, none);
-      __syncthreads();
-      if (tid == NTH - 1) s.before = x;
-      __syncthreads();
-      kept_m = s.before;
-      __syncthreads();
-    }
-    total = min(total, max(kept_m, (u64)1 << SCALE));  // (at least the first)
-  }
-  const double want = u * (double)total;
-  auto passes = [&](u64 x, u64) { return (double)x > want; };
-  if (listed)
-    find_listed(listed, 0, 0, passes);
-  else
-    find_in_bin(find_bin(0, 0, 0, passes), passes);
   if (tid == 0) {
     a.tokens[r] = (int)(INDEX - (unsigned)(got_place & INDEX));
     if (a.logprob) {
-      const double y = sc.log2w(value_of((unsigned)(got_place >> 20)));
+      const double y = sc.log2w(value_at(got_place));
       a.logprob[r] = (float)((y + SCALE - log2((double)total)) * 0.6931471805599453);
     }
   }

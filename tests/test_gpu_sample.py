@@ -208,3 +208,23 @@ def test_replayed(S):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(tokens, want[0]) and torch.equal(lp, want[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads", [1, 40])
+def test_draws_from_the_tail(S, dtype, heads):
+    """A few likely tokens and tens of thousands far below, which are drawn from at times: all alike,
+    nearly so, or spread; and the tokens at the end of the order."""
+    gen = torch.Generator().manual_seed(11)
+    logits = torch.empty(6, 60000)
+    logits[0] = -13.0
+    logits[1] = -13.0 + 1e-3 * torch.randn(60000, generator=gen)
+    logits[2] = -13.0 + 2 * torch.randn(60000, generator=gen)
+    logits[3] = -20.0 - 0.1 * torch.arange(60000) / 60000
+    logits[4] = torch.linspace(-29, -1, 60000)
+    logits[5] = -29.0
+    logits[:, torch.randperm(60000, generator=gen)[:heads]] = 0.0
+    logits = logits.to(dtype).cuda()
+    for u in (0.5, 0.97, 0.999, 0.99999, 1 - 2.0 ** -20, 1 - 2.0 ** -24):
+        check(S, logits, [u] * 6)
+        check(S, logits, [u] * 6, k=[50000] * 6, p=[0.99999] * 6)
