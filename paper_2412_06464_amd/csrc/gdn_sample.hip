@@ -32,6 +32,7 @@ typedef unsigned long long u64;
 constexpr int NTH = 1024, NW = NTH / 64;
 constexpr int BINS = 2048, CAP = 2048;  // of a histogram; tokens of the list
 constexpr int FEW = 512;                // top_k up to which the list is tried first
+constexpr int ROUNDS = 6;               // of the search for a bound of the k largest
 constexpr double LOWEST = -43;          // log2 of the least weight that counts
 constexpr int SCALE = 42;               // weights are multiples of 2^-SCALE
 // log2 of the weights that have bins of their own: with 16 one draw in 200 from a normal
@@ -70,7 +71,7 @@ struct Shared {
   u64 list[CAP];  // places
   u64 run[CAP];   // sums of weights up to each
   u64 part[2][NW];
-  unsigned votes[16][3];
+  u64 votes[ROUNDS];
   unsigned listed;
   int at;
   u64 before, nbefore, lo, hi;
@@ -132,9 +133,10 @@ __device__ inline void block_scan(Shared& s, u64& x, u64& c) {
     s.part[1][w] = c;
   }
   __syncthreads();
-  for (int i = 0; i < w; ++i) {
-    x += s.part[0][i];
-    c += s.part[1][i];
+#pragma unroll
+  for (int i = 0; i < NW - 1; ++i) {
+    x += i < w ? s.part[0][i] : 0;
+    c += i < w ? s.part[1][i] : 0;
   }
 }
 // The sum over the workgroup's threads, for all of them.
@@ -190,6 +192,10 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
   __shared__ Shared s;
   const int tid = threadIdx.x, wave = tid >> 6, r = blockIdx.x;
   const Row<E> row(a.logits + r * a.stride, a.vocab);
+  const float T = a.temperature ? a.temperature[r] : 1.f;
+  const int k = a.top_k ? a.top_k[r] : 0;
+  const double p = a.top_p ? (double)a.top_p[r] : 1.0, mp = a.min_p ? (double)a.min_p[r] : 0.0;
+  const float un = a.u ? a.u[r] : 0.f;
   // f(x, index) for this thread's tokens; two loads ahead.  Whole waves take part.
   auto each = [&](auto&& f) INLINE {
     u32x4 x = row.load(tid), y = row.load(tid + NTH);
@@ -222,8 +228,17 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
       s.part[0][wave] = best;
       s.part[1][wave] = __float_as_uint(low);
     }
-    if (tid < 128) s.power[tid] = exp2(SCALE + tid / 128.0);
-    if (tid < 48) s.votes[tid / 3][tid % 3] = 0;
+    if (tid < 128) {
+      // 2^(1/2), 2^(1/4), .. 2^(1/128)
+      constexpr double root[7] = {1.4142135623730951, 1.189207115002721,  1.0905077326652577,
+                                  1.0442737824274138, 1.0218971486541166, 1.0108892860517005,
+                                  1.0054299011128027};
+      double p = 0x1p42;
+#pragma unroll
+      for (int b = 0; b < 7; ++b) p *= tid >> (6 - b) & 1 ? root[b] : 1.0;
+      s.power[tid] = p;
+    }
+    if (tid < ROUNDS) s.votes[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
@@ -231,7 +246,6 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
       low = fminf(low, __uint_as_float((unsigned)s.part[1][i]));
     }
   }
-  const float T = a.temperature ? a.temperature[r] : 1.f;
   if (best == 0 || !(T > 0.f)) {  // nothing to draw, or no draw
     if (tid == 0) {
       a.tokens[r] = best ? (int)(INDEX - (unsigned)(best & INDEX)) : -1;
@@ -240,9 +254,6 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     return;
   }
   const Scale sc(value_at(best), T);
-  const int k = a.top_k ? a.top_k[r] : 0;
-  const double p = a.top_p ? (double)a.top_p[r] : 1.0, mp = a.min_p ? (double)a.min_p[r] : 0.0;
-  const float un = a.u ? a.u[r] : 0.f;
   const double u = un > 0.f ? fmin((double)un, 1 - 0x1p-24) : 0.0;
   const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.0, by_m = mp > 0.0;
 
@@ -268,6 +279,7 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
       const u64 x = tid < n ? s.list[tid] : 0;
       int at = 0;
       if (tid < n)
+#pragma unroll 8
         for (int i = 0; i < n; ++i) at += s.list[i] > x;
       __syncthreads();
       if (tid < n) s.list[at] = x;
@@ -328,46 +340,70 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     __syncthreads();
   };
 
-  // ---- few tokens, by a bound that the k largest reach
-  int listed = 0;  // tokens of the list, if it holds all that can be kept
-  u64 total = 0, kept_m = 0;
-  const Target reaches_k{COUNT, (u64)max(k, 0), 0};
-  if (by_k && k <= FEW) {
-    // the k-th largest of the threads' largest, two bits at a time (0: fewer have any)
-    const unsigned own = mine > -INFINITY ? rank_of(mine) : 0;
-    unsigned bound = 0;
-#pragma unroll 1
-    for (int i = 0; i < 16; ++i) {
-      const int at = 30 - 2 * i;
-#pragma unroll
-      for (unsigned c = 0; c < 3; ++c) {
-        const int n = __popcll(__ballot(own >= (bound | (c + 1) << at)));
-        if (lane_id() == 0 && n) atomicAdd(&s.votes[i][c], (unsigned)n);
-      }
-      __syncthreads();
-      unsigned digit = 0;
-#pragma unroll
-      for (unsigned c = 0; c < 3; ++c) digit += s.votes[i][c] >= (unsigned)k;
-      bound |= digit << at;
+  u64 total = 0;  // of the weights that are kept
+  auto put = [&]() INLINE {
+    if (tid) return;
+    a.tokens[r] = (int)(INDEX - (unsigned)(got_place & INDEX));
+    if (a.logprob) {
+      const double y = sc.log2w(value_at(got_place));
+      a.logprob[r] = (float)((y + SCALE - log2((double)total)) * 0.6931471805599453);
     }
-    const float least = bound ? value_of(bound) : -INFINITY;
+  };
+
+  // ---- few tokens, by a bound that the k largest reach
+  if (by_k && k <= FEW && value_at(best) < INFINITY) {
+    // A bound that the largest of at least k threads reach, and of not many more: five values
+    // at a time between the ends, 11 bits of a word for the count of each.
+    const float span = (float)fmin((double)sc.top - (double)low, -LOWEST / sc.per);
+    float least = (float)sc.top - span, end = (float)sc.top;
+#pragma unroll 1
+    for (int i = 0; i < ROUNDS; ++i) {
+      const float step = (end - least) * (1 / 6.f);
+      u64 n = 0;
+#pragma unroll
+      for (int c = 0; c < 5; ++c)
+        n |= (u64)__popcll(__ballot(mine >= least + step * (c + 1))) << (11 * c);
+      if (lane_id() == 0) atomicAdd(&s.votes[i], n);
+      __syncthreads();
+      n = s.votes[i];
+      int c = 0;  // the last that k reach
+      unsigned most = 1 << 30;
+#pragma unroll
+      for (int x = 0; x < 5; ++x) {
+        const unsigned m = (unsigned)(n >> (11 * x)) & 2047;
+        if (m >= (unsigned)k) c = x + 1, most = m;
+      }
+      end = c < 5 ? least + step * (c + 1) : end;
+      least += step * c;
+      if (most <= 2 * (unsigned)k + 64) break;
+    }
     const int n = gather([&](float x, int) INLINE { return x >= least; });
     if (n <= CAP) {
-      listed = n;
       sort(n, 0);
-      find_listed(n, 0, reaches_k);
-      total = got_sum;
-      if (by_m) {
-        u64 x = 0;
-        for (int i = tid; i < n; i += NTH) {
-          const u64 w = s.run[i] - (i ? s.run[i - 1] : 0);
-          if ((double)w >= mp * 0x1p42) x += w;
+      // the k-th, the one that reaches top_p, the drawn one
+#pragma unroll 1
+      for (int step = 0; step < 3; ++step) {
+        if (step == 1 && !by_p) continue;
+        Target t{COUNT, (u64)k, 0};
+        if (step == 1) t = {REACHES, 0, p * (double)total};
+        if (step == 2 && by_m) {
+          u64 x = 0;
+          for (int i = tid; i < n; i += NTH) {
+            const u64 w = s.run[i] - (i ? s.run[i - 1] : 0);
+            if ((double)w >= mp * 0x1p42) x += w;
+          }
+          total = min(total, max(block_sum(s, x), (u64)1 << SCALE));  // (at least the first)
         }
-        kept_m = block_sum(s, x);
+        if (step == 2) t = {PASSES, 0, u * (double)total};
+        find_listed(n, 0, t);
+        if (step < 2) total = got_sum;
       }
+      return put();
     }
   }
 
+  int listed = 0;  // tokens of the list, if it holds all that can be kept
+  u64 kept_m = 0;
   // ---- otherwise by a histogram: bins of equal width in log2 of the weight, from `first` on, as
   // fine as the row's range has it; the last takes all that is below
   double first = 0, fine = 0;
@@ -554,11 +590,11 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     const int j = find_bin(0, 0, test);
     if (list && j < BINS - 1) {
       // how many that are: a bin's tokens weigh alike
-      double n = 0;
+      float n = 0;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        if (2 * tid + i <= j) n += (double)s.sum[2 * tid + i] * exp2((2 * tid + i + 0.5) / fine - SCALE);
-      if (block_sum(s, (u64)(n * 1024)) < (u64)CAP * 1000) {
+        if (2 * tid + i <= j) n += (float)s.sum[2 * tid + i] * __builtin_amdgcn_exp2f((2 * tid + i + 0.5f) / (float)fine - SCALE);
+      if (block_sum(s, (u64)(n * 1024)) < (u64)500 * 1024) {  // (quickly sorted)
         const int n = gather([&](float x, int) INLINE { return bin_of(sc.log2w(x)) <= j; });
         if (n <= CAP) {
           listed = n;
@@ -571,15 +607,12 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     find_in_bin(j, test);
   };
 
-  if (!listed) {
-    whole();
-    if (!by_k) total = block_sum(s, s.sum[2 * tid] + s.sum[2 * tid + 1]);
-  }
-  // the k-th, the one that reaches top_p, the drawn one
+  whole();
+  if (!by_k) total = block_sum(s, s.sum[2 * tid] + s.sum[2 * tid + 1]);
 #pragma unroll 1
-  for (int step = 0; step < 3; ++step) {
-    if (step == 0 ? !by_k || listed : step == 1 ? !by_p : false) continue;
-    Target t = reaches_k;
+  for (int step = 0; step < 3; ++step) {  // as above
+    if (step == 0 ? !by_k : step == 1 ? !by_p : false) continue;
+    Target t{COUNT, (u64)max(k, 0), 0};
     if (step == 1) t = {REACHES, 0, p * (double)total};
     if (step == 2) {
       if (by_m) total = min(total, max(kept_m, (u64)1 << SCALE));  // (at least the first)
@@ -591,13 +624,7 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
       find(t, step == 1);
     if (step < 2) total = step == 0 ? got_sum : min(total, got_sum);
   }
-  if (tid == 0) {
-    a.tokens[r] = (int)(INDEX - (unsigned)(got_place & INDEX));
-    if (a.logprob) {
-      const double y = sc.log2w(value_at(got_place));
-      a.logprob[r] = (float)((y + SCALE - log2((double)total)) * 0.6931471805599453);
-    }
-  }
+  put();
 }
 
 }  // namespace
