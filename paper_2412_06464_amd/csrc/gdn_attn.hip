@@ -57,6 +57,7 @@ template <bool SHARED> struct Block {
   int seen, hi;       // keys that some row sees lie in [seen, hi)
   int lo;             // seen, down to a multiple of 16
   int all_lo, all_hi; // SHARED: the keys that all rows see
+  const int2* see;    // and what each of the block's tokens sees
   // first and one past the last key that token i sees
   __device__ int first(const AttnArgs& a, int i) const {
     // (a token before the cache's first sees nothing; its place may not pass 32 bits)
@@ -66,7 +67,7 @@ template <bool SHARED> struct Block {
   __device__ int last(const AttnArgs& a, int i) const {
     if constexpr (SHARED) {
       if (a.causal) return min(a.prefix, max(0, place(a, i) + 1));
-      return min(a.prefix, cached(a.cache, seq_of(a.tok, i)));
+      return min(a.prefix, cached(a.cache, seq_near(a.tok, i)));
     }
     return a.causal ? max(0, kv - m + i + 1) : kv;
   }
@@ -77,7 +78,7 @@ template <bool SHARED> struct Block {
   }
   // SHARED: position of the call's token i (behind the last sequence: before all keys)
   __device__ static int place(const AttnArgs& a, int i) {
-    const int s = seq_of(a.tok, i), end = seq_start(a.tok, s + 1);
+    const int s = seq_near(a.tok, i), end = seq_start(a.tok, s + 1);
     return i < end ? cached(a.cache, s) - end + i : -1;
   }
 };
@@ -254,8 +255,14 @@ __device__ inline void attn_block(const AttnArgs& a, const Block<SHARED>& b, int
       if (real) x = *reinterpret_cast<const uint4*>(p + (4 * kb + g) * 16);
       q[t][kb] = *reinterpret_cast<typename P::type*>(&x);
     }
-    first[t] = b.first(a, i);
-    last[t] = real ? min(end, b.last(a, i)) : 0;
+    if constexpr (SHARED) {
+      const int2 see = b.see[real ? i - b.r0 / a.G : 0];
+      first[t] = see.x;
+      last[t] = real ? min(end, see.y) : 0;
+    } else {
+      first[t] = b.first(a, i);
+      last[t] = real ? min(end, b.last(a, i)) : 0;
+    }
   }
   // the keys that all rows of the block see, and that some row of the wave sees
   const int all_lo = SHARED ? b.all_lo : b.first(a, (b.r1 - 1) / a.G);
@@ -634,12 +641,11 @@ __device__ inline void attn_block(const AttnArgs& a, const Block<SHARED>& b, int
 // the join, latency.
 // Grid: ((n * splits + split) * Hk + hk).
 template <class E, int D, int QT, int KW, int KT>
-__global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
+__device__ inline void few_block(const AttnArgs& a, int id, unsigned char* smem) {
   using C = AttnCfg<E, D, QT, 1, KW, KT>;
-  __shared__ __align__(1024) unsigned char smem[C::LDS];
   Block<false> b;
-  b.hk = blockIdx.x % a.Hk;
-  const int rest = blockIdx.x / a.Hk, split = rest % a.splits;
+  b.hk = id % a.Hk;
+  const int rest = id / a.Hk, split = rest % a.splits;
   b.n = rest / a.splits;
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;
@@ -652,6 +658,11 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
   // a range past the keys: no partial result is read there
   if (split > 0 && b.lo + split * a.len >= b.hi) return;
   attn_block<E, D, QT, 1, KW, KT, false>(a, b, split, smem);
+}
+template <class E, int D, int QT, int KW, int KT>
+__global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
+  __shared__ __align__(1024) unsigned char smem[AttnCfg<E, D, QT, 1, KW, KT>::LDS];
+  few_block<E, D, QT, KW, KT>(a, blockIdx.x, smem);
 }
 
 // The row block that comes at `rank` when all sequences' blocks are ordered by the
@@ -720,17 +731,14 @@ __device__ inline bool longest_first(const AttnArgs& a, int R, int rank, int* se
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
 // the next one's.
 template <class E, int D, int QT, int KT>
-__global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile(AttnArgs a,
-                                                                                int slots) {
-  using C = AttnCfg<E, D, QT, 4, 1, KT>;
-  constexpr int R = C::ROWS;
-  __shared__ __align__(1024) unsigned char smem[C::LDS];
+__device__ inline void tile_block(const AttnArgs& a, int slots, int block, int grid,
+                                  unsigned char* smem) {
+  constexpr int R = AttnCfg<E, D, QT, 4, 1, KT>::ROWS;
   Block<false> b;
   // A second workgroup for some CUs, but no third for any: they come in reverse, the
   // shortest beside the longest (a prompt of 4096 tokens, 16 heads, d = 128: 111 us, in
   // order 113; of 2048 in fp32, 8 heads, d = 64: 57 and 79, two at d = 128 166 and 259).
-  const int id =
-      gridDim.x > 512 || blockIdx.x < 256 ? blockIdx.x : 255 + gridDim.x - blockIdx.x;
+  const int id = grid > 512 || block < 256 ? block : 255 + grid - block;
   b.hk = id % a.Hk;
   const int rest = id / a.Hk, split = rest % a.splits;
   int tile;
@@ -740,14 +748,18 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
     // the last row blocks of a sequence see the most keys: they go first
     const int slot = slots - 1 - rest / a.splits;
     if (a.tok.cu) {
+      // 64 sequences at a time, one a lane: the last whose slots begin at this one or before
       const int64_t G = a.G;
-      int lo = 0, hi = a.tok.N;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((int)(a.tok.cu[mid] * G / R) + mid <= slot) lo = mid; else hi = mid;
+      auto begins = [&](int n) { return (int)(a.tok.cu[n] * G / R) + n; };
+      int lo = 0, step = (a.tok.N + 63) >> 6;
+      for (;;) {
+        const int n = lo + lane_id() * step;
+        lo += (__popcll(__ballot(n < a.tok.N && begins(min(n, a.tok.N - 1)) <= slot)) - 1) * step;
+        if (step == 1) break;
+        step = (step + 63) >> 6;
       }
-      b.n = lo;
-      tile = slot - ((int)(a.tok.cu[lo] * G / R) + lo);
+      b.n = __builtin_amdgcn_readfirstlane(lo);
+      tile = slot - begins(b.n);
     } else {
       const int per = (int)(((int64_t)a.tok.T * a.G + R - 1) / R);
       b.n = slot / per;
@@ -765,18 +777,33 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile
   if (split > 0 && b.lo + split * a.len >= b.hi) return;
   attn_block<E, D, QT, 4, 1, KT, false>(a, b, split, smem);
 }
+template <class E, int D, int QT, int KT>
+__global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile(AttnArgs a,
+                                                                                int slots) {
+  __shared__ __align__(1024) unsigned char smem[AttnCfg<E, D, QT, 4, 1, KT>::LDS];
+  tile_block<E, D, QT, KT>(a, slots, blockIdx.x, gridDim.x, smem);
+}
 
 // A prefix that all sequences of the call share, its keys read once for a block of rows of
 // all of them: the rows of a cache head are the query heads of every new token.  Only
 // partial sums leave; k_attn_join adds them to those of the sequences' own keys.
 
+// Keys of a tile of the sequences' own part where they have few rows: 64 KB of buffers, so that
+// two workgroups share a CU.
+template <class E, int D> struct SharedFew {
+  static constexpr int KT = D * (int)sizeof(E) == 128 ? 128 : 64;
+};
+
 // What the block's rows see of the prefix, by `threads` threads.
 template <int THREADS>
-__device__ inline void shared_range(const AttnArgs& a, Block<true>& b, unsigned char* smem) {
+__device__ inline void shared_range(const AttnArgs& a, Block<true>& b, unsigned char* smem,
+                                    int2* see) {
+  b.see = see;
   int lo = 1 << 30, hi = 0, all_lo = 0, all_hi = 1 << 30;
   // (a row of heads sees the same: a thread a token)
   for (int i = b.r0 / a.G + (int)threadIdx.x; i <= (b.r1 - 1) / a.G; i += THREADS) {
     const int f = b.first(a, i), l = b.last(a, i);
+    see[i - b.r0 / a.G] = make_int2(f, l);
     if (f < l) lo = min(lo, f);
     hi = max(hi, l);
     all_lo = max(all_lo, f);
@@ -808,36 +835,57 @@ __device__ inline void shared_range(const AttnArgs& a, Block<true>& b, unsigned 
   b.all_hi = __builtin_amdgcn_readfirstlane(all_hi);
 }
 
-// Grid: split * Hk + hk.
+// The prefix's blocks, p.splits * p.Hk of them for each row block, and behind them those of the
+// sequences' own keys, in one launch: the first are bound by the matrix cores, the others by
+// HBM.  (256 single tokens, 8192 shared keys, up to 1000 of each: apart 37 and 65 us.)
 template <class E, int D, int QT, int KW, int KT>
-__global__ __launch_bounds__(64 * KW, 1) void k_attn_shared_few(AttnArgs a) {
+__global__ __launch_bounds__(64 * KW, 1) void k_attn_shared_few(AttnArgs p, AttnArgs a) {
   using C = AttnCfg<E, D, QT, 1, KW, KT>;
   __shared__ __align__(1024) unsigned char smem[C::LDS];
+  __shared__ int2 see[C::ROWS];
+  const int n = p.splits * p.Hk;
+  if ((int)blockIdx.x >= n) return few_block<E, D, QT, KW, KT>(a, blockIdx.x - n, smem);
   Block<true> b;
-  b.hk = blockIdx.x % a.Hk;
+  b.hk = blockIdx.x % p.Hk;
   b.n = b.q0 = b.r0 = 0;
-  b.m = a.tok.total;
-  b.kv = a.prefix;
-  b.r1 = b.m * a.G;  // (at most C::ROWS, by the plan)
-  shared_range<64 * KW>(a, b, smem);
-  attn_block<E, D, QT, 1, KW, KT, true>(a, b, blockIdx.x / a.Hk, smem);
+  b.m = p.tok.total;
+  b.kv = p.prefix;
+  b.r1 = b.m * p.G;  // (at most C::ROWS, by the plan)
+  shared_range<64 * KW>(p, b, smem, see);
+  attn_block<E, D, QT, 1, KW, KT, true>(p, b, blockIdx.x / p.Hk, smem);
 }
 
-// Grid: (tile * splits + split) * Hk + hk.
-template <class E, int D, int QT, int KT>
-__global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_shared_tile(AttnArgs a) {
-  using C = AttnCfg<E, D, QT, 4, 1, KT>;
-  __shared__ __align__(1024) unsigned char smem[C::LDS];
+// QT == 0: at most 16 rows a sequence, all four waves on its keys (256 single tokens, 8192 shared
+// keys, up to 1000 own: 92 us; by the tile kernel, with one wave of rows, 98).
+template <class E, int D, int QP, int QT, int KT>
+__global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_shared_tile(AttnArgs p,
+                                                                                        AttnArgs a,
+                                                                                        int slots) {
+  using C = AttnCfg<E, D, QP, 4, 1, KT>;
+  constexpr int KF = SharedFew<E, D>::KT;
+  constexpr int LDS = QT == 0 && AttnCfg<E, D, 1, 1, 4, KF>::LDS > C::LDS
+                          ? AttnCfg<E, D, 1, 1, 4, KF>::LDS : C::LDS;
+  __shared__ __align__(1024) unsigned char smem[LDS];
+  __shared__ int2 see[C::ROWS];
+  const int64_t rows = (int64_t)p.tok.total * p.G;
+  const int n = (int)((rows + C::ROWS - 1) / C::ROWS) * p.splits * p.Hk;
+  if ((int)blockIdx.x >= n) {
+    if constexpr (QT == 0)
+      few_block<E, D, 1, 4, KF>(a, blockIdx.x - n, smem);
+    else
+      tile_block<E, D, QT, KT>(a, slots, blockIdx.x - n, gridDim.x - n, smem);
+    return;
+  }
   Block<true> b;
-  b.hk = blockIdx.x % a.Hk;
-  const int rest = blockIdx.x / a.Hk, tile = rest / a.splits;
+  b.hk = blockIdx.x % p.Hk;
+  const int rest = blockIdx.x / p.Hk, tile = rest / p.splits;
   b.n = b.q0 = 0;
-  b.m = a.tok.total;
-  b.kv = a.prefix;
+  b.m = p.tok.total;
+  b.kv = p.prefix;
   b.r0 = tile * C::ROWS;
-  b.r1 = (int)min((int64_t)b.m * a.G, (int64_t)b.r0 + C::ROWS);
-  shared_range<256>(a, b, smem);
-  attn_block<E, D, QT, 4, 1, KT, true>(a, b, rest - tile * a.splits, smem);
+  b.r1 = (int)min(rows, (int64_t)b.r0 + C::ROWS);
+  shared_range<256>(p, b, smem, see);
+  attn_block<E, D, QP, 4, 1, KT, true>(p, b, rest - tile * p.splits, smem);
 }
 
 // Joins the splits' sums of a row by T threads: they turn the splits' maxima m_s into
@@ -855,7 +903,7 @@ template <class E, int D, int T> __global__ __launch_bounds__(256) void k_attn_j
   const int t = (int)(at / a.Hq), h = (int)(at - (int64_t)t * a.Hq);
   if (a.lead && t >= seq_start(a.tok, a.tok.N)) return;  // behind the last sequence
   Block<false> b;
-  b.n = seq_of(a.tok, t);
+  b.n = seq_near(a.tok, t);
   b.q0 = seq_start(a.tok, b.n);
   b.m = seq_start(a.tok, b.n + 1) - b.q0;
   const int64_t all = (int64_t)b.m * a.G;
@@ -1005,22 +1053,40 @@ hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStrea
   });
 }
 
-hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& a, hipStream_t s) {
-  const int64_t tiles = ((int64_t)a.tok.total * a.G + a.block - 1) / a.block;
-  const unsigned grid = (unsigned)(tiles * a.splits * a.Hk);
+bool attn_shared_few(Dt dt, int d) { return d * (dt == Dt::F32 ? 4 : 2) <= 256; }
+
+hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& p, const AttnArgs& a, int slots,
+                              hipStream_t s) {
+  const int64_t tiles = few ? 1 : ((int64_t)p.tok.total * p.G + p.block - 1) / p.block;
+  const unsigned grid =
+      (unsigned)((tiles * p.splits + (a.block < 64 ? (int64_t)a.tok.N : slots) * a.splits) * p.Hk);
   return by_dim(dt, d, [&](auto e, auto dim) {
     using E = decltype(e);
     constexpr int D = decltype(dim)::value;
     using F = Few<E, D>;
     constexpr int KT = Tile<E, D>::KT;
-    if (few && a.block == 16)
-      hipLaunchKernelGGL((k_attn_shared_few<E, D, 1, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
+    auto tile = [&](auto qp, auto qt) {
+      hipLaunchKernelGGL((k_attn_shared_tile<E, D, decltype(qp)::value, decltype(qt)::value, KT>),
+                         dim3(grid), dim3(256), 0, s, p, a, slots);
+    };
+    constexpr std::integral_constant<int, 0> none{};
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    if constexpr (D * sizeof(E) <= 256)
+      if (!few && a.block < 64) {
+        p.block == 64 ? tile(one, none) : tile(two, none);
+        return hipGetLastError();
+      }
+    if (few && p.block == 16)
+      hipLaunchKernelGGL((k_attn_shared_few<E, D, 1, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0,
+                         s, p, a);
     else if (few)
-      hipLaunchKernelGGL((k_attn_shared_few<E, D, 2, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0, s, a);
-    else if (a.block == 64)
-      hipLaunchKernelGGL((k_attn_shared_tile<E, D, 1, KT>), dim3(grid), dim3(256), 0, s, a);
+      hipLaunchKernelGGL((k_attn_shared_few<E, D, 2, F::KW, F::KT>), dim3(grid), dim3(64 * F::KW), 0,
+                         s, p, a);
+    else if (p.block == 64)
+      a.block == 64 ? tile(one, one) : tile(one, two);
     else
-      hipLaunchKernelGGL((k_attn_shared_tile<E, D, 2, KT>), dim3(grid), dim3(256), 0, s, a);
+      a.block == 64 ? tile(two, one) : tile(two, two);
     return hipGetLastError();
   });
 }

@@ -141,9 +141,10 @@ struct Plan {
   size_t part = 0, bytes = 0;  // workspace: offset of {maximum, sum}; size
 };
 
-// from: keys before it are not the plan's (a shared prefix).
+// from: keys before it are not the plan's (a shared prefix, beside which the kernel of few
+// rows runs if and only if `few`).
 gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cache* c,
-                     const gdn_attn* a, int64_t from, Plan* out) {
+                     const gdn_attn* a, int64_t from, bool few, Plan* out) {
   if (!a) return GDN_ERR_NULL;
   if (!(a->scale > 0.f) || !isfinite(a->scale) || a->window < 0 || a->max_kv < 0 ||
       (a->window > 0 && !a->causal))
@@ -194,6 +195,7 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
   const int64_t few_units = std::max<int64_t>(1, seqs * t->Hk), few_keys = keys(most);
   p.few = most * G <= gdn::FEW_ROWS &&
           (few_units <= 256 || few_keys * (dt == Dt::F32 ? 8 : 1) > 1024);
+  if (from > 0) p.few = few;
   if (p.few) {
     p.block = most * G <= 16 ? 16 : 32;
     // A workgroup of this kernel has a CU to itself (128 KB of LDS at most head
@@ -290,25 +292,41 @@ gdn_status plan_shared(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_ca
   if (prefix < 1) return GDN_ERR_VALUE;
   if (prefix > (int64_t)c->max_blocks * c->page_size) return GDN_ERR_SHAPE;
   SharedPlan p;
-  const gdn_status st = plan_attn(t, tok, c, a, prefix, &p.own);
-  if (st != GDN_OK) return st;
+  if (!a) return GDN_ERR_NULL;
+  if (t->Hq % t->Hk) return GDN_ERR_SHAPE;
   const Dt dt = type_of(t->dtype);
   const int64_t rows = (int64_t)tok.total * (t->Hq / t->Hk);  // of a cache head
   if (rows >= (int64_t)1 << 30) return GDN_ERR_SHAPE;
   p.few = rows <= gdn::FEW_ROWS;
+  int64_t longest = tok.T;  // new tokens of a sequence
+  if (tok.cu)
+    for (int n = 0; n < tok.N; ++n)
+      longest = std::max<int64_t>(longest, t->cu_seqlens_host[n + 1] - t->cu_seqlens_host[n]);
+  const bool own_few = p.few || (longest * (t->Hq / t->Hk) <= 16 && gdn::attn_shared_few(dt, t->d));
+  const gdn_status st = plan_attn(t, tok, c, a, prefix, own_few, &p.own);
+  if (st != GDN_OK) return st;
   p.block = p.few ? (rows <= 16 ? 16 : 32) : rows <= 64 ? 64 : 128;
   const int step = p.few ? gdn::attn_few_keys(dt, t->d) : gdn::attn_tile_keys(dt, t->d);
   const int64_t units = (rows + p.block - 1) / p.block * t->Hk;
-  const int64_t want = p.few || size_of(t->dtype) * t->d > 512 ? 256 : 512;
+  // Of the workgroups that run at once the prefix gets its share of the time: its products'
+  // beside that of the own keys' way from HBM (256 single tokens, 8192 shared keys, up to 1000
+  // own: 4 splits 85 us, 8 90, 16 110, 1 214; 64 sequences of 8 tokens, 300 own keys: 4 77, 8 61,
+  // 16 70; in fp32, 64 single tokens, 4096 and 500: 16 93, 32 81, 64 106).
+  const double own = std::min<double>(c->max_blocks * (double)c->page_size, a->max_kv > 0 ? a->max_kv : 1e18) - prefix;
+  const double hbm = std::max(0., own) * tok.N * t->Hk * t->d * 2 * size_of(t->dtype) / 5.3e6;  // us
+  const double mma = 4.0 * rows * t->Hk * t->d * prefix / (dt == Dt::F32 ? 1e8 : 6e8);
+  const double all = p.few || size_of(t->dtype) * t->d > 512 ? 256 : 512;
+  const int64_t want = (int64_t)(all * mma / (mma + hbm));
   const int64_t most = std::min<int64_t>(gdn::MAX_SPLITS - p.own.splits, (prefix + step - 1) / step);
-  const int64_t splits = std::max<int64_t>(1, std::min(want / std::max<int64_t>(1, units), most));
+  const int64_t splits = std::max<int64_t>(1, std::min((want + units - 1) / std::max<int64_t>(1, units), most));
   p.len = (int)(((prefix + splits - 1) / splits + step - 1) / step * step);
   p.splits = (int)((prefix - 1) / p.len + 1);
   // a launch holds less than 2^32 threads, 256 to a workgroup
-  if (units * p.splits >= (int64_t)1 << 24) return GDN_ERR_SHAPE;
-  const int64_t all = (int64_t)tok.total * t->Hq, parts = p.splits + p.own.splits;
-  p.part = up((size_t)(parts * all * t->d * 4));
-  p.bytes = p.part + up((size_t)(parts * all * 8));
+  if (units * p.splits + (own_few ? tok.N : p.own.slots) * p.own.splits * t->Hk >= (int64_t)1 << 24)
+    return GDN_ERR_SHAPE;
+  const int64_t every = (int64_t)tok.total * t->Hq, parts = p.splits + p.own.splits;
+  p.part = up((size_t)(parts * every * t->d * 4));
+  p.bytes = p.part + up((size_t)(parts * every * 8));
   *out = p;
   return GDN_OK;
 }
@@ -455,7 +473,7 @@ size_t gdn_cache_attn_workspace_size(const gdn_tokens* t, const gdn_cache* cache
   gdn::Cache c;
   Plan p;
   if (check_tokens(t, &tok) != GDN_OK || check_cache(cache, 1, false, &c) != GDN_OK ||
-      plan_attn(t, tok, cache, a, 0, &p) != GDN_OK)
+      plan_attn(t, tok, cache, a, 0, false, &p) != GDN_OK)
     return 0;
   return p.bytes;
 }
@@ -473,7 +491,7 @@ gdn_status gdn_cache_attn(const gdn_tokens* t, const gdn_attn* at, const gdn_row
   if ((st = check_rows(o, esz, &a.o)) != GDN_OK) return st;
   if (!aligned(lse, 4)) return GDN_ERR_ALIGN;
   Plan p;
-  if ((st = plan_attn(t, a.tok, cache, at, 0, &p)) != GDN_OK) return st;
+  if ((st = plan_attn(t, a.tok, cache, at, 0, false, &p)) != GDN_OK) return st;
   if (p.bytes) {
     if (!workspace || workspace_bytes < p.bytes) return GDN_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return GDN_ERR_ALIGN;
@@ -551,19 +569,16 @@ gdn_status gdn_cache_attn_shared(const gdn_tokens* t, const gdn_attn* at, const 
   b.block = p.block;
   b.splits = p.splits;
   b.len = p.len;
-  hipError_t e = gdn::launch_attn_shared(dt, t->d, p.few, b, s);
-  if (e != hipSuccess) return GDN_ERR_HIP;
   // the sequences' own keys, their sums behind the prefix's
   a.from = prefix;
-  a.block = p.own.block;
+  a.block = p.few ? p.block : p.own.block;
   a.splits = p.own.splits;
   a.len = p.own.len;
   a.longest = p.own.longest;
-  b = a;
-  b.part += p.splits * rows * t->d;
-  b.part_ml += p.splits * rows * 2;
-  e = p.own.few ? gdn::launch_attn_few(dt, t->d, b, s)
-                : gdn::launch_attn_tile(dt, t->d, (int)p.own.slots, b, s);
+  AttnArgs own = a;
+  own.part += p.splits * rows * t->d;
+  own.part_ml += p.splits * rows * 2;
+  const hipError_t e = gdn::launch_attn_shared(dt, t->d, p.few, b, own, (int)p.own.slots, s);
   if (e != hipSuccess) return GDN_ERR_HIP;
   a.lead = p.splits;
   return done(gdn::launch_attn_join(dt, t->d, a, s));

@@ -74,8 +74,13 @@ int attn_tile_keys(Dt dt, int d);
 hipError_t launch_attn_few(Dt dt, int d, const AttnArgs& a, hipStream_t s);
 // a.block: 64 or 128 rows; slots: row blocks
 hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStream_t s);
-// the rows of all sequences over the prefix (few: at most FEW_ROWS of a cache head, as a.block)
-hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& a, hipStream_t s);
+// p: the rows of all sequences over the prefix; a: each sequence's over its own keys (slots: its
+// row blocks).  few: both by the kernel of few rows, a.block as p.block, at most FEW_ROWS of
+// a cache head in all; else a.block may be 16, each sequence's rows at most, where
+// attn_shared_few.
+bool attn_shared_few(Dt dt, int d);
+hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& p, const AttnArgs& a, int slots,
+                              hipStream_t s);
 hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s);
 
 struct Book {
@@ -120,6 +125,14 @@ __device__ inline int seq_of(const Tokens& k, int t) {
     if (k.cu[mid] <= t) lo = mid; else hi = mid;
   }
   return lo;
+}
+// The same where sequences are most often alike (single tokens): the place that equal lengths
+// would give is tried before the search, whose loads follow one another.
+__device__ inline int seq_near(const Tokens& k, int t) {
+  if (!k.cu) return t / k.T;
+  const int n = min(k.N - 1, (int)(((float)t + 0.5f) * (float)k.N / (float)k.total));
+  const int lo = k.cu[n], hi = k.cu[n + 1];
+  return lo <= t && t < hi ? n : seq_of(k, t);
 }
 __device__ inline int seq_start(const Tokens& k, int n) { return k.cu ? k.cu[n] : n * k.T; }
 // Tokens a sequence holds in the cache, within what its row of the table can; none if it
