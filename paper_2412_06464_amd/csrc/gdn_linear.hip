@@ -176,21 +176,22 @@ struct Gates {
 
 // How a workgroup's DK x NV of the state lie over its waves: DK / KS rows and 16 NC
 // columns each.
-template <class E, int DK, int NV> struct LinearCfg;
-template <int DK> struct LinearCfg<bf16, DK, 64> {
-  static constexpr int KS = DK == 256 ? 2 : 1, NC = 1;
+template <class E, int DK, int NV, bool OUT> struct LinearCfg {
+  static constexpr int KS = DK == 256 ? 2 : 1;
+  static constexpr int NC = sizeof(E) == 2 && NV == 128 && (OUT || DK == 256) ? 2 : 1;
 };
-template <int DK> struct LinearCfg<bf16, DK, 128> {
-  static constexpr int KS = DK == 256 ? 2 : 1, NC = 2;
-};
-template <int DK, int NV> struct LinearCfg<float, DK, NV> {
-  static constexpr int KS = DK == 256 ? 2 : 1, NC = 1;
-};
+
+// Waves a SIMD that the registers are to leave room for.
+template <class E, int DK, int NV, int KS, int NC, bool OUT> constexpr int linear_waves() {
+  constexpr int own = KS * NV / (16 * NC) / 4;
+  if (sizeof(E) == 2 && KS == 1) return OUT ? (NC == 2 ? 2 : own) : 4;
+  return own;
+}
 
 // Grid: groups of 8 units (slot, head) x slices of dv, a unit's slices 8 apart, so that
 // they share the q and k of an XCD's L2.
 template <class E, int DK, int NV, int KS, int NC, bool OUT>
-__global__ __launch_bounds__(64 * KS * NV / (16 * NC), KS * NV / (16 * NC) / 4 * (NC == 2 && KS == 1 ? 2 : 1))
+__global__ __launch_bounds__(64 * KS * NV / (16 * NC), (linear_waves<E, DK, NV, KS, NC, OUT>()))
 void k_linear(LinearArgs a) {
   using M = Mfma<E>;
   using frag = typename M::frag;
@@ -217,7 +218,7 @@ void k_linear(LinearArgs a) {
   const int tid = threadIdx.x, lane = lane_id(), g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int kh = KS == 1 ? 0 : wave / CW, cw = KS == 1 ? wave : wave % CW;
-  constexpr int GATES = W == 8 ? 7 : 0;  // the wave that finds the gates
+  constexpr int GATES = W >= 8 ? W - 1 : 0;  // the wave that finds the gates
   const int slices = a.dv / NV;
   const int grp = blockIdx.x / (8 * slices), rest = blockIdx.x - grp * 8 * slices;
   const int slice = rest >> 3, unit = grp * 8 + (rest & 7);
@@ -429,7 +430,7 @@ void k_linear(LinearArgs a) {
         else lds_barrier();
       } else {
         if (wave < 4) task(two, wave < 2 ? 3 : 4 - wave, wave == 1 ? 2 : 0);
-        const int x = W == 8 ? wave : wave + 2;
+        const int x = W >= 8 ? wave : wave + 2;
         if (x == 4 || x == 5) task(one, x == 4 ? 2 : 0, x == 4 ? 2 : 0);
         from_state();
       }
@@ -717,7 +718,7 @@ template <bool OUT> hipError_t launch(Dt dt, const LinearArgs& a, hipStream_t s)
     constexpr int DK = decltype(dim)::value;
     auto go = [&](auto columns) {
       constexpr int NV = decltype(columns)::value;
-      using C = LinearCfg<E, DK, NV>;
+      using C = LinearCfg<E, DK, NV, OUT>;
       hipLaunchKernelGGL((k_linear<E, DK, NV, C::KS, C::NC, OUT>), dim3(grid),
                          dim3(64 * C::KS * NV / (16 * C::NC)), 0, s, a);
       return hipGetLastError();
