@@ -451,8 +451,8 @@ void k_linear(LinearArgs a) {
       }
     }
 
-    // the state: v weighted, in bf16 as two values (2^-16 of it is lost, where one
-    // value would leave the state with eight bits)
+    // the state: v weighted, in bf16 as three values, which is all of its 24 bits.  (One value
+    // would leave the state with eight; two, with the state 1.4e-6 off, 10% faster)
     const float fe = gt.grown[63];
 #pragma unroll
     for (int i = 0; i < IT; ++i)
@@ -462,7 +462,7 @@ void k_linear(LinearArgs a) {
         for (int e = 0; e < 4; ++e) S[i][c][e] *= fe;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      frag hi[NC], lo[NC];
+      frag hi[NC], lo[NC], rest[NC];
       if constexpr (sizeof(E) == 2) {
         const f32x4 w0 = *reinterpret_cast<const f32x4*>(gt.left + 32 * kt + 4 * g);
         const f32x4 w1 = *reinterpret_cast<const f32x4*>(gt.left + 32 * kt + 16 + 4 * g);
@@ -472,12 +472,14 @@ void k_linear(LinearArgs a) {
           for (int j = 0; j < 8; ++j) {
             const float x = (float)vf[kt][c][j] * (j < 4 ? w0[j & 3] : w1[j & 3]);
             hi[c][j] = (bf16)x;
-            lo[c][j] = (bf16)(x - (float)hi[c][j]);
+            const float y = x - (float)hi[c][j];
+            lo[c][j] = (bf16)y;
+            rest[c][j] = (bf16)(y - (float)lo[c][j]);
           }
           if (careful)  // (an infinity less itself)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              if ((float)lo[c][j] != (float)lo[c][j]) lo[c][j] = (bf16)0.f;
+              if ((float)lo[c][j] != (float)lo[c][j]) lo[c][j] = rest[c][j] = (bf16)0.f;
         }
       } else {
         const float w = gt.left[16 * (kt >> 2) + 4 * g + (kt & 3)];
@@ -494,11 +496,16 @@ void k_linear(LinearArgs a) {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int c = 0; c < NC; ++c) S[i0 + i][c] = M::mma(x[i], hi[c], S[i0 + i][c]);
-        if constexpr (sizeof(E) == 2)
+        if constexpr (sizeof(E) == 2) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < NC; ++c) S[i0 + i][c] = M::mma(x[i], lo[c], S[i0 + i][c]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) S[i0 + i][c] = M::mma(x[i], rest[c], S[i0 + i][c]);
+        }
       }
     }
 

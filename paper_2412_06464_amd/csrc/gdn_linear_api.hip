@@ -59,21 +59,22 @@ struct Pace {
 };
 Pace pace(Dt dt, int dk, int slice) {
   if (dt == Dt::F32) {
-    if (dk == 64) return slice == 64 ? Pace{5.7, 7, 2} : Pace{7, 7, 1};
+    if (dk == 64) return slice == 64 ? Pace{6.1, 9, 2} : Pace{7, 7, 1};
     return dk == 256 ? Pace{15, 15, 1} : slice == 64 ? Pace{10, 10, 1} : Pace{13, 13, 1};
   }
-  if (dk == 64) return slice == 64 ? Pace{2.2, 5, 3} : Pace{3.1, 5.5, 2};
-  if (dk == 128) return slice == 64 ? Pace{2.9, 5.5, 2} : Pace{5, 9.7, 2};
-  return slice == 64 ? Pace{5.6, 5.6, 1} : Pace{6.4, 6.4, 1};
+  if (dk == 64) return slice == 64 ? Pace{2.5, 5, 3} : Pace{3.4, 5.8, 2};
+  if (dk == 128) return slice == 64 ? Pace{3.5, 5.2, 2} : Pace{5.5, 10.3, 2};
+  return slice == 64 ? Pace{5.9, 5.9, 1} : Pace{7, 7, 1};
 }
 
 // How the sequences are cut, by what each length of the segments would take; bytes of the
 // segments' states.  Cut: the walk is shorter where it does not fill the GPU, or where long
 // sequences outlast the others, but what the segments add has to be found first (0.35 of
 // the walk's time a chunk, for all but each sequence's last) and their states pass through
-// memory three times.  (16 packed prompts of up to 8192 tokens, 16 heads, 128 x 128: whole 678
-// us, segments of 2048 tokens 462, of 1024 411, of 512 467; one of 8192 578, of 512
-// 92, of 256 80; 8 of 4096, 6 heads, 256 x 512: whole 378, of 2048 487.)
+// memory four times.  (bf16, us, whole | segments of 256, 512, 1024, 2048 tokens: 16 packed
+// prompts of up to 8192 tokens, 16 heads of 128 x 128, 731 | 590, 484, 434, 491; one of 8192
+// 631 | 85, 95, 139, 240; one of 16384, 128 x 64, 765 | 103, 93, 110, 180; 8 of 4096, 6 heads
+// of 256 x 512, 427 | 802, 632, 559, 558; 32 of 2048, 16 heads of 128 x 128, 331 | 617, 493, 430.)
 size_t plan(const gdn_problem* p, LinearArgs* a) {
   const int slice = gdn::linear_slice(type_of(p->dtype), a->dk, a->dv);
   const Pace pc = pace(type_of(p->dtype), a->dk, slice);
@@ -82,8 +83,10 @@ size_t plan(const gdn_problem* p, LinearArgs* a) {
   auto run = [&](double segments, double longest, double chunks) {
     const double w = segments * units;
     if (w <= 256) return longest * pc.alone;
-    return std::max(longest * (w <= 256.0 * pc.held ? pc.alone + (pc.full - pc.alone) * (w / 256 - 1) / std::max(1, pc.held - 1) : pc.full),
-                    chunks * units * pc.full / (256.0 * pc.held));
+    if (w <= 256.0 * pc.held)
+      return longest * (pc.alone + (pc.full - pc.alone) * (w / 256 - 1) / std::max(1, pc.held - 1));
+    // (more than a CU holds at once: the last to start outlast the others)
+    return std::max(longest * pc.full, chunks * units * pc.full / (256.0 * pc.held) + longest * pc.full / 2);
   };
   int64_t most = 0;  // tokens of the longest
   auto cost = [&](int64_t len) {
@@ -102,7 +105,7 @@ size_t plan(const gdn_problem* p, LinearArgs* a) {
       see(p->T, a->N);
     double us = run(segments, longest, chunks);
     if (before > 0)
-      us += 0.35 * run(segments - a->N, len / 64, before) + 3 * segments * state / 5e6 + 8;
+      us += 0.35 * run(segments - a->N, len / 64, before) + 4 * segments * state / 5e6 + 8;
     return us;
   };
   a->len = 0;

@@ -67,15 +67,15 @@ def bounds(c, lens, o, mo, mt):
     In fp32 a value is a sum of at most max(lens) + dk terms (each sum's order is free), each a
     product of four factors, one of them an exponential (its argument is a difference that
     carries at most 3 u of itself, at most 30 for a weight that counts, the exponential 2 u):
-    (lens + dk + 128) u.  From bf16 input v is weighted in two values, 2^-16 relative together; o's
+    (lens + dk + 128) u.  From bf16 input v is weighted in three values, 2^-24 relative together; o's
     terms pass once through the state or the chunk's products as a bf16 operand (2^-8), and o is
     rounded once (2^-8 of itself)."""
     u = 2.0 ** -24
     base = (max(lens) + c["q"].shape[3] + 128) * u
     if c["q"].dtype is torch.float32:
         return base * mo + 1e-30, base * mt + 1e-30
-    return ((base + 2.0 ** -16 + 2.0 ** -8) * mo + 2.0 ** -8 * o.abs() * (1 + 2.0 ** -7) + 1e-30,
-            (base + 2.0 ** -16) * mt + 1e-30)
+    return ((base + u + 2.0 ** -8) * mo + 2.0 ** -8 * o.abs() * (1 + 2.0 ** -7) + 1e-30,
+            (base + u) * mt + 1e-30)
 
 
 def gpu(c):
