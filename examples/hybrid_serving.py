@@ -9,7 +9,11 @@ sequence's pages and recurrent states, and shows the calls in the order in which
 serving program makes them: pages for a prompt, the prompt in one packed call,
 single tokens, rows that go on from other rows (gdn_pages_select, and
 gdn_pages_copy for the states), pages that left the window, and a compacted cache.
-Projections and normalisations are plain torch.
+``Server.answers`` draws many answers to one prompt: its tokens in one call, a fork for every
+row, single tokens whose attention computes the prompt's part once for all rows
+(gdn_cache_attn_shared), and gdn_sample for the next ones.  With ``linear`` each pair is led
+by a layer of linear attention with a decay (gdn_linear_chunk_fwd,
+gdn_linear_recurrent_fwd).  Projections and normalisations are plain torch.
 """
 from __future__ import annotations
 
@@ -20,14 +24,15 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_2412_06464_amd import gdn, paged  # noqa: E402
+from paper_2412_06464_amd import gdn, linear, paged, sample  # noqa: E402
 
 
 class HybridModel:
-    """Weights and sizes: ``layers`` pairs of a rule layer and an attention layer."""
+    """Weights and sizes: ``layers`` pairs of a rule layer and an attention layer (``window`` 0:
+    over all earlier tokens), with ``linear`` a layer of linear attention before each."""
 
     def __init__(self, vocab=211, width=256, layers=2, heads=4, d=64, q_heads=4, kv_heads=2,
-                 window=96, seed=0, device="cuda", dtype=torch.bfloat16):
+                 window=96, seed=0, device="cuda", dtype=torch.bfloat16, linear=False):
         g = torch.Generator().manual_seed(seed)
         self.__dict__.update(vocab=vocab, width=width, layers=layers, heads=heads, d=d,
                              q_heads=q_heads, kv_heads=kv_heads, window=window, device=device,
@@ -42,6 +47,9 @@ class HybridModel:
         self.attn = [dict(qkv=weight(width, (q_heads + 2 * kv_heads) * d),
                           out=weight(q_heads * d, width)) for _ in range(layers)]
         self.head = weight(width, vocab)
+        self.linear = [dict(qkv=weight(width, 3 * heads * d),
+                            gates=weight(width, 2 * heads).float(), out=weight(heads * d, width))
+                       for _ in range(layers if linear else 0)]
         self.rotary = paged.gdn_rotary(d, base=10000.0, device=device)
 
     @staticmethod
@@ -71,8 +79,9 @@ class Server:
         self.blocks = -(-max_tokens // page_size)
         self.cache = torch.zeros(m.layers, 2, num_pages, m.kv_heads, page_size, m.d, dtype=m.dtype,
                                  device=dev)
-        self.states = torch.zeros(m.layers, 2 * S, m.heads, m.d, m.d, device=dev)
-        self.side = 0
+        # the rules' first, then those of linear attention
+        self.states = torch.zeros(m.layers + len(m.linear), 2 * S, m.heads, m.d, m.d, device=dev)
+        self.side = self.prefix = 0  # (prefix: tokens that all rows begin with)
         self.table = torch.full((S, self.blocks), -1, dtype=torch.int32, device=dev)
         self.lens = torch.zeros(S, dtype=torch.int32, device=dev)
         self.refs = torch.zeros(num_pages, dtype=torch.int32, device=dev)
@@ -92,6 +101,8 @@ class Server:
     def _release(self):
         """Drops the pages that lie whole before every later token's window: their entries become
         holes, which later calls neither read nor store to.  On the device, with no copy back."""
+        if not self.m.window:
+            return
         first = self.lens + 1 - self.m.window  # the first key that a row's next token sees
         end = torch.arange(1, self.blocks + 1, dtype=torch.int32, device=first.device) * self.page
         gone = (self.table >= 0) & (end <= first[:, None])
@@ -102,10 +113,23 @@ class Server:
     def _state(self, layer):
         return self.states[layer, self.side * self.S:(self.side + 1) * self.S]
 
-    def _layers(self, x, rule, cu):
-        """x [B, T, width] through the stack; ``rule(layer, inputs)`` applies the rule."""
+    def _attend(self, q, k_pages, v_pages, cu):
+        window = self.m.window
+        if self.prefix:
+            return paged.gdn_cache_attn_shared(q, k_pages, v_pages, self.table, self.lens,
+                                               self.table[0], self.prefix, window=window, **cu)
+        return paged.gdn_cache_attn(q, k_pages, v_pages, self.table, self.lens, window=window, **cu)
+
+    def _layers(self, x, rule, cu, decayed):
+        """x [B, T, width] through the stack; ``rule(layer, inputs)`` applies the rule,
+        ``decayed(layer, q, k, v, log_alpha)`` linear attention."""
         m = self.m
         for i in range(m.layers):
+            if m.linear:
+                w = m.linear[i]
+                q, k, v, _, log_alpha = m.rule_inputs(w, x)
+                o = decayed(m.layers + i, q, k, v, log_alpha)
+                x = x + m.norm(o).to(m.dtype).flatten(2) @ w["out"]
             w = m.rule[i]
             o = rule(i, m.rule_inputs(w, x))
             x = x + m.norm(o).to(m.dtype).flatten(2) @ w["out"]
@@ -115,8 +139,7 @@ class Server:
             k_pages, v_pages = self.cache[i, 0], self.cache[i, 1]
             q = paged.gdn_cache_append(q, k, v, k_pages, v_pages, self.table, self.lens, m.rotary,
                                        **cu)
-            o = paged.gdn_cache_attn(q, k_pages, v_pages, self.table, self.lens, window=m.window,
-                                     **cu)
+            o = self._attend(q, k_pages, v_pages, cu)
             x = x + o.flatten(2) @ w["out"]
         self._release()
         return m.norm(x).to(m.dtype) @ m.head
@@ -135,7 +158,11 @@ class Server:
             state = self._state(i)
             return gdn.gdn_chunk_fwd(*x, h0=state, ht=state, **cu)[0]
 
-        logits = self._layers(m.embed[ids][None], rule, cu)[0]
+        def decayed(i, *x):
+            state = self._state(i)
+            return linear.gdn_linear_chunk_fwd(*x, h0=state, ht=state, **cu)[0]
+
+        logits = self._layers(m.embed[ids][None], rule, cu, decayed)[0]
         last = (host[1:] - 1).clamp(min=0).long()
         return logits[last.to(m.device)]
 
@@ -148,7 +175,36 @@ class Server:
             state = self._state(i)
             return gdn.gdn_recurrent_fwd(*x, h0=state, ht=state)[0]
 
-        return self._layers(m.embed[ids][:, None], rule, {})[:, 0]
+        def decayed(i, *x):
+            state = self._state(i)
+            return linear.gdn_linear_recurrent_fwd(*x, h0=state, ht=state)[0]
+
+        return self._layers(m.embed[ids][:, None], rule, {}, decayed)[:, 0]
+
+    def answers(self, prompt, count, temperature=0.8, top_k=50, top_p=0.95, generator=None):
+        """S answers of ``count`` tokens to a prompt (a list), on a server without sequences:
+        their tokens [S, count] and log probabilities."""
+        S, dev = self.S, self.m.device
+        rows = dict(temperature=torch.full((S,), temperature, device=dev),
+                    top_k=torch.full((S,), top_k, dtype=torch.int32, device=dev),
+                    top_p=torch.full((S,), top_p, device=dev))
+        logits = self.prefill([prompt] + [[]] * (S - 1))[:1].expand(S, -1)
+        if self.select([0] * S).any():  # every row a fork of the first, on the same full pages
+            raise RuntimeError("no pages left for the answers")
+        # the prompt's full pages are the same in every row
+        self.prefix = 0 if self.m.window else len(prompt) // self.page * self.page
+        tokens, logprobs = [], []
+        try:
+            for step in range(count):
+                if step:
+                    logits = self.decode(tokens[-1])
+                u = torch.rand(S, device=dev, generator=generator)
+                token, logprob = sample.gdn_sample(logits, u, **rows)
+                tokens.append(token)
+                logprobs.append(logprob)
+        finally:
+            self.prefix = 0  # (rows may go their own ways from here)
+        return torch.stack(tokens, 1), torch.stack(logprobs, 1)
 
     def select(self, parents):
         """Row i goes on from row parents[i] (-1: it ends)."""
@@ -185,6 +241,10 @@ def main():
     server.select([4, -1, -1, 3, -1, -1, -1, -1])
     print("after ending six rows", server.compact())
     print("next", server.decode(ids)[[0, 3]].argmax(-1).tolist())
+
+    server = Server(HybridModel(window=0, linear=True))
+    tokens, logprobs = server.answers(prompts[3], 12)
+    print("answers", tuple(tokens.shape), "of log probability", logprobs.sum(1).tolist())
 
 
 if __name__ == "__main__":

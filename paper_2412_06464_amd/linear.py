@@ -51,6 +51,8 @@ def _arguments(q, k, v, log_alpha, h0, cu_seqlens, cu_seqlens_host, output_final
     _check_tensors(q, rows=(("k", k), ("v", v), ("o", o)),
                    gates=() if per_head else (("log_alpha", log_alpha),),
                    states=(("h0", h0, v.shape[3]), ("ht", ht, v.shape[3])), nstate=n)
+    if q.get_device() < 0:
+        raise ValueError("q must be on the GPU")
     if k.shape != q.shape or o.shape != v.shape:
         raise ValueError("k must match q, and o must match v")
     return p, keep, int(per_head), o, ht
@@ -74,13 +76,19 @@ def gdn_linear_chunk_fwd(q, k, v, log_alpha, h0=None, cu_seqlens=None, cu_seqlen
     p, keep, per_head, o, ht = _arguments(q, k, v, log_alpha, h0, cu_seqlens, cu_seqlens_host,
                                           output_final_state, o, ht)
     need = lib.gdn_linear_chunk_fwd_workspace_size(ctypes.byref(p))
-    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    size = 0
+    if need:
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        elif (workspace.dtype != torch.uint8 or workspace.device != q.device
+              or not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
+        size = workspace.numel()
     with _on(q.device):
         _check(lib.gdn_linear_chunk_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v),
                                         _ptr(log_alpha), per_head, _ptr(h0), _ptr(o), _ptr(ht),
-                                        _ptr(workspace), size, _stream(q.device)))
+                                        _ptr(workspace) if size else None, size,
+                                        _stream(q.device)))
     del keep
     return o, ht
 

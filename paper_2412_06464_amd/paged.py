@@ -23,7 +23,7 @@ from typing import NamedTuple
 
 import torch
 
-from .gdn import _check, _cu_pair, _ptr, _stream, load_library as _load
+from .gdn import _check, _cu_pair, _on, _ptr, _stream, load_library as _load
 
 EXPORTS = ("gdn_rotary_turns", "gdn_rotary_fwd", "gdn_rotary_bwd", "gdn_cache_append",
            "gdn_cache_attn", "gdn_cache_attn_workspace_size", "gdn_cache_attn_shared",
@@ -343,8 +343,9 @@ def _attend(q, k_pages, v_pages, table, kv_lens, prefix_table, prefix, scale, ca
     pt = _n.ints("prefix_table", prefix_table, q)
     if prefix > prefix_table.numel() * k_pages.shape[2]:
         raise ValueError("prefix_table must hold the pages of %d tokens" % prefix)
-    _check(lib.gdn_cache_attn_shared(t, a, rq, c, pt, prefix, ro, _ptr(lse), ws, size,
-                                     _stream(dev)))
+    with _on(dev):
+        _check(lib.gdn_cache_attn_shared(t, a, rq, c, pt, prefix, ro, _ptr(lse), ws, size,
+                                         _stream(dev)))
     return o
 
 
