@@ -40,9 +40,10 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // 64 lanes x 16 bytes from base + off (bytes, one per lane) straight into LDS
 // at lds + lane * 16; base and lds are the same for the whole wave.  As
-// dma_frag: the caller waits.
+// dma_frag: the caller waits.  Base may come from a vector instruction right before (a
+// scalar register kept in a vector one): five wait states, the write to m0 among them.
 __device__ inline void dma_rows(const unsigned char* base, unsigned off, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
                "v"(off), "s"(base)
                : "memory");
 }
