@@ -7,6 +7,8 @@
 // keeps is a prefix too, and the shortest prefix has the smallest sum).  No row is sorted:
 //   - with a top_k of few tokens, the k-th largest of the threads' largest logits is a
 //     bound that the k largest reach; what reaches it is gathered and sorted;
+//   - otherwise, in bf16, the tokens of each of the 2^16 values are counted, weights are found
+//     once for a value, and the place among its equals by a second pass over the row;
 //   - otherwise a histogram of weights over their logarithm says in which bin a place lies,
 //     and the bin's tokens (or all up to there, where they are few) are gathered.
 //
@@ -39,6 +41,9 @@ constexpr int SCALE = 42;               // weights are multiples of 2^-SCALE
 // distribution (of 2.5 at T = 1, 128,000 tokens) was from the last bin, and took another histogram
 constexpr double RANGE = 22;
 constexpr unsigned INDEX = (1u << 20) - 1;
+// bf16 logits as keys, in their order: that of the least finite one, of infinity; words of two counts
+constexpr unsigned LOW_KEY = 0x80, INF_KEY = 0xff80;
+constexpr int WORDS = 1 << 15;
 
 struct SampleArgs {
   const unsigned char* logits;
@@ -62,19 +67,34 @@ __device__ inline u64 place_of(float x, int i) {
   return (u64)rank_of(x) << 20 | (INDEX - (unsigned)i);
 }
 __device__ inline float value_at(u64 place) { return value_of((unsigned)(place >> 20)); }
+// The upper half of rank_of(x) where x is a bf16 value.
+__device__ inline unsigned key_of(float x) {
+  const unsigned b = __float_as_uint(x) >> 16, key = b & 0x8000u ? 0xffffu - b : b | 0x8000u;
+  return key + (key == 0x7fff);
+}
+__device__ inline float value_of_key(unsigned key) {
+  return __uint_as_float((key & 0x8000u ? key & 0x7fffu : 0xffffu - key) << 16);
+}
 
-struct Shared {
+struct Common {
   double power[128];  // 2^(SCALE + j / 128)
-  unsigned count[BINS];
-  // (the last bin's, of the many small weights, in a place for each lane)
-  u64 sum[BINS - 1 + 64];
-  u64 list[CAP];  // places
-  u64 run[CAP];   // sums of weights up to each
   u64 part[2][NW];
   u64 votes[ROUNDS];
   unsigned listed;
   int at;
   u64 before, nbefore, lo, hi;
+};
+template <class E> struct Shared : Common {
+  union {
+    struct {
+      unsigned count[BINS];
+      // (the last bin's, of the many small weights, in a place for each lane)
+      u64 sum[BINS - 1 + 64];
+      u64 list[CAP];  // places
+      u64 run[CAP];   // sums of weights up to each
+    };
+    u32x4 words[sizeof(E) == 2 ? WORDS / 4 : 1];  // counts of bf16 keys, two to a word
+  };
 };
 
 struct Scale {
@@ -93,7 +113,7 @@ struct Scale {
 
 // 2^y in units of 2^-SCALE, y <= 0 (0 at NONE), from a table of 2^(j / 128) and the Taylor series
 // of the rest, whose first term left out is 2.2e-12 at most.
-__device__ inline u64 weight(const Shared& s, double y) {
+__device__ inline u64 weight(const Common& s, double y) {
   // the sum's last bits are round(128 y)
   const double shift = 0x1.8p45, z = y + shift, f = y - (z - shift);
   const int i = (int)__double_as_longlong(z);
@@ -123,7 +143,7 @@ __device__ inline u64 wave_scan(u64 x) {
 }
 
 // Inclusive sums over the workgroup's threads of two values at a time.
-__device__ inline void block_scan(Shared& s, u64& x, u64& c) {
+__device__ inline void block_scan(Common& s, u64& x, u64& c) {
   const int w = threadIdx.x >> 6;
   x = wave_scan(x);
   c = wave_scan(c);
@@ -140,7 +160,7 @@ __device__ inline void block_scan(Shared& s, u64& x, u64& c) {
   }
 }
 // The sum over the workgroup's threads, for all of them.
-__device__ inline u64 block_sum(Shared& s, u64 x) {
+__device__ inline u64 block_sum(Common& s, u64 x) {
   x = wave_scan(x);
   __syncthreads();
   if (lane_id() == 63) s.part[0][threadIdx.x >> 6] = x;
@@ -185,11 +205,16 @@ template <class E> struct Row {
   }
 };
 
-// 64 rows of 100,000 in fp32, top_p: bound by the histogram's 64-bit exponentials, an instruction
-// for 64 tokens each; with a small top_k by two passes over the row, the second from cache.
+// Bound by instructions for each token, not by HBM.  64 rows of 100,003 in fp32 (25.6 MB; a copy
+// takes 4.9 us): top_p 72 us, the histogram's 64-bit exponentials and sums; top_k of 50 24, the
+// likeliest alone 11.  256 rows of 128,000 in bf16 (65.5 MB, 12.6): top_p 58 us (102 by
+// the histogram; twice the row 87, so half of it is passes over the tokens, half the
+// values' weights and the searches), top_k of 50 34, the likeliest 16.  Equal logits meet in one LDS
+// word: 64 flat rows of 100,003 in fp32 265 us, 256 of 128,000 in bf16 400 (their counts
+// pass 16 bits, and the histogram follows).
 template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a) {
   constexpr int N = Row<E>::N;
-  __shared__ Shared s;
+  __shared__ Shared<E> s;
   const int tid = threadIdx.x, wave = tid >> 6, r = blockIdx.x;
   const Row<E> row(a.logits + r * a.stride, a.vocab);
   const float T = a.temperature ? a.temperature[r] : 1.f;
@@ -208,6 +233,226 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
       y = z;
     }
   };
+
+  const double u = un > 0.f ? fmin((double)un, 1 - 0x1p-24) : 0.0;
+  const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.0, by_m = mp > 0.0;
+  // What is looked for: the token with which the count reaches n, the sum `want`, or passes it.
+  enum Kind { COUNT, REACHES, PASSES };
+  struct Target {
+    Kind kind;
+    u64 n;
+    double want;
+    __device__ bool operator()(u64 sum, u64 count) const {
+      if (kind == COUNT) return count >= n;
+      return kind == REACHES ? (double)sum >= want && sum > 0 : (double)sum > want;
+    }
+  };
+      if (tid < 128) {
+        // 2^(1/2), 2^(1/4), .. 2^(1/128)
+        constexpr double root[7] = {1.4142135623730951, 1.189207115002721,  1.0905077326652577,
+                                    1.0442737824274138, 1.0218971486541166, 1.0108892860517005,
+                                    1.0054299011128027};
+        double p = 0x1p42;
+  #pragma unroll
+        for (int b = 0; b < 7; ++b) p *= tid >> (6 - b) & 1 ? root[b] : 1.0;
+        s.power[tid] = p;
+      }
+
+  // ---- bf16: a row has few different logits, and counts of each are all that a draw needs
+  if constexpr (sizeof(E) == 2)
+    if (T > 0.f && !(by_k && k <= FEW)) {
+      unsigned* const words = reinterpret_cast<unsigned*>(s.words);
+      for (int i = tid; i < WORDS / 4; i += NTH) s.words[i] = u32x4{0, 0, 0, 0};
+      __syncthreads();
+      unsigned top = 0, low = 0, counted = 0;
+      each([&](float x, int) INLINE {
+        const unsigned key = key_of(x);
+        const bool in = key - (LOW_KEY + 1) < INF_KEY - LOW_KEY;
+        // (the least finite value stands for all that is masked: counted apart)
+        low += (unsigned)__popcll(__ballot(key == LOW_KEY));
+        counted += (unsigned)__popcll(__ballot(in));
+        if (in) {
+          top = max(top, key);
+          atomicAdd(&words[key >> 1], key & 1 ? 0x10000u : 1u);
+        }
+      });
+      if (low) top = max(top, LOW_KEY);
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, 64));
+      if (lane_id() == 0) {
+        s.part[0][wave] = top;
+        s.part[1][wave] = (u64)low << 32 | counted;
+      }
+      __syncthreads();
+      low = counted = 0;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        top = max(top, (unsigned)s.part[0][i]);
+        low += (unsigned)(s.part[1][i] >> 32);
+        counted += (unsigned)s.part[1][i];
+      }
+      if (top == 0) {
+        if (tid == 0) {
+          a.tokens[r] = -1;
+          if (a.logprob) a.logprob[r] = -INFINITY;
+        }
+        return;
+      }
+      const Scale sc(value_of_key(top), T);
+      // A thread has OWN words, the first thread those of the largest keys: the upper half of a
+      // word is the larger key.  (Each lane begins at another of its words: another bank.)
+      constexpr int OWN = WORDS / NTH;
+      auto count = [&](unsigned key) INLINE {
+        return key == LOW_KEY ? low : words[key >> 1] >> (key & 1 ? 16 : 0) & 0xffffu;
+      };
+      u64 sum = 0, kept = 0;
+      unsigned n = 0, stored = 0;
+#pragma unroll 2
+      for (int step = 0; step < OWN; ++step) {
+        const int at = WORDS - 1 - tid * OWN - ((step + lane_id()) & (OWN - 1));
+        const unsigned c = words[at];
+        stored += (c >> 16) + (c & 0xffffu);
+        if (!__ballot(c != 0 || (low && at == LOW_KEY / 2))) continue;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const unsigned key = 2 * at + 1 - i;
+          const unsigned m = i == 0 ? c >> 16 : key == LOW_KEY ? low : c & 0xffffu;
+          const double y = sc.log2w(value_of_key(key));
+          const u64 w = weight(s, y), all = w * m;
+          sum += all;
+          n += y >= LOWEST ? m : 0;
+          if ((double)w >= mp * 0x1p42) kept += all;
+        }
+      }
+      u64 upto = sum, both = (u64)stored << 32 | n;
+      block_scan(s, upto, both);
+      const u64 nupto = (unsigned)both;
+      if (tid == NTH - 1) {
+        s.before = upto;
+        s.nbefore = both >> 32;
+      }
+      if (by_m) kept = block_sum(s, kept);
+      __syncthreads();
+      u64 total = s.before;
+      const bool fits = s.nbefore == counted;  // no count has passed 16 bits
+      __syncthreads();
+      if (fits) {
+        // The key of the token that the test first holds with (the last with any weight if none
+        // does), which of the key's tokens it is, and the sum with it.
+        u64 got = 0;
+        auto find = [&](const Target& test) INLINE {
+          if (tid == 0) s.at = -1;
+          __syncthreads();
+          const bool is = test(upto, nupto), was = tid > 0 && test(upto - sum, nupto - n);
+          if (is && !was) s.at = tid;
+          __syncthreads();
+          int at = s.at;
+          const bool none = at < 0;
+          __syncthreads();
+          if (none) {
+            if (sum) atomicMax(&s.at, tid);
+            __syncthreads();
+            at = s.at;
+          }
+          if (tid == at) {
+            s.before = upto - sum;
+            s.nbefore = nupto - n;
+          }
+          __syncthreads();
+          if (wave == 0) {  // a lane for each of the thread's keys
+            const unsigned key = 2 * (WORDS - at * OWN) - 1 - lane_id();
+            const double y = sc.log2w(value_of_key(key));
+            const u64 one = weight(s, y), most = y >= LOWEST ? count(key) : 0;
+            const u64 b = s.before + wave_scan(one * most) - one * most;
+            const u64 nb = s.nbefore + wave_scan(most) - most;
+            const u64 hits = none ? 0 : __ballot(test(b + one * most, nb + most));
+            const u64 some = __ballot(one * most != 0);
+            if (lane_id() == (hits ? __ffsll(hits) - 1 : 63 - __clzll(some))) {
+              u64 lo = hits ? 1 : most, hi = most;  // the least with which the test holds
+              while (lo < hi) {
+                const u64 mid = (lo + hi) >> 1;
+                if (test(b + one * mid, nb + mid)) hi = mid; else lo = mid + 1;
+              }
+              s.at = (int)key;
+              s.lo = hi;
+              s.hi = most;
+              s.before = b + one * hi;
+            }
+          }
+          __syncthreads();
+          got = s.before;
+        };
+#pragma unroll 1
+        for (int step = 0; step < 3; ++step) {  // the k-th, the one that reaches top_p, the drawn one
+          if (step == 0 ? !by_k : step == 1 ? !by_p : false) continue;
+          Target t{COUNT, (u64)max(k, 0), 0};
+          if (step == 1) t = {REACHES, 0, p * (double)total};
+          if (step == 2) {
+            if (by_m) total = min(total, max(kept, (u64)1 << SCALE));  // (at least the first)
+            t = {PASSES, 0, u * (double)total};
+          }
+          find(t);
+          if (step < 2) total = min(total, got);
+          __syncthreads();
+        }
+        const float x = value_of_key((unsigned)s.at);
+        const unsigned nth = (unsigned)s.lo, most = (unsigned)s.hi;
+        if (tid == 0 && a.logprob)
+          a.logprob[r] = (float)((sc.log2w(x) + SCALE - log2((double)total)) * 0.6931471805599453);
+        // the nth token of this value
+        if (most <= 512) {
+          if (tid == 0) s.listed = 0;
+          __syncthreads();
+          each([&](float y, int i) INLINE {
+            if (y != x) return;
+            const unsigned at = atomicAdd(&s.listed, 1u);
+            if (at < CAP) s.list[at] = (u64)i;
+          });
+          __syncthreads();
+          if (tid < (int)most) {
+            const u64 mine = s.list[tid];
+            unsigned before = 0;
+#pragma unroll 8
+            for (unsigned i = 0; i < most; ++i) before += s.list[i] < mine;
+            if (before + 1 == nth) a.tokens[r] = (int)mine;
+          }
+          return;
+        }
+        // by counts: a wave has a sixteenth of the row
+        const int per = (row.pieces + NW - 1) / NW, from = wave * per, to = min(from + per, row.pieces);
+        auto equal = [&](const u32x4& y) INLINE {
+          unsigned c = 0;
+#pragma unroll
+          for (int e = 0; e < N; ++e) c += Row<E>::get(y, e) == x;
+          return c;
+        };
+        unsigned mine = 0;
+#pragma unroll 2
+        for (int j = from + lane_id(); j < to; j += 64) mine += equal(row.load(j));
+        const u64 sums = wave_scan(mine);
+        if (lane_id() == 63) s.part[0][wave] = sums;
+        __syncthreads();
+        unsigned before = 0;
+        int w = 0;
+        while (w < NW - 1 && before + (unsigned)s.part[0][w] < nth) before += (unsigned)s.part[0][w++];
+        if (wave == w)
+          for (int j = from; j < to; j += 64) {
+            const u32x4 y = j + lane_id() < to ? row.load(j + lane_id()) : u32x4{~0u, ~0u, ~0u, ~0u};
+            const unsigned c = equal(y), upto = before + (unsigned)wave_scan(c);
+            if (upto >= nth && upto - c < nth) {
+              unsigned left = nth - (upto - c);
+#pragma unroll
+              for (int e = 0; e < N; ++e)
+                if (Row<E>::get(y, e) == x && --left == 0)
+                  a.tokens[r] = (j + lane_id()) * N + e - row.off;
+            }
+            before = (unsigned)__shfl((int)upto, 63);
+            if (before >= nth) break;
+          }
+        return;
+      }
+      __syncthreads();  // many equal logits: as below
+    }
 
   // the largest, the lowest index first; the smallest
   float mine = -INFINITY, low = INFINITY;
@@ -228,16 +473,6 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
       s.part[0][wave] = best;
       s.part[1][wave] = __float_as_uint(low);
     }
-    if (tid < 128) {
-      // 2^(1/2), 2^(1/4), .. 2^(1/128)
-      constexpr double root[7] = {1.4142135623730951, 1.189207115002721,  1.0905077326652577,
-                                  1.0442737824274138, 1.0218971486541166, 1.0108892860517005,
-                                  1.0054299011128027};
-      double p = 0x1p42;
-#pragma unroll
-      for (int b = 0; b < 7; ++b) p *= tid >> (6 - b) & 1 ? root[b] : 1.0;
-      s.power[tid] = p;
-    }
     if (tid < ROUNDS) s.votes[tid] = 0;
     __syncthreads();
 #pragma unroll
@@ -254,9 +489,6 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     return;
   }
   const Scale sc(value_at(best), T);
-  const double u = un > 0.f ? fmin((double)un, 1 - 0x1p-24) : 0.0;
-  const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.0, by_m = mp > 0.0;
-
   // Gathers the tokens for which in(x, index) holds; how many they are (they are all in the list
   // if that is at most CAP).
   auto gather = [&](auto&& in) INLINE {
@@ -308,17 +540,6 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     s.run[2 * tid] = x - w[1];
     s.run[2 * tid + 1] = x;
     __syncthreads();
-  };
-  // What is looked for: the token with which the count reaches n, the sum `want`, or passes it.
-  enum Kind { COUNT, REACHES, PASSES };
-  struct Target {
-    Kind kind;
-    u64 n;
-    double want;
-    __device__ bool operator()(u64 sum, u64 count) const {
-      if (kind == COUNT) return count >= n;
-      return kind == REACHES ? (double)sum >= want && sum > 0 : (double)sum > want;
-    }
   };
   // The first token of the sorted list up to which the test holds (the last if none does): its
   // place, and the sum with it.

@@ -228,3 +228,26 @@ def test_draws_from_the_tail(S, dtype, heads):
     for u in (0.5, 0.97, 0.999, 0.99999, 1 - 2.0 ** -20, 1 - 2.0 ** -24):
         check(S, logits, [u] * 6)
         check(S, logits, [u] * 6, k=[50000] * 6, p=[0.99999] * 6)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kw", [{}, dict(k=700), dict(p=0.9), dict(p=0.5, m=0.2), dict(k=3)])
+def test_masked_and_zeros(S, dtype, kw):
+    """Rows most of which is the type's lowest value, or -infinity, or zeros of both signs: more of
+    one value than 16 bits count, too."""
+    vocab, gen = 150001, torch.Generator().manual_seed(12)
+    low = torch.finfo(dtype).min
+    logits = torch.full((6, vocab), low)
+    logits[1] = -math.inf
+    some = torch.randperm(vocab, generator=gen)[:900]
+    for r in (0, 1):
+        logits[r, some] = torch.randn(900, generator=gen) * 2
+    logits[3] = 0.0
+    logits[3, ::2] = -0.0
+    logits[4] = torch.where(torch.rand(vocab, generator=gen) < 0.5, 0.0, -0.0)
+    logits[4, some] = torch.randn(900, generator=gen)
+    logits[5] = -math.inf
+    logits[5, 700:1400] = 1.0
+    logits = logits.to(dtype).cuda()
+    rows = {x: [v] * 6 for x, v in kw.items()}
+    check(S, logits, [0.3, 0.6, 0.99999, 0.5, 0.7, 0.25], **rows)
