@@ -71,10 +71,11 @@ Pace pace(Dt dt, int dk, int slice) {
 // segments' states.  Cut: the walk is shorter where it does not fill the GPU, or where long
 // sequences outlast the others, but what the segments add has to be found first (0.35 of
 // the walk's time a chunk, for all but each sequence's last) and their states pass through
-// memory four times.  (bf16, us, whole | segments of 256, 512, 1024, 2048 tokens: 16 packed
-// prompts of up to 8192 tokens, 16 heads of 128 x 128, 731 | 590, 484, 434, 491; one of 8192
-// 631 | 85, 95, 139, 240; one of 16384, 128 x 64, 765 | 103, 93, 110, 180; 8 of 4096, 6 heads
-// of 256 x 512, 427 | 802, 632, 559, 558; 32 of 2048, 16 heads of 128 x 128, 331 | 617, 493, 430.)
+// memory four times.  (us, whole | segments of 64, 128, 256, 512, 1024, 2048 tokens; bf16: 16 packed
+// prompts of up to 8192 tokens, 16 heads of 128 x 128, 731 | -, -, 590, 484, 434, 491; one of 8192
+// 634 | 143, 106, 79, 87, 132, 240, of 512 43 | 27, 29, 40, four of 300 30 | 35, 33, 45; 8 of 4096,
+// 6 heads of 256 x 512, 427 | -, -, 802, 632, 559, 558, one of 1000 100 | 63, 47, 60, 92; fp32, two of
+// 1001, 4 heads of 64 x 64, 89 | 20, 26, 41, 71.)
 size_t plan(const gdn_problem* p, LinearArgs* a) {
   const int slice = gdn::linear_slice(type_of(p->dtype), a->dk, a->dv);
   const Pace pc = pace(type_of(p->dtype), a->dk, slice);
@@ -111,7 +112,7 @@ size_t plan(const gdn_problem* p, LinearArgs* a) {
   a->len = 0;
   a->slots = a->N;
   double best = cost((int64_t)1 << 40);
-  for (int64_t len = 256; len < most; len *= 2) {
+  for (int64_t len = 64; len < most; len *= 2) {
     const int64_t slots = a->cu ? total / len + a->N : a->N * ((p->T - 1) / len + 1);
     if (slots * a->H * (a->dv / 64) >= MAX_GRID) continue;
     const double us = cost(len);
