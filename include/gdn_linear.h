@@ -10,7 +10,7 @@
  *
  *     S_t = alpha_t S_{t-1} + k_t v_t^T,    o_t = S_t^T q_t,    alpha_t = exp(log_alpha_t)
  *
- * (the rule of gdn.h without its correction, Sec. 2.1, Eq. mamba2).  No scale is applied to q.
+ * (the rule of gdn.h without its correction, Sec. 2.1, Eq. mamba2-update-o).  No scale is applied to q.
  * These are the forms that serve a model: prompts in chunks, and token by
  * token.
  *
