@@ -634,23 +634,24 @@ __global__ __launch_bounds__(256) void k_linear_scan(LinearArgs a) {
   f32x4 z = E;
   if (J > 1) z = *place(0);
   *place(0) = E;
-  // (eight loads on their way at a time; past the last: that one again)
+  // (eight loads on their way at a time)
   constexpr int AHEAD = 8;
   for (int j0 = 1; j0 < J; j0 += AHEAD) {
     f32x4 y[AHEAD];
     float f[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const int j = min(j0 + i, J - 1);
-      y[i] = *place(j);
-      f[i] = a.fade[(size_t)(slot + j) * a.H + h];
+      if (j0 + i + 1 >= J) break;  // (the last's is not needed)
+      y[i] = *place(j0 + i);
+      f[i] = a.fade[(size_t)(slot + j0 + i) * a.H + h];
     }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       if (j0 + i >= J) break;
       E = z;
+      if (j0 + i + 1 < J)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) z[e] = fmaf(f[i], E[e], y[i][e]);
+        for (int e = 0; e < 4; ++e) z[e] = fmaf(f[i], E[e], y[i][e]);
       *place(j0 + i) = E;
     }
   }
