@@ -21,7 +21,7 @@
 //
 // Bound by a wave's chain of products, exponentials and barriers for each chunk, two waves
 // to a SIMD (registers: 128 x 16 NC of the state, v and the outputs): 16 packed prompts of up to
-// 8192 tokens, 16 heads of 128 x 128, bf16, 421 us (972 MB, a copy takes 187): states 136, scan 22,
+// 8192 tokens, 16 heads of 128 x 128, bf16, 417 us (972 MB, a copy takes 187): states 136, scan 22,
 // walk 280, the matrix cores busy in a quarter to a third of it.  8 prompts of 4096, 6 heads of
 // 256 x 512: 192 workgroups, one to a CU, 6.6 us a chunk, 421 us (a copy takes 126).
 #include <hip/hip_runtime.h>
