@@ -574,28 +574,35 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
   // ---- few tokens, by a bound that the k largest reach
   if (by_k && k <= FEW && value_at(best) < INFINITY) {
     // A bound that the largest of at least k threads reach, and of not many more: five values
-    // at a time between the ends, 11 bits of a word for the count of each.
-    const float span = (float)fmin((double)sc.top - (double)low, -LOWEST / sc.per);
-    float least = (float)sc.top - span, end = (float)sc.top;
+    // at a time between the ends, 11 bits of a word for the count of each.  The first bound is one
+    // that all tokens with a weight reach: the row's lowest logit as it is, or (half a power below
+    // LOWEST) where the temperature ends the weights.  A difference rounded and taken from
+    // the top again may lie above the lowest logit, and lose it.
+    float least = fmaxf(low, (float)(sc.top + (LOWEST - 0.5) / sc.per)), end = (float)sc.top;
 #pragma unroll 1
     for (int i = 0; i < ROUNDS; ++i) {
+      float bound[5];  // (what is counted and what is kept are the same floats)
       const float step = (end - least) * (1 / 6.f);
       u64 n = 0;
 #pragma unroll
-      for (int c = 0; c < 5; ++c)
-        n |= (u64)__popcll(__ballot(mine >= least + step * (c + 1))) << (11 * c);
+      for (int c = 0; c < 5; ++c) {
+        bound[c] = least + step * (c + 1);
+        n |= (u64)__popcll(__ballot(mine >= bound[c])) << (11 * c);
+      }
       if (lane_id() == 0) atomicAdd(&s.votes[i], n);
       __syncthreads();
       n = s.votes[i];
-      int c = 0;  // the last that k reach
       unsigned most = 1 << 30;
+      bool over = false;
 #pragma unroll
       for (int x = 0; x < 5; ++x) {
         const unsigned m = (unsigned)(n >> (11 * x)) & 2047;
-        if (m >= (unsigned)k) c = x + 1, most = m;
+        if (m >= (unsigned)k) {  // the last that k reach
+          least = bound[x], most = m;
+        } else if (!over) {
+          end = bound[x], over = true;
+        }
       }
-      end = c < 5 ? least + step * (c + 1) : end;
-      least += step * c;
       if (most <= 2 * (unsigned)k + 64) break;
     }
     const int n = gather([&](float x, int) INLINE { return x >= least; });
