@@ -16,6 +16,7 @@
 // bits), so that sums are exact, whatever their order, atomics included, and two
 // places that differ are told apart: with weights in 32 bits one draw in 10^5 from a flat
 // distribution would be off by a token.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -577,12 +578,15 @@ template <class E> __global__ __launch_bounds__(NTH) void k_sample(SampleArgs a)
     // at a time between the ends, 11 bits of a word for the count of each.  The first bound is one
     // that all tokens with a weight reach: the row's lowest logit as it is, or (half a power below
     // LOWEST) where the temperature ends the weights.  A difference rounded and taken from
-    // the top again may lie above the lowest logit, and lose it.
-    float least = fmaxf(low, (float)(sc.top + (LOWEST - 0.5) / sc.per)), end = (float)sc.top;
+    // the top again may lie above the lowest logit, and lose it.  Both ends are finite, and
+    // their difference, which may not be, is not formed: of -infinity and the largest float
+    // beside an enormous temperature, too, the bounds are numbers.
+    float least = fmaxf(fmaxf(low, -FLT_MAX), (float)(sc.top + (LOWEST - 0.5) / sc.per));
+    float end = (float)sc.top;
 #pragma unroll 1
     for (int i = 0; i < ROUNDS; ++i) {
       float bound[5];  // (what is counted and what is kept are the same floats)
-      const float step = (end - least) * (1 / 6.f);
+      const float step = end * (1 / 6.f) - least * (1 / 6.f);
       u64 n = 0;
 #pragma unroll
       for (int c = 0; c < 5; ++c) {
