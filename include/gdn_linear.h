@@ -20,7 +20,9 @@
  *    decay for every token of a head; NULL: alpha == 1.  Values are expected
  *    to be <= 0; -infinity forgets all that came before the token.
  *  - An infinity or NaN in a token reaches no earlier token of its sequence and no
- *    other sequence or head; one in v stays in its column.
+ *    other sequence or head; one in v stays in its column, one in k in its row of the
+ *    state, as the infinity that its product with v is (chunks make it a NaN where the
+ *    alphas behind it, multiplied together, fall below what float32 holds).
  *  - Outputs must not overlap inputs, but ht may be h0 (updated in place).
  *  - The same call on the same inputs gives the same bits; a sequence's results
  *    can differ in rounding between calls whose B, H or boundaries differ

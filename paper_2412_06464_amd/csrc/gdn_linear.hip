@@ -36,6 +36,7 @@ typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 #define LDS_AS __attribute__((address_space(3)))
 
@@ -145,13 +146,33 @@ __device__ inline typename Mfma<E>::frag col_operand(const E* m, int c0, int kt)
   }
 }
 
-template <class E> __device__ inline bool has_odd(u32x4 w) {
-  bool odd = false;
+// Infinities and NaN: the largest of the pieces' values without their signs (bf16: of each half
+// of the words), and whether it is one.
+template <class E> __device__ inline void see_odd(unsigned& most, u32x4 w) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    odd = odd || (w[i] & 0x7f800000u) == 0x7f800000u ||
-          (sizeof(E) == 2 && (w[i] & 0x7f80u) == 0x7f80u);
-  return odd;
+    if constexpr (sizeof(E) == 2) {
+      const unsigned x = w[i] & 0x7fff7fffu;
+      const u16x2 y = __builtin_elementwise_max(*reinterpret_cast<const u16x2*>(&most),
+                                                *reinterpret_cast<const u16x2*>(&x));
+      most = *reinterpret_cast<const unsigned*>(&y);
+    } else {
+      most = max(most, w[i] & 0x7fffffffu);
+    }
+}
+template <class E> __device__ inline bool is_odd(unsigned most) {
+  return most >= 0x7f800000u || (sizeof(E) == 2 && (most & 0xffffu) >= 0x7f80u);
+}
+
+// An operand with zeros in their place.
+__device__ inline bf16x8 without_odd(bf16x8 x) {
+  u32x4 w = *reinterpret_cast<const u32x4*>(&x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
+    if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+  }
+  return *reinterpret_cast<const bf16x8*>(&w);
 }
 
 // Inclusive prefix sums over the 64 lanes: within rows of 16 lanes by shifts of 1, 2, 4 and
@@ -324,7 +345,10 @@ void k_linear(LinearArgs a) {
       if (OUT) *piece<E, LK>(sq, r, tid % PK) = turned<E>(nq[i], r);
       *piece<E, LK>(sk, r, tid % PK) = turned<E>(nk[i], r);
     }
-    bool odd = false;
+    unsigned most = 0;
+#pragma unroll
+    for (int i = 0; i < RK; ++i)
+      if (sizeof(E) == 2) see_odd<E>(most, nk[i]);
 #pragma unroll
     for (int i = 0; i < RV; ++i) {
       const int r = tid / PV + NTH / PV * i;
@@ -333,13 +357,13 @@ void k_linear(LinearArgs a) {
       // counter holds both)
       if (OUT && t > seg.t0) put_out(t - 64, r, *at);
       *at = turned<E>(nv[i], r);
-      odd = odd || has_odd<E>(nv[i]);
+      see_odd<E>(most, nv[i]);
     }
-    if (odd) sodd[buf] = 1;
+    if (is_odd<E>(most)) sodd[buf] = 1;
     if (t + 64 < seg.t1) fetch(t + 64);
     lds_barrier();
     const Gates& gt = gates[buf];
-    const bool careful = sodd[buf] != 0;
+    const bool careful = __builtin_amdgcn_readfirstlane(sodd[buf]) != 0;
     if (tid == 0) sodd[buf ^ 1] = 0;
     if (wave == GATES) {
       find_gates(gates[buf ^ 1]);
@@ -503,6 +527,10 @@ void k_linear(LinearArgs a) {
 #pragma unroll
           for (int c = 0; c < NC; ++c) S[i0 + i][c] = M::mma(x[i], hi[c], S[i0 + i][c]);
         if constexpr (sizeof(E) == 2) {
+          // (an infinity meets the first value: the others may be 0, or of the other sign)
+          if (careful)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = without_odd(x[i]);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
