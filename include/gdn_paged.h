@@ -178,8 +178,8 @@ gdn_status gdn_cache_attn(const gdn_tokens *t, const gdn_attn *a, const gdn_rows
  * hold there; later keys are where the table has them.  kv_lens counts the
  * prefix; a sequence that holds fewer tokens sees those it holds.  prefix
  * is at most max_blocks * page_size; with 0 it is gdn_cache_attn.
- * In bfloat16 p is rounded as there, in the prefix's part as for sequences of many
- * rows unless the call's new tokens x Hq / Hk are at most 32 in all.
+ * In bfloat16 p enters as two values where every sequence has few rows (at most 32), as
+ * one otherwise.
  * The workspace (gdn_cache_attn_shared_workspace_size bytes) holds the partial
  * results of the prefix and of the sequences' own keys. */
 size_t gdn_cache_attn_shared_workspace_size(const gdn_tokens *t, const gdn_cache *cache,

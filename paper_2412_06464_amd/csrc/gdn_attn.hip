@@ -158,7 +158,17 @@ __device__ inline float col_sum(float x) {
 // (a prompt of 8192 tokens, d = 128: 279 us, with 0 306).
 constexpr float SLACK = 8.f;
 
-template <class E, int D, int QT, int RW, int KW, int KT, bool SHARED>
+// PARTS: the bf16 values that stand for a weight p in its product with v.  Two (p's rounding, and
+// what that left over: 2^-16 of p is lost) make o exact but for its own rounding; one
+// leaves its error, against 64 bits, at 1.3 to 1.4 times that.  With few rows the keys'
+// way from HBM hides the second product (256 single tokens in a 2K window 147.2 us, with
+// one 147.4; two with 131072 keys 96.7 and 96.6; 8 tokens a sequence, up to 4000 keys,
+// 55.3 and 55.8), and sequences of few rows keep it where they share a prefix (16 single tokens,
+// 131072 shared keys, 63.7 and 62.7; 256, 8192 and up to 1000 own, 84.1 and 82.5; 64 sequences of 8
+// tokens, 80.5 and 68.4).  With many it is matrix cores' time that binds (a prompt of 8192 tokens
+// 345 us, with one 269; d = 64 245 and 165; prompts in a 2K window, d = 256, 201 and 164; 32
+// sequences of 64 tokens, 8192 shared keys, 209 and 168).
+template <class E, int D, int QT, int RW, int KW, int KT, int PARTS, bool SHARED>
 __device__ inline void attn_block(const AttnArgs& a, const Block<SHARED>& b, int split,
                                   unsigned char* smem) {
   using C = AttnCfg<E, D, QT, RW, KW, KT>;
@@ -169,14 +179,6 @@ __device__ inline void attn_block(const AttnArgs& a, const Block<SHARED>& b, int
   // fills in with its softmax (a prompt of 8192 tokens, d = 128: 275 us, without 285;
   // with three waves, bf16 at d = 64, 174 and 166, so not there).
   constexpr bool PRIO = KW == 1 && RB >= 256 && RB <= 512;
-  // The bf16 values that stand for a weight p in its product with v.  Two (p's rounding, and
-  // what that left over: 2^-16 of p is lost) make o exact but for its own rounding; one
-  // leaves its error, against 64 bits, at 1.3 to 1.4 times that.  With few rows the keys'
-  // way from HBM hides the second product (256 single tokens in a 2K window 147.2 us, with
-  // one 147.4; two with 131072 keys 96.7 and 96.6; 8 tokens a sequence, up to 4000 keys,
-  // 55.3 and 55.8).  With many it is matrix cores' time that binds (a prompt of 8192 tokens
-  // 345 us, with one 269; d = 64 245 and 165; prompts in a 2K window, d = 256, 201 and 164).
-  constexpr int PARTS = KW == 1 ? 1 : 2;
   constexpr int MINE = KW == 1 ? (GROUPS + RW - 1) / RW : NT;  // groups this wave copies
   const int lane = lane_id(), g = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -658,7 +660,7 @@ __device__ inline void few_block(const AttnArgs& a, int id, unsigned char* smem)
   b.range(a);
   // a range past the keys: no partial result is read there
   if (split > 0 && b.lo + split * a.len >= b.hi) return;
-  attn_block<E, D, QT, 1, KW, KT, false>(a, b, split, smem);
+  attn_block<E, D, QT, 1, KW, KT, 2, false>(a, b, split, smem);
 }
 template <class E, int D, int QT, int KW, int KT>
 __global__ __launch_bounds__(64 * KW, 1) void k_attn_few(AttnArgs a) {
@@ -731,7 +733,7 @@ __device__ inline bool longest_first(const AttnArgs& a, int R, int rank, int* se
 // block of a slot follow from the boundaries: sequence n's slots begin at
 // floor(cu[n] G / R) + n, which leaves at least ceil(m G / R) of them before
 // the next one's.
-template <class E, int D, int QT, int KT>
+template <class E, int D, int QT, int KT, int PARTS>
 __device__ inline void tile_block(const AttnArgs& a, int slots, int block, int grid,
                                   unsigned char* smem) {
   constexpr int R = AttnCfg<E, D, QT, 4, 1, KT>::ROWS;
@@ -776,13 +778,13 @@ __device__ inline void tile_block(const AttnArgs& a, int slots, int block, int g
   b.kv = cached(a.cache, b.n);
   b.range(a);
   if (split > 0 && b.lo + split * a.len >= b.hi) return;
-  attn_block<E, D, QT, 4, 1, KT, false>(a, b, split, smem);
+  attn_block<E, D, QT, 4, 1, KT, PARTS, false>(a, b, split, smem);
 }
 template <class E, int D, int QT, int KT>
 __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_tile(AttnArgs a,
                                                                                 int slots) {
   __shared__ __align__(1024) unsigned char smem[AttnCfg<E, D, QT, 4, 1, KT>::LDS];
-  tile_block<E, D, QT, KT>(a, slots, blockIdx.x, gridDim.x, smem);
+  tile_block<E, D, QT, KT, 1>(a, slots, blockIdx.x, gridDim.x, smem);
 }
 
 // A prefix that all sequences of the call share, its keys read once for a block of rows of
@@ -853,12 +855,12 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_shared_few(AttnArgs p, Attn
   b.kv = p.prefix;
   b.r1 = b.m * p.G;  // (at most C::ROWS, by the plan)
   shared_range<64 * KW>(p, b, smem, see);
-  attn_block<E, D, QT, 1, KW, KT, true>(p, b, blockIdx.x / p.Hk, smem);
+  attn_block<E, D, QT, 1, KW, KT, 2, true>(p, b, blockIdx.x / p.Hk, smem);
 }
 
 // QT == 0: at most 16 rows a sequence, all four waves on its keys (256 single tokens, 8192 shared
 // keys, up to 1000 own: 92 us; by the tile kernel, with one wave of rows, 98).
-template <class E, int D, int QP, int QT, int KT>
+template <class E, int D, int QP, int QT, int KT, int PARTS>
 __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_shared_tile(AttnArgs p,
                                                                                         AttnArgs a,
                                                                                         int slots) {
@@ -874,7 +876,7 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_shar
     if constexpr (QT == 0)
       few_block<E, D, 1, 4, KF>(a, blockIdx.x - n, smem);
     else
-      tile_block<E, D, QT, KT>(a, slots, blockIdx.x - n, gridDim.x - n, smem);
+      tile_block<E, D, QT, KT, PARTS>(a, slots, blockIdx.x - n, gridDim.x - n, smem);
     return;
   }
   Block<true> b;
@@ -886,7 +888,7 @@ __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_shar
   b.r0 = tile * C::ROWS;
   b.r1 = (int)min(rows, (int64_t)b.r0 + C::ROWS);
   shared_range<256>(p, b, smem, see);
-  attn_block<E, D, QP, 4, 1, KT, true>(p, b, rest - tile * p.splits, smem);
+  attn_block<E, D, QP, 4, 1, KT, PARTS, true>(p, b, rest - tile * p.splits, smem);
 }
 
 // Joins the splits' sums of a row by T threads: they turn the splits' maxima m_s into
@@ -1056,8 +1058,8 @@ hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStrea
 
 bool attn_shared_few(Dt dt, int d) { return d * (dt == Dt::F32 ? 4 : 2) <= 256; }
 
-hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& p, const AttnArgs& a, int slots,
-                              hipStream_t s) {
+hipError_t launch_attn_shared(Dt dt, int d, bool few, int parts, const AttnArgs& p, const AttnArgs& a,
+                              int slots, hipStream_t s) {
   const int64_t tiles = few ? 1 : ((int64_t)p.tok.total * p.G + p.block - 1) / p.block;
   const unsigned grid =
       (unsigned)((tiles * p.splits + (a.block < 64 ? (int64_t)a.tok.N : slots) * a.splits) * p.Hk);
@@ -1067,8 +1069,16 @@ hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& p, const A
     using F = Few<E, D>;
     constexpr int KT = Tile<E, D>::KT;
     auto tile = [&](auto qp, auto qt) {
-      hipLaunchKernelGGL((k_attn_shared_tile<E, D, decltype(qp)::value, decltype(qt)::value, KT>),
-                         dim3(grid), dim3(256), 0, s, p, a, slots);
+      constexpr int QP = decltype(qp)::value, QT = decltype(qt)::value;
+      if constexpr (sizeof(E) == 2)
+        if (QT == 0 || parts == 2) {  // (QT == 0 has few rows)
+          hipLaunchKernelGGL((k_attn_shared_tile<E, D, QP, QT, KT, 2>), dim3(grid), dim3(256), 0, s, p,
+                             a, slots);
+          return;
+        }
+      if constexpr (sizeof(E) == 4 || QT > 0)
+        hipLaunchKernelGGL((k_attn_shared_tile<E, D, QP, QT, KT, 1>), dim3(grid), dim3(256), 0, s, p,
+                           a, slots);
     };
     constexpr std::integral_constant<int, 0> none{};
     constexpr std::integral_constant<int, 1> one{};

@@ -283,6 +283,7 @@ gdn_status plan_attn(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_cach
 struct SharedPlan {
   bool few;
   int block, splits, len;
+  int parts;                   // bf16 values that stand for a weight
   Plan own;                    // the sequences' own keys
   size_t part, bytes;          // workspace: offset of {maximum, sum}; size
 };
@@ -305,16 +306,19 @@ gdn_status plan_shared(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_ca
   const bool own_few = p.few || (longest * (t->Hq / t->Hk) <= 16 && gdn::attn_shared_few(dt, t->d));
   const gdn_status st = plan_attn(t, tok, c, a, prefix, own_few, &p.own);
   if (st != GDN_OK) return st;
+  // two where gdn_cache_attn may have two: a program that goes over to this call loses no accuracy
+  p.parts = longest * (t->Hq / t->Hk) <= gdn::FEW_ROWS ? 2 : 1;
   p.block = p.few ? (rows <= 16 ? 16 : 32) : rows <= 64 ? 64 : 128;
   const int step = p.few ? gdn::attn_few_keys(dt, t->d) : gdn::attn_tile_keys(dt, t->d);
   const int64_t units = (rows + p.block - 1) / p.block * t->Hk;
   // Of the workgroups that run at once the prefix gets its share of the time: its products'
-  // beside that of the own keys' way from HBM (256 single tokens, 8192 shared keys, up to 1000
-  // own: 4 splits 85 us, 8 90, 16 110, 1 214; 64 sequences of 8 tokens, 300 own keys: 4 77, 8 61,
-  // 16 70; in fp32, 64 single tokens, 4096 and 500: 16 93, 32 81, 64 106).
+  // (a half more where weights are two values) beside that of the own keys' way from HBM (256
+  // single tokens, 8192 shared keys, up to 1000 own: 5 splits, the rule's, 85 us, 4 91, 8 87, 16 110,
+  // 1 259; 64 sequences of 8 tokens, 300 own keys: 4 89, 8 81, 16 96; in fp32, 64 single tokens, 4096
+  // and 500: 16 91, 24 86, 32 80).
   const double own = std::min<double>(c->max_blocks * (double)c->page_size, a->max_kv > 0 ? a->max_kv : 1e18) - prefix;
   const double hbm = std::max(0., own) * tok.N * t->Hk * t->d * 2 * size_of(t->dtype) / 5.3e6;  // us
-  const double mma = 4.0 * rows * t->Hk * t->d * prefix / (dt == Dt::F32 ? 1e8 : 6e8);
+  const double mma = (dt == Dt::F32 ? 4e-8 : (1 + p.parts) / 3e8) * rows * t->Hk * t->d * prefix;
   const double all = p.few || size_of(t->dtype) * t->d > 512 ? 256 : 512;
   const int64_t want = (int64_t)(all * mma / (mma + hbm));
   const int64_t most = std::min<int64_t>(gdn::MAX_SPLITS - p.own.splits, (prefix + step - 1) / step);
@@ -578,7 +582,7 @@ gdn_status gdn_cache_attn_shared(const gdn_tokens* t, const gdn_attn* at, const 
   AttnArgs own = a;
   own.part += p.splits * rows * t->d;
   own.part_ml += p.splits * rows * 2;
-  const hipError_t e = gdn::launch_attn_shared(dt, t->d, p.few, b, own, (int)p.own.slots, s);
+  const hipError_t e = gdn::launch_attn_shared(dt, t->d, p.few, p.parts, b, own, (int)p.own.slots, s);
   if (e != hipSuccess) return GDN_ERR_HIP;
   a.lead = p.splits;
   return done(gdn::launch_attn_join(dt, t->d, a, s));

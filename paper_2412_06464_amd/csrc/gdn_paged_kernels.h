@@ -77,10 +77,10 @@ hipError_t launch_attn_tile(Dt dt, int d, int slots, const AttnArgs& a, hipStrea
 // p: the rows of all sequences over the prefix; a: each sequence's over its own keys (slots: its
 // row blocks).  few: both by the kernel of few rows, a.block as p.block, at most FEW_ROWS of
 // a cache head in all; else a.block may be 16, each sequence's rows at most, where
-// attn_shared_few.
+// attn_shared_few.  parts: bf16 values for a weight (one or two; two where few).
 bool attn_shared_few(Dt dt, int d);
-hipError_t launch_attn_shared(Dt dt, int d, bool few, const AttnArgs& p, const AttnArgs& a, int slots,
-                              hipStream_t s);
+hipError_t launch_attn_shared(Dt dt, int d, bool few, int parts, const AttnArgs& p, const AttnArgs& a,
+                              int slots, hipStream_t s);
 hipError_t launch_attn_join(Dt dt, int d, const AttnArgs& a, hipStream_t s);
 
 struct Book {
