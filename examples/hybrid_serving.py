@@ -121,7 +121,9 @@ class Server:
         return paged.gdn_cache_attn(q, k_pages, v_pages, self.table, self.lens, window=window, **cu)
 
     def _layers(self, x, rule, cu, decayed):
-        """x [B, T, width] through the stack; ``rule(layer, inputs)`` applies the rule,
+        """x [B, T, width] (in 32 bits, as the sum of what the layers add: where a head's output
+        nearly cancels, its normalisation magnifies what x is off by) through the stack;
+        ``rule(layer, inputs)`` applies the rule,
         ``decayed(layer, q, k, v, log_alpha)`` linear attention."""
         m = self.m
         for i in range(m.layers):
@@ -162,7 +164,7 @@ class Server:
             state = self._state(i)
             return linear.gdn_linear_chunk_fwd(*x, h0=state, ht=state, **cu)[0]
 
-        logits = self._layers(m.embed[ids][None], rule, cu, decayed)[0]
+        logits = self._layers(m.embed[ids][None].float(), rule, cu, decayed)[0]
         last = (host[1:] - 1).clamp(min=0).long()
         return logits[last.to(m.device)]
 
@@ -179,7 +181,7 @@ class Server:
             state = self._state(i)
             return linear.gdn_linear_recurrent_fwd(*x, h0=state, ht=state)[0]
 
-        return self._layers(m.embed[ids][:, None], rule, {}, decayed)[:, 0]
+        return self._layers(m.embed[ids][:, None].float(), rule, {}, decayed)[:, 0]
 
     def answers(self, prompt, count, temperature=0.8, top_k=50, top_p=0.95, generator=None):
         """S answers of ``count`` tokens to a prompt (a list), on a server without sequences:
