@@ -15,14 +15,17 @@
  * token.
  *
  *  - Head dims: dk in {64, 128, 256} and dv in {64, 128, 256, 512}, any pair,
- *    in bfloat16 (fp32 sums and states) and in float32.
+ *    in bfloat16 (fp32 sums and states) and in float32.  In chunks of bfloat16 the products
+ *    for o take the state and the tokens' weights to 2^-16 of their values, and o is
+ *    rounded once; what a token adds to the state keeps all 24 bits.
  *  - log_alpha: float32 [B, T, H], or with per_head != 0 float32 [H], the same
  *    decay for every token of a head; NULL: alpha == 1.  Values are expected
  *    to be <= 0; -infinity forgets all that came before the token.
  *  - An infinity or NaN in a token reaches no earlier token of its sequence and no
  *    other sequence or head; one in v stays in its column, one in k in its row of the
  *    state, as the infinity that its product with v is (chunks make it a NaN where the
- *    alphas behind it, multiplied together, fall below what float32 holds).
+ *    alphas behind it, multiplied together, fall below what float32 holds), and one in q in
+ *    its token's row of o (in chunks as an infinity or NaN).
  *  - Outputs must not overlap inputs, but ht may be h0 (updated in place).
  *  - The same call on the same inputs gives the same bits; a sequence's results
  *    can differ in rounding between calls whose B, H or boundaries differ

@@ -19,11 +19,15 @@
 // k_linear_scan turns that into entry states, and the segments are walked side by
 // side.
 //
+// In bf16 the entry state and P are operands as two values each (PARTS), so that o is off by its
+// own rounding alone; as one they left 1.4 times that, at 433 us of 487 for the packed prompts
+// below, 412 of 508 for the wide heads (P's second value 6%, the state's the rest).
+//
 // Bound by a wave's chain of products, exponentials and barriers for each chunk, two waves
-// to a SIMD (registers: 128 x 16 NC of the state, v and the outputs): 16 packed prompts of up to
-// 8192 tokens, 16 heads of 128 x 128, bf16, 417 us (972 MB, a copy takes 187): states 136, scan 22,
-// walk 280, the matrix cores busy in a quarter to a third of it.  8 prompts of 4096, 6 heads of
-// 256 x 512: 192 workgroups, one to a CU, 6.6 us a chunk, 421 us (a copy takes 126).
+// to a SIMD (registers: 128 x 16 NC of the state, v and the outputs; the walks of 128 columns keep
+// 64, at dk = 256 20 bytes a lane in scratch memory): 16 packed prompts of up to
+// 8192 tokens, 16 heads of 128 x 128, bf16, 487 us (972 MB, a copy takes 187).  8 prompts of 4096, 6
+// heads of 256 x 512: 192 workgroups, one to a CU, 7.9 us a chunk, 508 us (a copy takes 126).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -81,15 +85,25 @@ __device__ inline Segment segment(const LinearArgs& a, int slot) {
 // sums stay defined.
 __device__ inline float finite_log(float x) { return x < -1e4f ? -1e4f : x; }
 
-// Four rows of two accumulator tiles (bf16), or one element (fp32), as an operand.
-template <class E> __device__ inline typename Mfma<E>::frag operand(const f32x4* tiles, int stride, int kt);
-template <> __device__ inline bf16x8 operand<bf16>(const f32x4* t, int stride, int kt) {
-  const f32x4 x = t[2 * kt * stride], y = t[(2 * kt + 1) * stride];
-  return bf16x8{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3],
-                (bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
-}
-template <> __device__ inline float operand<float>(const f32x4* t, int stride, int kt) {
-  return t[(kt >> 2) * stride][kt & 3];
+// Four rows of two accumulator tiles (bf16), or one element (fp32), as an operand.  In bf16 as
+// two: part 0 is the value rounded, part 1 what that left over (2^-16 of the value is lost).
+// FINITE: part 1 of an infinity or NaN is 0.
+template <class E, int PART, bool FINITE>
+__device__ inline typename Mfma<E>::frag operand(const f32x4* t, int stride, int kt) {
+  if constexpr (sizeof(E) == 4) {
+    return t[(kt >> 2) * stride][kt & 3];
+  } else {
+    const f32x4 x = t[2 * kt * stride], y = t[(2 * kt + 1) * stride];
+    bf16x8 r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = j < 4 ? x[j & 3] : y[j & 3];
+      const bf16 hi = (bf16)v;
+      const float lo = v - (float)hi;
+      r[j] = PART == 0 ? hi : FINITE && !(fabsf(lo) < INFINITY) ? (bf16)0.f : (bf16)lo;
+    }
+    return r;
+  }
 }
 
 // Matrices in LDS.  In bf16 an operand read takes 8 bytes of each of 16 rows, a transposing one
@@ -228,7 +242,8 @@ void k_linear(LinearArgs a) {
   constexpr int PK = DK / EPP, PV = NV / EPP;  // pieces of a row
   constexpr int RK = 64 * PK / NTH, RV = 64 * PV / NTH;
   constexpr int KQ = DK / M::K / KS, KT = 64 / M::K, IT = DK / 16 / KS;
-  constexpr int BP = 64 * LP * (int)sizeof(E), BX = KS > 1 ? W * 2 * NC * 1024 : 0;
+  constexpr int PARTS = sizeof(E) == 2 ? 2 : 1;  // operands that stand for the state, or for P
+  constexpr int BP = PARTS * 64 * LP * (int)sizeof(E), BX = KS > 1 ? W * 2 * NC * 1024 : 0;
   // where LDS is short, P and the sums that waves exchange take the place of q, at the price
   // of a barrier
   constexpr bool OVER = OUT && 64 * (2 * LK + LV) * (int)sizeof(E) + BP + BX > 156 * 1024;
@@ -238,7 +253,7 @@ void k_linear(LinearArgs a) {
   __shared__ __align__(16) unsigned char more[OUT && !OVER ? BP + BX : 16];
   __shared__ Gates gates[2];
   __shared__ int sodd[2];
-  E* const sp = OVER ? sq : (E*)more;                                       // P [t][s]
+  E* const sp = OVER ? sq : (E*)more;                                       // P [part][t][s]
   f32x4* const sx = (f32x4*)((OVER ? (unsigned char*)sq : more) + BP);      // sums to add
   static_assert(!OVER || 64 * LK * (int)sizeof(E) >= BP + BX, "q's place is too small");
 
@@ -426,26 +441,68 @@ void k_linear(LinearArgs a) {
         for (int j = 0; j < CNT; ++j) {
           typename Raw4<E>::type y = {to_e<E>(p[j][0]), to_e<E>(p[j][1]), to_e<E>(p[j][2]),
                                       to_e<E>(p[j][3])};
-          *reinterpret_cast<typename Raw4<E>::type*>(row_part<E, LP>(sp, tt) + 16 * (s + j)) = y;
+          E* const to = row_part<E, LP>(sp, tt) + 16 * (s + j);
+          *reinterpret_cast<typename Raw4<E>::type*>(to) = y;
+          if constexpr (PARTS == 2) {
+            typename Raw4<E>::type z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float left = p[j][e] - to_f(y[e]);  // (of an infinity: nothing)
+              z[e] = to_e<E>(fabsf(left) < INFINITY ? left : 0.f);
+            }
+            *reinterpret_cast<typename Raw4<E>::type*>(to + 64 * LP) = z;
+          }
         }
       };
       // the entry state's part
       f32x4 o[4][NC];
-      auto from_state = [&]() {
+      auto state_part = [&](auto finite) {
+        constexpr bool FINITE = decltype(finite)::value;
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
           for (int c = 0; c < NC; ++c) o[tt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kt = 0; kt < KQ; ++kt) {
-          frag sf[NC];
+          frag sf[PARTS][NC];
 #pragma unroll
-          for (int c = 0; c < NC; ++c) sf[c] = operand<E>(&S[0][c], NC, kt);
+          for (int c = 0; c < NC; ++c) {
+            sf[0][c] = operand<E, 0, FINITE>(&S[0][c], NC, kt);
+            if constexpr (PARTS == 2) sf[1][c] = operand<E, 1, FINITE>(&S[0][c], NC, kt);
+          }
 #pragma unroll
           for (int tt = 0; tt < 4; ++tt) {
-            const frag q = row_operand<E>(row_part<E, LK>(sq, tt) + k0, kt);
+            frag q = row_operand<E>(row_part<E, LK>(sq, tt) + k0, kt);
 #pragma unroll
-            for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[c], q, o[tt][c]);
+            for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[0][c], q, o[tt][c]);
+            if constexpr (PARTS == 2) {
+              if constexpr (FINITE) q = without_odd(q);
+#pragma unroll
+              for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[1][c], q, o[tt][c]);
+            }
+          }
+        }
+      };
+      auto from_state = [&]() {
+        state_part(std::false_type{});
+        if constexpr (PARTS == 2) {
+          // An infinity of the state or of q meets the first parts alone: the second ones
+          // may be NaN, 0, or of the other sign.
+          float most = 0.f;  // (a NaN stays one)
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                most = __builtin_elementwise_maximum(most, fabsf(o[tt][c][e]));
+          if (__any(!(most < INFINITY))) {
+            // (opaque, or the first pass' operands are kept in registers for this one)
+#pragma unroll
+            for (int i = 0; i < IT; ++i)
+#pragma unroll
+              for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(S[i][c])::"memory");
+            state_part(std::true_type{});
           }
         }
       };
@@ -564,23 +621,26 @@ void k_linear(LinearArgs a) {
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
           const int tt = tile(j), most = KS == 1 ? j : 1 + 2 * j;  // (most: at compile time)
-          frag x[KT];
-          const E* const p = row_part<E, LP>(sp, tt);
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) x[kt] = row_operand<E>(p, kt);
+          for (int part = 0; part < PARTS; ++part) {
+            frag x[KT];
+            const E* const p = row_part<E, LP>(sp, tt) + part * 64 * LP;
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            // what is past the diagonal tile was not written
-            if constexpr (sizeof(E) == 2) {
-              if (2 * kt > most) continue;
-              const bf16x8 half = __builtin_shufflevector(x[kt], bf16x8{}, 0, 1, 2, 3, 8, 9, 10, 11);
-              x[kt] = 2 * kt < tt ? x[kt] : half;
-            } else {
-              if (kt / 4 > most) continue;
-              x[kt] = kt / 4 <= tt ? x[kt] : 0.f;
+            for (int kt = 0; kt < KT; ++kt) x[kt] = row_operand<E>(p, kt);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+              // what is past the diagonal tile was not written
+              if constexpr (sizeof(E) == 2) {
+                if (2 * kt > most) continue;
+                const bf16x8 half = __builtin_shufflevector(x[kt], bf16x8{}, 0, 1, 2, 3, 8, 9, 10, 11);
+                x[kt] = 2 * kt < tt ? x[kt] : half;
+              } else {
+                if (kt / 4 > most) continue;
+                x[kt] = kt / 4 <= tt ? x[kt] : 0.f;
+              }
+#pragma unroll
+              for (int c = 0; c < NC; ++c) mine[j][c] = M::mma(vf[kt][c], x[kt], mine[j][c]);
             }
-#pragma unroll
-            for (int c = 0; c < NC; ++c) mine[j][c] = M::mma(vf[kt][c], x[kt], mine[j][c]);
           }
         }
       } else {
@@ -591,7 +651,8 @@ void k_linear(LinearArgs a) {
 #pragma unroll 1
           for (int s = 0; s <= 16 * tt + c16; ++s) {
             const bool b = sizeof(E) == 2;
-            const float w = to_f(sp[(16 * tt + c16) * LP + (b ? s ^ 4 * units(c16) : s)]);
+            const E* const p = sp + (16 * tt + c16) * LP + (b ? s ^ 4 * units(c16) : s);
+            const float w = to_f(p[0]) + (PARTS == 2 ? to_f(p[(PARTS - 1) * 64 * LP]) : 0.f);
             const E* from = sv + s * LV + cw * 16 * NC + 4 * (b ? g ^ units(s) : g);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
