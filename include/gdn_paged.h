@@ -180,6 +180,9 @@ gdn_status gdn_cache_attn(const gdn_tokens *t, const gdn_attn *a, const gdn_rows
  * is at most max_blocks * page_size; with 0 it is gdn_cache_attn.
  * In bfloat16 p enters as two values where every sequence has few rows (at most 32), as
  * one otherwise.
+ * max_kv also says how the launch is shared out between the prefix and the sequences'
+ * own keys; with 0 these are taken to fill the table's room, and the prefix gets a
+ * quarter of the launch at least.
  * The workspace (gdn_cache_attn_shared_workspace_size bytes) holds the partial
  * results of the prefix and of the sequences' own keys. */
 size_t gdn_cache_attn_shared_workspace_size(const gdn_tokens *t, const gdn_cache *cache,

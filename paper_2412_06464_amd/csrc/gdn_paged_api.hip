@@ -320,7 +320,11 @@ gdn_status plan_shared(const gdn_tokens* t, const gdn::Tokens& tok, const gdn_ca
   const double hbm = std::max(0., own) * tok.N * t->Hk * t->d * 2 * size_of(t->dtype) / 5.3e6;  // us
   const double mma = (dt == Dt::F32 ? 4e-8 : (1 + p.parts) / 3e8) * rows * t->Hk * t->d * prefix;
   const double all = p.few || size_of(t->dtype) * t->d > 512 ? 256 : 512;
-  const int64_t want = (int64_t)(all * mma / (mma + hbm));
+  // Without max_kv the own keys are not known, and a quarter is the least, in ranges of 256 keys or more
+  // (in a table of 131072 tokens the first call above takes 93 us without max_kv, and 259 with the
+  // one range that the unused room would leave it).
+  const double least = a->max_kv > 0 ? 0. : std::min(all / 4, units * (prefix / 256.));
+  const int64_t want = (int64_t)std::max(all * mma / (mma + hbm), least);
   const int64_t most = std::min<int64_t>(gdn::MAX_SPLITS - p.own.splits, (prefix + step - 1) / step);
   const int64_t splits = std::max<int64_t>(1, std::min((want + units - 1) / std::max<int64_t>(1, units), most));
   p.len = (int)(((prefix + splits - 1) / splits + step - 1) / step * step);

@@ -378,7 +378,8 @@ def gdn_cache_attn_shared(q, k_pages, v_pages, table, kv_lens, prefix_table, pre
 
     ``prefix_table`` int32 [blocks]: the prefix's pages (a row of a table that holds it: what
     gdn_pages_select leaves in every fork of a prompt).  A sequence's own row of ``table`` is read
-    from the prefix's end on; kv_lens counts the prefix.  The rest as in gdn_cache_attn."""
+    from the prefix's end on; kv_lens counts the prefix.  The rest as in gdn_cache_attn (``max_kv``
+    also shares out the launch between the prefix and the sequences' own keys)."""
     if not isinstance(prefix_table, torch.Tensor):
         raise TypeError("prefix_table must be a tensor")
     return _attend(q, k_pages, v_pages, table, kv_lens, prefix_table, _prefix(prefix), scale,
