@@ -21,13 +21,13 @@
 //
 // In bf16 the entry state and P are operands as two values each (PARTS), so that o is off by its
 // own rounding alone; as one they left 1.4 times that, at 433 us of 487 for the packed prompts
-// below, 412 of 508 for the wide heads (P's second value 6%, the state's the rest).
+// below, 412 of 485 for the wide heads (P's second value 6%, the state's the rest).
 //
 // Bound by a wave's chain of products, exponentials and barriers for each chunk, two waves
 // to a SIMD (registers: 128 x 16 NC of the state, v and the outputs; the walks of 128 columns keep
 // 64, at dk = 256 20 bytes a lane in scratch memory): 16 packed prompts of up to
 // 8192 tokens, 16 heads of 128 x 128, bf16, 487 us (972 MB, a copy takes 187).  8 prompts of 4096, 6
-// heads of 256 x 512: 192 workgroups, one to a CU, 7.9 us a chunk, 508 us (a copy takes 126).
+// heads of 256 x 512: 192 workgroups, one to a CU, 7.6 us a chunk, 485 us (a copy takes 126).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -36,9 +36,11 @@
 
 namespace gdn {
 
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
@@ -85,25 +87,42 @@ __device__ inline Segment segment(const LinearArgs& a, int slot) {
 // sums stay defined.
 __device__ inline float finite_log(float x) { return x < -1e4f ? -1e4f : x; }
 
+// Two values as bf16 in a word, and what they left over.  (The word is opaque: the compiler would
+// convert each again for the difference.  Wide heads, below, 508 us -> 485; the weighted v's three
+// values, put this way, take registers that the walk does not have: 524.)
+__device__ inline unsigned rounded(float a, float b, float& left_a, float& left_b) {
+  const bf16x2 x = {(bf16)a, (bf16)b};
+  unsigned w = *reinterpret_cast<const unsigned*>(&x);
+  asm("" : "+v"(w));
+  left_a = a - __uint_as_float(w << 16);
+  left_b = b - __uint_as_float(w & 0xffff0000u);
+  return w;
+}
+__device__ inline unsigned rounded(float a, float b) {
+  const bf16x2 x = {(bf16)a, (bf16)b};
+  return *reinterpret_cast<const unsigned*>(&x);
+}
+__device__ inline float finite(float x) { return fabsf(x) < INFINITY ? x : 0.f; }
+
 // Four rows of two accumulator tiles (bf16), or one element (fp32), as an operand.  In bf16 as
-// two: part 0 is the value rounded, part 1 what that left over (2^-16 of the value is lost).
-// FINITE: part 1 of an infinity or NaN is 0.
-template <class E, int PART, bool FINITE>
-__device__ inline typename Mfma<E>::frag operand(const f32x4* t, int stride, int kt) {
-  if constexpr (sizeof(E) == 4) {
-    return t[(kt >> 2) * stride][kt & 3];
-  } else {
-    const f32x4 x = t[2 * kt * stride], y = t[(2 * kt + 1) * stride];
-    bf16x8 r;
+// two: the values rounded, and what that left over (2^-16 of the value is lost).  FINITE: of an
+// infinity or NaN nothing is left.
+template <bool FINITE>
+__device__ inline void operands(const f32x4* t, int stride, int kt, bf16x8 (&to)[2]) {
+  u32x4 hi, lo;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float v = j < 4 ? x[j & 3] : y[j & 3];
-      const bf16 hi = (bf16)v;
-      const float lo = v - (float)hi;
-      r[j] = PART == 0 ? hi : FINITE && !(fabsf(lo) < INFINITY) ? (bf16)0.f : (bf16)lo;
-    }
-    return r;
+  for (int j = 0; j < 4; ++j) {
+    const f32x4 x = t[(2 * kt + (j >> 1)) * stride];
+    float a, b;
+    hi[j] = rounded(x[2 * j & 3], x[2 * j + 1 & 3], a, b);
+    lo[j] = FINITE ? rounded(finite(a), finite(b)) : rounded(a, b);
   }
+  to[0] = *reinterpret_cast<const bf16x8*>(&hi);
+  to[1] = *reinterpret_cast<const bf16x8*>(&lo);
+}
+template <bool FINITE>
+__device__ inline void operands(const f32x4* t, int stride, int kt, float (&to)[1]) {
+  to[0] = t[(kt >> 2) * stride][kt & 3];
 }
 
 // Matrices in LDS.  In bf16 an operand read takes 8 bytes of each of 16 rows, a transposing one
@@ -439,18 +458,18 @@ void k_linear(LinearArgs a) {
         if constexpr (OVER) lds_barrier();
 #pragma unroll
         for (int j = 0; j < CNT; ++j) {
-          typename Raw4<E>::type y = {to_e<E>(p[j][0]), to_e<E>(p[j][1]), to_e<E>(p[j][2]),
-                                      to_e<E>(p[j][3])};
           E* const to = row_part<E, LP>(sp, tt) + 16 * (s + j);
-          *reinterpret_cast<typename Raw4<E>::type*>(to) = y;
-          if constexpr (PARTS == 2) {
-            typename Raw4<E>::type z;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float left = p[j][e] - to_f(y[e]);  // (of an infinity: nothing)
-              z[e] = to_e<E>(fabsf(left) < INFINITY ? left : 0.f);
-            }
-            *reinterpret_cast<typename Raw4<E>::type*>(to + 64 * LP) = z;
+          if constexpr (PARTS == 1) {
+            *reinterpret_cast<f32x4*>(to) = p[j];
+          } else {  // (of an infinity nothing is left over)
+            float r[4];
+            u32x2 y, z;
+            y[0] = rounded(p[j][0], p[j][1], r[0], r[1]);
+            y[1] = rounded(p[j][2], p[j][3], r[2], r[3]);
+            z[0] = rounded(finite(r[0]), finite(r[1]));
+            z[1] = rounded(finite(r[2]), finite(r[3]));
+            *reinterpret_cast<u32x2*>(to) = y;
+            *reinterpret_cast<u32x2*>(to + 64 * LP) = z;
           }
         }
       };
@@ -464,21 +483,18 @@ void k_linear(LinearArgs a) {
           for (int c = 0; c < NC; ++c) o[tt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kt = 0; kt < KQ; ++kt) {
-          frag sf[PARTS][NC];
+          frag sf[NC][PARTS];
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            sf[0][c] = operand<E, 0, FINITE>(&S[0][c], NC, kt);
-            if constexpr (PARTS == 2) sf[1][c] = operand<E, 1, FINITE>(&S[0][c], NC, kt);
-          }
+          for (int c = 0; c < NC; ++c) operands<FINITE>(&S[0][c], NC, kt, sf[c]);
 #pragma unroll
           for (int tt = 0; tt < 4; ++tt) {
             frag q = row_operand<E>(row_part<E, LK>(sq, tt) + k0, kt);
 #pragma unroll
-            for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[0][c], q, o[tt][c]);
+            for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[c][0], q, o[tt][c]);
             if constexpr (PARTS == 2) {
               if constexpr (FINITE) q = without_odd(q);
 #pragma unroll
-              for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[1][c], q, o[tt][c]);
+              for (int c = 0; c < NC; ++c) o[tt][c] = M::mma(sf[c][1], q, o[tt][c]);
             }
           }
         }

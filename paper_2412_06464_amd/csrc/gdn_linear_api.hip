@@ -52,7 +52,7 @@ gdn_status check_problem(const gdn_problem* p, LinearArgs* a) {
 }
 
 // What a chunk takes, in us: of a workgroup that has its CU to itself, of one of as many as
-// a CU holds, and how many those are.  (The weights of a choice: in bf16 a chunk takes 3 to 16%
+// a CU holds, and how many those are.  (The weights of a choice: in bf16 a chunk takes 3 to 15%
 // more, which added to these picks worse lengths for packed prompts, 512 for 1024.)
 struct Pace {
   double alone, full;
@@ -75,7 +75,7 @@ Pace pace(Dt dt, int dk, int slice) {
 // memory four times.  (us, whole | segments of 64, 128, 256, 512, 1024, 2048 tokens, * the rule's; bf16:
 // 16 packed prompts of up to 8192 tokens, 16 heads of 128 x 128, 899 | -, 795, 587, 515, 482*, 577; one
 // of 8192 820 | 158, 115, 88, 97*, 153, 284, of 512 54 | 28*, 32, 45, four of 300 37* | 37, 37, 51; 8 of
-// 4096, 6 heads of 256 x 512, 506* | -, -, 856, 673, 599, 634, one of 1000 119 | 66, 48*, 65, 101; fp32,
+// 4096, 6 heads of 256 x 512, 485* | -, -, 856, 673, 599, 634, one of 1000 119 | 66, 48*, 65, 101; fp32,
 // two of 1001, 4 heads of 64 x 64, 89 | 20*, 26, 41, 71.)
 size_t plan(const gdn_problem* p, LinearArgs* a) {
   const int slice = gdn::linear_slice(type_of(p->dtype), a->dk, a->dv);
