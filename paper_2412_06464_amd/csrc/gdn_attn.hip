@@ -840,7 +840,7 @@ __device__ inline void shared_range(const AttnArgs& a, Block<true>& b, unsigned 
 
 // The prefix's blocks, p.splits * p.Hk of them for each row block, and behind them those of the
 // sequences' own keys, in one launch: the first are bound by the matrix cores, the others by
-// HBM.  (256 single tokens, 8192 shared keys, up to 1000 of each: apart 37 and 65 us.)
+// HBM.  (256 single tokens, 8192 shared keys, up to 1000 of each: apart 66 and 74 us, together 85.)
 template <class E, int D, int QT, int KW, int KT>
 __global__ __launch_bounds__(64 * KW, 1) void k_attn_shared_few(AttnArgs p, AttnArgs a) {
   using C = AttnCfg<E, D, QT, 1, KW, KT>;
@@ -859,7 +859,7 @@ __global__ __launch_bounds__(64 * KW, 1) void k_attn_shared_few(AttnArgs p, Attn
 }
 
 // QT == 0: at most 16 rows a sequence, all four waves on its keys (256 single tokens, 8192 shared
-// keys, up to 1000 own: 92 us; by the tile kernel, with one wave of rows, 98).
+// keys, up to 1000 own: 85 us; by the tile kernel, with one wave of rows, 101).
 template <class E, int D, int QP, int QT, int KT, int PARTS>
 __global__ __launch_bounds__(256, sizeof(E) * D <= 512 ? 2 : 1) void k_attn_shared_tile(AttnArgs p,
                                                                                         AttnArgs a,
